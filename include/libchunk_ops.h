@@ -164,6 +164,48 @@ size_t lc_rmsnorm_scratch_bytes(int64_t T, int64_t d);
 #define LC_RMSNORM_NOALLOC_SCRATCH_BYTES ((size_t)16 << 20)
 lc_status lc_rmsnorm_backward_noalloc(const lc_norm_args *args, void *stream);
 
+/* ------------------------------------------------------------------ LayerNorm
+ * Forward over T rows of d, with gain g and bias b (b may be NULL: 0):
+ *   mean[t] = mean_k x[t,k],  rstd[t] = 1/sqrt(mean_k (x[t,k] - mean[t])^2 + eps)
+ *   y[t,k]  = (x[t,k] - mean[t]) * rstd[t] * g[k] + b[k]
+ * Backward, with xh = (x - mean) * rstd and dxh = dy * g:
+ *   dx[t,k] = dres[t,k] + rstd[t] * (dxh[t,k] - mean_k'(dxh) - xh[t,k] * mean_k'(dxh*xh))
+ *   dg_accum[k] += sum_t dy[t,k] * xh[t,k],  db_accum[k] += sum_t dy[t,k]
+ * (stored instead of added when store_dg is 1). Row t of a tensor starts at
+ * t * its leading dimension (0: rows of d, one after the other); mean and rstd
+ * are fp32 [T], dg_accum and db_accum fp32 [d], g and b have type w_dtype. dres
+ * may be NULL (0); dx_copy, if non-NULL, receives dx again as bf16 rows with
+ * dx's leading dimension; dg_accum and db_accum may each be NULL. All sums are
+ * fp32; the variance is summed from differences to the mean. The weight
+ * gradients are fixed-order reductions (partial sums of row blocks in `scratch`,
+ * lc_layernorm_scratch_bytes, needed only for them, then one ordered sum):
+ * run-to-run deterministic. Any T >= 0 (0: nothing happens) and d >= 1; rows
+ * that are whole 16-byte runs (d and the leading dimensions multiples of 8)
+ * are read and written in such runs.
+ * Overlap: y may lie over x, and dx over dy or dres, element for element (the
+ * same type and leading dimension); no other output may overlap a tensor that
+ * the call reads.
+ */
+typedef struct lc_layernorm_args {
+  int64_t T, d;
+  float eps;
+  int32_t x_dtype;     /* x */
+  int32_t w_dtype;     /* g, b */
+  int32_t out_dtype;   /* y (forward) or dx (backward) */
+  int32_t dy_dtype;    /* dy (backward) */
+  int32_t dres_dtype;  /* dres (backward) */
+  int32_t store_dg;
+  int32_t reserved;
+  const void *x; const void *g; const void *b; void *y; float *mean; float *rstd;
+  const void *dy; const void *dres; void *dx; void *dx_copy; float *dg_accum; float *db_accum;
+  int64_t ld_x, ld_y, ld_dy, ld_dres, ld_dx;
+  void *scratch; size_t scratch_bytes;
+} lc_layernorm_args;
+
+lc_status lc_layernorm_forward(const lc_layernorm_args *args, void *stream);
+lc_status lc_layernorm_backward(const lc_layernorm_args *args, void *stream);
+size_t lc_layernorm_scratch_bytes(int64_t T, int64_t d);
+
 /* ------------------------------------------------------------------ attention
  * Causal softmax attention per (batch row b, head h): for query i,
  *   o_i = sum_{j<=i} softmax_j(q_i.k_j / sqrt(hd)) v_j,
@@ -217,6 +259,102 @@ lc_status lc_attention_backward(const lc_attn_args *args, void *stream);
 size_t lc_attention_scratch_bytes(int32_t B, int32_t S, int32_t H);
 /* The backward's scratch with Hkv key/value heads (grouped-query attention). */
 size_t lc_attention_scratch_bytes_kv(int32_t B, int32_t S, int32_t H, int32_t Hkv);
+
+/* ------------------------------------------------------------------ sliding-window attention
+ * Causal attention of packed sequences in which a token sees the last `window`
+ * tokens of its sequence, itself included, and the first n_sink tokens of its
+ * sequence (the sinks), however far back. T rows hold B sequences one after the
+ * other: sequence b is rows [seq_offsets[b], seq_offsets[b + 1]), seq_offsets a
+ * device array of B + 1 nondecreasing int32 (equal ones: an empty sequence;
+ * values are clamped to [0, T]); NULL: B sequences of T / B rows each. Query row
+ * i of the sequence that starts at row s sees key row j when
+ *   s <= j <= i  and  (i - j < window  or  j < s + n_sink),
+ * so every row sees itself, and window >= the longest sequence is plain causal
+ * attention. Over the keys that it sees,
+ *   o_i = sum_j softmax_j(q_i.k_j / sqrt(hd)) v_j,
+ *   lse[h, i] = log sum_j exp(q_i.k_j / sqrt(hd))  (fp32 [H, T]).
+ * Element (i, h, e) of q sits at q[i*ld_q + h*hd + e], likewise the others with
+ * their own leading dimensions. Grouped-query attention: k, v, dk and dv have
+ * Hkv heads (0: H) and query head h uses key/value head h / (H / Hkv).
+ * Backward: the formulas of lc_attention_backward over the pairs above, given o
+ * and lse of the forward; dk and dv sum over the query heads of their group.
+ * A value in a place that a result does not depend on never reaches it, infinite
+ * and NaN ones included: later tokens, tokens behind the window, other sequences.
+ * Rows of no sequence (before seq_offsets[0], from seq_offsets[B] on) are left as
+ * they were in every output. Any T >= 0 (0: nothing happens); T < 2^30.
+ * Deterministic (no atomics). The backward's scratch
+ * (lc_window_attention_scratch_bytes, for the same arguments) needs no clearing.
+ * No output may overlap a tensor that the call reads.
+ * Types: matrix-core path: q, k, v LC_FP16 or LC_BF16 (`dtype`; forward
+ * products in that type), o, dout, dq, dk, dv LC_BF16 (gradient products in
+ * bf16), head_dim 64 or 128, leading dimensions multiples of 8. fp32 path:
+ * everything LC_FP32, even head_dim <= 128.
+ */
+typedef struct lc_window_attn_args {
+  int32_t dtype;       /* q, k, v */
+  int32_t o_dtype;     /* o, dout, dq, dk, dv */
+  int64_t T;           /* rows of every tensor */
+  int32_t B;           /* sequences, 1 .. 2^20 */
+  int32_t H, Hkv, hd;
+  int32_t window;      /* >= 1 */
+  int32_t n_sink;      /* >= 0 */
+  const int32_t *seq_offsets;
+  const void *q; int64_t ld_q; const void *k; int64_t ld_k; const void *v; int64_t ld_v;
+  void *o; int64_t ld_o; float *lse;
+  const void *dout; int64_t ld_dout;
+  void *dq; int64_t ld_dq; void *dk; int64_t ld_dk; void *dv; int64_t ld_dv;
+  void *scratch; size_t scratch_bytes;
+} lc_window_attn_args;
+
+lc_status lc_window_attention_forward(const lc_window_attn_args *args, void *stream);
+lc_status lc_window_attention_backward(const lc_window_attn_args *args, void *stream);
+size_t lc_window_attention_scratch_bytes(int32_t dtype, int64_t T, int32_t H, int32_t Hkv,
+                                         int32_t hd, int32_t window, int32_t n_sink);
+
+/* ------------------------------------------------------------------ rotary positions with several axes
+ * RoPE for tokens with a position on each of n_axes axes (text: one; images and
+ * video: time, height, width). A head's hd / 2 pairs (i, i + hd/2), in order, are
+ * dealt to the axes in sections: the first sections[0] pairs turn by the position
+ * on axis 0, the next sections[1] by that on axis 1, and so on; pairs past the
+ * sections' sum stay as they are. Token t's position on axis a is
+ * pos[a*ld_pos + t] (device, int32 of any sign, 4-byte aligned). A pair turns by
+ * position * f, where pair i of the head, pair j of its section, has
+ *   LC_ROPE_FREQ_HEAD  f = base^(-i / (hd/2))        (one run over the head)
+ *   LC_ROPE_FREQ_AXIS  f = base^(-j / sections[a])   (a whole run per axis)
+ * Angles are reduced exactly (fixed-point fractions of a turn), so far positions
+ * lose nothing; cos and sin are within 2^-23 of the exact ones.
+ * Forward: y = x rotated (a c - b s, b c + a s for the pair a, b) for every head
+ * of T rows, n_heads heads of hd values each, row t at t * ld_x (ld_y). Call it on
+ * q and k together (rows of H + Hkv heads) or one by one.
+ * Backward: the same with the angles negated (the transpose: x the gradient at
+ * the rotated rows, y the gradient at the raw ones).
+ * Table: cos, sin (fp32 [T, hd/2]) of every token and pair (1 and 0 for pairs past
+ * the sections). Given with rope_seq = T to lc_gemm's LC_EPI_ROPE, or with
+ * seq_len = T to lc_qk_norm_rope_forward, it makes those rotate by several axes.
+ * Overlap: y may lie over x, element for element (the same type and leading
+ * dimension). Any T >= 0 (0: nothing happens), 1 <= n_axes <= 4, even hd <= 256,
+ * 1 <= sum of sections <= hd/2, base >= 1.
+ */
+typedef enum lc_rope_freq { LC_ROPE_FREQ_HEAD = 0, LC_ROPE_FREQ_AXIS = 1 } lc_rope_freq;
+
+typedef struct lc_rope_axes_args {
+  int64_t T;
+  int32_t n_heads, hd;
+  int32_t x_dtype, y_dtype;
+  int32_t n_axes;
+  int32_t sections[4];
+  int32_t freq;        /* lc_rope_freq */
+  float base;
+  int32_t reserved;
+  const int32_t *pos; int64_t ld_pos;
+  const void *x; int64_t ld_x;
+  void *y; int64_t ld_y;
+  float *cos; float *sin;  /* table */
+} lc_rope_axes_args;
+
+lc_status lc_rope_axes_forward(const lc_rope_axes_args *args, void *stream);
+lc_status lc_rope_axes_backward(const lc_rope_axes_args *args, void *stream);
+lc_status lc_rope_axes_table(const lc_rope_axes_args *args, void *stream);
 
 /* ------------------------------------------------------------------ q/k norm
  * Qwen3-style per-head RMSNorm of q and k fused with RoPE, over T tokens of

@@ -38,6 +38,7 @@ LC_ORDER_WITH_NEXT = 0x100
 (LC_EPI_STORE, LC_EPI_STORE_F32, LC_EPI_ACCUM_F32, LC_EPI_RESIDUAL, LC_EPI_ROPE,
  LC_EPI_SWIGLU, LC_EPI_SWIGLU_BWD) = range(7)
 LC_GROUP_NONE, LC_GROUP_ROWS, LC_GROUP_K = 0, 1, 2
+LC_ROPE_FREQ_HEAD, LC_ROPE_FREQ_AXIS = 0, 1
 
 
 class LibchunkError(RuntimeError):
@@ -145,6 +146,40 @@ class lc_qknorm_args(C.Structure):
                 ("reserved", C.c_int32), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
 
 
+class lc_layernorm_args(C.Structure):
+    _fields_ = [("T", C.c_int64), ("d", C.c_int64), ("eps", C.c_float),
+                ("x_dtype", C.c_int32), ("w_dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("dy_dtype", C.c_int32), ("dres_dtype", C.c_int32), ("store_dg", C.c_int32),
+                ("reserved", C.c_int32), ("x", C.c_void_p), ("g", C.c_void_p), ("b", C.c_void_p),
+                ("y", C.c_void_p), ("mean", C.c_void_p), ("rstd", C.c_void_p),
+                ("dy", C.c_void_p), ("dres", C.c_void_p), ("dx", C.c_void_p),
+                ("dx_copy", C.c_void_p), ("dg_accum", C.c_void_p), ("db_accum", C.c_void_p),
+                ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_dy", C.c_int64),
+                ("ld_dres", C.c_int64), ("ld_dx", C.c_int64),
+                ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
+
+
+class lc_window_attn_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("o_dtype", C.c_int32), ("T", C.c_int64), ("B", C.c_int32),
+                ("H", C.c_int32), ("Hkv", C.c_int32), ("hd", C.c_int32), ("window", C.c_int32),
+                ("n_sink", C.c_int32), ("seq_offsets", C.c_void_p),
+                ("q", C.c_void_p), ("ld_q", C.c_int64), ("k", C.c_void_p), ("ld_k", C.c_int64),
+                ("v", C.c_void_p), ("ld_v", C.c_int64), ("o", C.c_void_p), ("ld_o", C.c_int64),
+                ("lse", C.c_void_p), ("dout", C.c_void_p), ("ld_dout", C.c_int64),
+                ("dq", C.c_void_p), ("ld_dq", C.c_int64), ("dk", C.c_void_p), ("ld_dk", C.c_int64),
+                ("dv", C.c_void_p), ("ld_dv", C.c_int64),
+                ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
+
+
+class lc_rope_axes_args(C.Structure):
+    _fields_ = [("T", C.c_int64), ("n_heads", C.c_int32), ("hd", C.c_int32),
+                ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("n_axes", C.c_int32),
+                ("sections", C.c_int32 * 4), ("freq", C.c_int32), ("base", C.c_float),
+                ("reserved", C.c_int32), ("pos", C.c_void_p), ("ld_pos", C.c_int64),
+                ("x", C.c_void_p), ("ld_x", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("cos", C.c_void_p), ("sin", C.c_void_p)]
+
+
 # name -> (restype, argtypes)
 _SIGS = {
     "lc_last_error": (C.c_char_p, []),
@@ -208,6 +243,16 @@ _SIGS = {
     "lc_qk_norm_rope_forward": (C.c_int, [C.POINTER(lc_qknorm_args), C.c_void_p]),
     "lc_qk_norm_rope_backward": (C.c_int, [C.POINTER(lc_qknorm_args), C.c_void_p]),
     "lc_qk_norm_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int32]),
+    "lc_layernorm_forward": (C.c_int, [C.POINTER(lc_layernorm_args), C.c_void_p]),
+    "lc_layernorm_backward": (C.c_int, [C.POINTER(lc_layernorm_args), C.c_void_p]),
+    "lc_layernorm_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
+    "lc_window_attention_forward": (C.c_int, [C.POINTER(lc_window_attn_args), C.c_void_p]),
+    "lc_window_attention_backward": (C.c_int, [C.POINTER(lc_window_attn_args), C.c_void_p]),
+    "lc_window_attention_scratch_bytes": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int32, C.c_int32,
+                                                       C.c_int32, C.c_int32, C.c_int32]),
+    "lc_rope_axes_forward": (C.c_int, [C.POINTER(lc_rope_axes_args), C.c_void_p]),
+    "lc_rope_axes_backward": (C.c_int, [C.POINTER(lc_rope_axes_args), C.c_void_p]),
+    "lc_rope_axes_table": (C.c_int, [C.POINTER(lc_rope_axes_args), C.c_void_p]),
     "lc_cast_bf16": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "lc_moe_route": (C.c_int, [C.POINTER(lc_moe_args), C.c_void_p]),
     "lc_moe_dispatch": (C.c_int, [C.POINTER(lc_moe_args), C.c_void_p]),
@@ -582,6 +627,79 @@ def lc_attention_backward(dtype, o_dtype, B, S, H, hd, q, k, v, ld_qkv, o, dout,
               ld_dqkv=ld_dqkv, rope_cos=rope_cos, rope_sin=rope_sin, scratch=scratch,
               scratch_bytes=scratch_bytes, Hkv=Hkv, qkv_bf16=qkv_bf16, ld_qkv_bf16=ld_qkv_bf16)
     return _check(lib().lc_attention_backward(C.byref(a), C.c_void_p(stream_ptr(stream) or None)))
+
+
+def lc_layernorm_scratch_bytes(T, d) -> int:
+    return int(lib().lc_layernorm_scratch_bytes(T, d))
+
+
+def lc_layernorm_forward(T, d, x, g, b, eps, y, mean, rstd, x_dtype, w_dtype, out_dtype, ld_x=0,
+                         ld_y=0, stream=None):
+    """LayerNorm with gain g and bias b (None: 0); leading dimensions of 0 mean rows of d."""
+    a = lc_layernorm_args(T, d, eps, x_dtype, w_dtype, out_dtype, 0, 0, 0, 0, ptr(x), ptr(g), ptr(b),
+                          ptr(y), ptr(mean), ptr(rstd), 0, 0, 0, 0, 0, 0, ld_x, ld_y)
+    return _check(lib().lc_layernorm_forward(C.byref(a), stream_ptr(stream)))
+
+
+def lc_layernorm_backward(T, d, dy, x, mean, rstd, g, dres, dx, dg_accum, db_accum, scratch,
+                          scratch_bytes, dy_dtype, x_dtype, w_dtype, dres_dtype, out_dtype,
+                          dx_copy=None, store_dg=0, ld_x=0, ld_dy=0, ld_dres=0, ld_dx=0, stream=None):
+    a = lc_layernorm_args(T, d, 0.0, x_dtype, w_dtype, out_dtype, dy_dtype, dres_dtype, store_dg, 0,
+                          ptr(x), ptr(g), 0, 0, ptr(mean), ptr(rstd), ptr(dy), ptr(dres), ptr(dx),
+                          ptr(dx_copy), ptr(dg_accum), ptr(db_accum), ld_x, 0, ld_dy, ld_dres, ld_dx,
+                          ptr(scratch), scratch_bytes)
+    return _check(lib().lc_layernorm_backward(C.byref(a), stream_ptr(stream)))
+
+
+def lc_window_attention_scratch_bytes(dtype, T, H, Hkv, hd, window, n_sink) -> int:
+    return int(lib().lc_window_attention_scratch_bytes(dtype, T, H, Hkv, hd, window, n_sink))
+
+
+def lc_window_attention_forward(dtype, o_dtype, T, B, seq_offsets, H, Hkv, hd, window, n_sink, q, ld_q,
+                                k, ld_k, v, ld_v, o, ld_o, lse, stream=None):
+    """Sliding-window attention with sinks over B packed sequences (seq_offsets: device
+    int32 [B + 1], or None: equal sequences)."""
+    a = lc_window_attn_args(dtype, o_dtype, T, B, H, Hkv, hd, window, n_sink, ptr(seq_offsets), ptr(q),
+                            ld_q, ptr(k), ld_k, ptr(v), ld_v, ptr(o), ld_o, ptr(lse))
+    return _check(lib().lc_window_attention_forward(C.byref(a), stream_ptr(stream)))
+
+
+def lc_window_attention_backward(dtype, o_dtype, T, B, seq_offsets, H, Hkv, hd, window, n_sink, q, ld_q,
+                                 k, ld_k, v, ld_v, o, ld_o, lse, dout, ld_dout, dq, ld_dq, dk, ld_dk,
+                                 dv, ld_dv, scratch, scratch_bytes, stream=None):
+    a = lc_window_attn_args(dtype, o_dtype, T, B, H, Hkv, hd, window, n_sink, ptr(seq_offsets), ptr(q),
+                            ld_q, ptr(k), ld_k, ptr(v), ld_v, ptr(o), ld_o, ptr(lse), ptr(dout), ld_dout,
+                            ptr(dq), ld_dq, ptr(dk), ld_dk, ptr(dv), ld_dv, ptr(scratch), scratch_bytes)
+    return _check(lib().lc_window_attention_backward(C.byref(a), stream_ptr(stream)))
+
+
+def _rope_axes(fn, T, n_heads, hd, sections, pos, ld_pos, base, freq, x=None, ld_x=0, y=None, ld_y=0,
+               x_dtype=LC_FP32, y_dtype=LC_FP32, cos=None, sin=None, stream=None):
+    n = len(sections)  # (a fifth axis and more is the library's to refuse)
+    a = lc_rope_axes_args(T, n_heads, hd, x_dtype, y_dtype, n, (C.c_int32 * 4)(*sections[:4]), freq, base,
+                          0, ptr(pos), ld_pos, ptr(x), ld_x, ptr(y), ld_y, ptr(cos), ptr(sin))
+    return _check(fn(C.byref(a), stream_ptr(stream)))
+
+
+def lc_rope_axes_forward(T, n_heads, hd, sections, pos, ld_pos, x, ld_x, y, ld_y, x_dtype, y_dtype,
+                         base=10000.0, freq=LC_ROPE_FREQ_HEAD, stream=None):
+    """Rotates head rows by positions on several axes (sections: pairs per axis)."""
+    return _rope_axes(lib().lc_rope_axes_forward, T, n_heads, hd, sections, pos, ld_pos, base, freq, x,
+                      ld_x, y, ld_y, x_dtype, y_dtype, stream=stream)
+
+
+def lc_rope_axes_backward(T, n_heads, hd, sections, pos, ld_pos, x, ld_x, y, ld_y, x_dtype, y_dtype,
+                          base=10000.0, freq=LC_ROPE_FREQ_HEAD, stream=None):
+    """The transpose of lc_rope_axes_forward: rotates gradients back."""
+    return _rope_axes(lib().lc_rope_axes_backward, T, n_heads, hd, sections, pos, ld_pos, base, freq, x,
+                      ld_x, y, ld_y, x_dtype, y_dtype, stream=stream)
+
+
+def lc_rope_axes_table(T, hd, sections, pos, ld_pos, cos, sin, base=10000.0, freq=LC_ROPE_FREQ_HEAD,
+                       stream=None):
+    """cos and sin [T, hd/2] of every token's pairs."""
+    return _rope_axes(lib().lc_rope_axes_table, T, 1, hd, sections, pos, ld_pos, base, freq, cos=cos,
+                      sin=sin, stream=stream)
 
 
 def lc_qk_norm_rope_forward(T, H, Hkv, hd, seq_len, eps, qk, ld, raw, rstd, gq, gk, x_dtype,

@@ -1,0 +1,104 @@
+"""LayerNorm, the projection, rotary positions of three axes and sliding-window attention as
+a layer's attention half uses them, forward and backward, on a packed batch with a padded end,
+against float64 with autograd.
+
+Tolerance: every tensor between the operators is rounded to bf16 once (half a step, 2^-8); the
+forward passes five of them (n, qkv, rotated qkv, o, weights), the backward five more, each
+adding in squares: sqrt(10) * 2^-8 * (their mean of 0.6 of a half step) < 2^-7 forward, and twice
+that backward."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_11169_amd import libchunk as lc
+from tests.gpu_util import DEV, banner
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = lc.LC_FP32, lc.LC_BF16
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_attention_half_of_a_layer(fused):
+    banner(f"layer forms fused={fused}")
+    g = torch.Generator(device=DEV)
+    g.manual_seed(21)
+    lens, tail, H, Hkv, hd, W, S = [150, 1, 210], 7, 4, 2, 128, 64, 4
+    T, d, cols, rc = sum(lens) + tail, 512, (H + 2 * Hkv) * hd, (H + Hkv) * hd
+    sections, base = [16, 24, 24], 1e6
+    off = torch.tensor([0, 150, 151, 361], dtype=torch.int32, device=DEV)
+    pos = torch.randint(0, 500, (3, T), generator=g, device=DEV, dtype=torch.int32)
+    x = torch.randn((T, d), generator=g, device=DEV)
+    dy = torch.randn((T, d), generator=g, device=DEV)
+    dy[sum(lens):] = 0
+    gain, bias = 1 + 0.1 * torch.randn(d, generator=g, device=DEV), 0.1 * torch.randn(d, generator=g, device=DEV)
+    w = (torch.randn((cols, d), generator=g, device=DEV) * d ** -0.5).to(torch.bfloat16)
+    wo = (torch.randn((d, H * hd), generator=g, device=DEV) * d ** -0.5).to(torch.bfloat16)
+    bf = dict(dtype=torch.bfloat16, device=DEV)
+
+    # forward
+    n, mean, rstd = torch.empty((T, d), **bf), torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+    lc.lc_layernorm_forward(T, d, x, gain, bias, 1e-5, n, mean, rstd, F32, F32, BF16)
+    qkv = torch.empty((T, cols), **bf)
+    if fused:
+        cos, sin = (torch.empty((T, hd // 2), device=DEV) for _ in range(2))
+        lc.lc_rope_axes_table(T, hd, sections, pos, T, cos, sin, base=base)
+        lc.lc_gemm(BF16, lc.LC_EPI_ROPE, T, cols, d, n, d, 1, w, d, 1, qkv, cols, rope_cos=cos, rope_sin=sin,
+                   rope_seq=T, rope_cols=rc, head_dim=hd)
+    else:
+        lc.lc_gemm(BF16, lc.LC_EPI_STORE, T, cols, d, n, d, 1, w, d, 1, qkv, cols)
+        lc.lc_rope_axes_forward(T, H + Hkv, hd, sections, pos, T, qkv, cols, qkv, cols, BF16, BF16, base=base)
+    q, k, v = qkv, qkv[:, H * hd:], qkv[:, rc:]
+    o, lse = torch.zeros((T, H * hd), **bf), torch.empty((H, T), device=DEV)
+    lc.lc_window_attention_forward(BF16, BF16, T, 3, off, H, Hkv, hd, W, S, q, cols, k, cols, v, cols, o, H * hd, lse)
+    y = torch.empty((T, d), device=DEV)
+    lc.lc_gemm(BF16, lc.LC_EPI_RESIDUAL, T, d, H * hd, o, H * hd, 1, wo, H * hd, 1, y, d, R=x, ldr=d, c_dtype=F32,
+               r_dtype=F32)
+    # backward
+    dy16, do = dy.to(torch.bfloat16), torch.empty((T, H * hd), **bf)
+    lc.lc_gemm(BF16, lc.LC_EPI_STORE, T, H * hd, d, dy16, d, 1, wo, H * hd, 0, do, H * hd)
+    dqkv = torch.zeros((T, cols), **bf)
+    nb = lc.lc_window_attention_scratch_bytes(BF16, T, H, Hkv, hd, W, S)
+    scratch = torch.empty(nb, dtype=torch.uint8, device=DEV)
+    lc.lc_window_attention_backward(BF16, BF16, T, 3, off, H, Hkv, hd, W, S, q, cols, k, cols, v, cols, o, H * hd, lse,
+                                    do, H * hd, dqkv, cols, dqkv[:, H * hd:], cols, dqkv[:, rc:], cols, scratch, nb)
+    lc.lc_rope_axes_backward(T, H + Hkv, hd, sections, pos, T, dqkv, cols, dqkv, cols, BF16, BF16, base=base)
+    dn = torch.empty((T, d), device=DEV)
+    lc.lc_gemm(BF16, lc.LC_EPI_STORE_F32, T, d, cols, dqkv, cols, 1, w, d, 0, dn, d)
+    # (a product over the batch's rows wants a multiple of 8: 368)
+    dw = torch.zeros((cols, d), device=DEV)
+    lc.lc_gemm(BF16, lc.LC_EPI_ACCUM_F32, cols, d, T, dqkv, cols, 0, n, d, 0, dw, d)
+    dx, dg, db = torch.empty((T, d), device=DEV), torch.zeros(d, device=DEV), torch.zeros(d, device=DEV)
+    ns = lc.lc_layernorm_scratch_bytes(T, d)
+    sc = torch.empty(ns, dtype=torch.uint8, device=DEV)
+    lc.lc_layernorm_backward(T, d, dn, x, mean, rstd, gain, dy, dx, dg, db, sc, ns, F32, F32, F32, F32, F32)
+    torch.cuda.synchronize()
+
+    # float64, on the CPU
+    X, Gn, Bn, Wq = (t.double().cpu().requires_grad_() for t in (x, gain, bias, w))
+    mu = X.mean(1, keepdim=True)
+    N = (X - mu) * ((X - mu).square().mean(1, keepdim=True) + 1e-5).rsqrt() * Gn + Bn
+    Z = (N @ Wq.T).view(T, H + 2 * Hkv, hd)
+    ang = torch.zeros((T, hd // 2), dtype=torch.float64)
+    for i in range(hd // 2):
+        ang[:, i] = pos[0 if i < 16 else 1 if i < 40 else 2].double().cpu() * base ** (-i / (hd // 2))
+    c, s = torch.cos(ang)[:, None], torch.sin(ang)[:, None]
+    a, b = Z[:, :H + Hkv, :64], Z[:, :H + Hkv, 64:]
+    R = torch.cat([a * c - b * s, b * c + a * s], 2)
+    Q, K, V = R[:, :H], R[:, H:].repeat_interleave(H // Hkv, 1), Z[:, H + Hkv:].repeat_interleave(H // Hkv, 1)
+    st = torch.repeat_interleave(torch.tensor([0, 150, 151, 361]), torch.tensor([150, 1, 210, tail]))
+    i, j = torch.arange(T)[:, None], torch.arange(T)[None, :]
+    see = (j <= i) & (j >= st[:, None]) & ((i - j < W) | (j < st[:, None] + S))
+    sc = torch.einsum("ihe,jhe->hij", Q, K) / math.sqrt(hd)
+    P = torch.softmax(sc.masked_fill(~see, -math.inf), -1)
+    O = torch.einsum("hij,jhe->ihe", P, V).reshape(T, H * hd)
+    live = (torch.arange(T) < sum(lens)).double()[:, None]
+    Y = X + (O * live) @ wo.double().cpu().T
+    (Y * dy.double().cpu()).sum().backward()
+
+    def rel(a, b):
+        return float((a.double().cpu() - b).norm() / b.norm())
+
+    assert rel(y, Y.detach()) < 2.0 ** -7
+    assert rel(dx, X.grad) < 2.0 ** -6 and rel(dw, Wq.grad) < 2.0 ** -6
+    assert rel(dg, Gn.grad) < 2.0 ** -6 and rel(db, Bn.grad) < 2.0 ** -6
