@@ -288,7 +288,7 @@ size_t lc_attention_scratch_bytes_kv(int32_t B, int32_t S, int32_t H, int32_t Hk
  * Types: matrix-core path: q, k, v LC_FP16 or LC_BF16 (`dtype`; forward
  * products in that type), o, dout, dq, dk, dv LC_BF16 (gradient products in
  * bf16), head_dim 64 or 128, leading dimensions multiples of 8. fp32 path:
- * everything LC_FP32, even head_dim <= 128.
+ * everything LC_FP32, even head_dim <= 128. Leading dimensions up to 2^24.
  */
 typedef struct lc_window_attn_args {
   int32_t dtype;       /* q, k, v */

@@ -41,6 +41,7 @@ EXTRA_FLAGS = {
     # them with vector instructions, and accumulation-register copies cost more
     # than they save
     "k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "k_attn_window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

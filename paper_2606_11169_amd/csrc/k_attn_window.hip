@@ -1,146 +1,895 @@
-// Sliding-window causal attention with sinks over packed sequences: one wave per
-// query (key) row and head, the head's features over its lanes.
-#include "common.hpp"
+// Sliding-window causal attention with sinks over packed sequences on CDNA4 matrix cores
+// (head_dim 64 or 128, fp16 or bf16 q/k/v, fp32 softmax and accumulation), forward and
+// backward. The fp32 path is k_attn_window_f32.hip.
+//
+// The products, the online softmax and the LDS row tiles are those of causal attention
+// (k_attn.hip): S^T = K Q^T with one query per lane pair, O^T += V^T P^T with the score
+// registers as operand; backward dQ^T += K^T dS^T over keys, dV^T += dO^T P and dK^T += Q^T dS
+// over queries, P recomputed from the log-sum-exp, gradient products in bf16.
+//
+// Work is laid over the packed rows, not over the sequences: a workgroup owns consecutive
+// rows whatever sequences they belong to, each row knows its sequence's start (a search
+// over the offsets, 64 per step), and the visible keys of a workgroup's rows are two runs
+// of 64-row blocks: the first row's sinks, then everything from the first row's window on
+// (sequences that start inside the workgroup's rows lie in the second run as a whole). So a
+// grid has no empty workgroups however ragged the batch, and many short sequences share one.
+//
+// Masks: query i sees key j in [wlo_i, i] or [start_i, start_i + ns_i) (its window, and
+// its sinks before the window); seen from key j the queries are [j, hi_j). Each is one
+// unsigned comparison per pair, made only in blocks where some pair of the wave is masked.
+//
+// A masked pair has weight 0, but 0 times an infinite or NaN value is NaN. Where a
+// workgroup's result is not finite it makes a second pass with the second products of its
+// masked blocks pair by pair, leaving out the masked ones: a value that a result does not
+// depend on never reaches it, and finite data pay one look at the result.
+#include "attn_tiles.hpp"
+#include "attn_window.hpp"
 
 #include <math.h>
 
 namespace lc {
 namespace {
 
-constexpr int NTH = 256;
-constexpr int MAXHD = 128;
+constexpr int KB = 64;         // keys (or queries) per inner block
+constexpr int KV_ROWS = 128;   // keys per dK/dV workgroup
+constexpr int MAXSINK = 256;   // sinks whose dK/dV work is split over chunks of queries
+
+// ---------------------------------------------------------------- row tiles
+// [64 rows][HD] tiles of 2-byte elements in HD / 8 load runs (one wave instruction each,
+// 16 bytes per lane, lanes of a row in address order). HD = 128: run q holds rows f(q) + 16 p,
+// p = 0..3, f swapping bit pairs (k_attn.hip). HD = 64: run q holds the rows whose bit 0 is
+// bit 2 of q and whose bits 2, 3 are its bits 0, 1; p gives bits 1, 4, 5. In both, 16
+// consecutive rows of one 16-byte chunk, and four consecutive rows of 64 bytes, touch every
+// bank once, rows 16 on sit 256 bytes on and rows 8 on two runs on, so that fragment
+// addresses are a per-lane base plus immediates.
+template <int HD> struct Tile {
+  static constexpr int NR = HD / 8;
+  static constexpr int BYTES = NR * RUNB;
+  __device__ __forceinline__ static int lane_row(int lane) {  // row of a run that a lane brings
+    return HD == 128 ? 16 * (lane >> 4) : ((lane >> 3 & 1) << 1) + ((lane >> 4) << 4);
+  }
+  __device__ __forceinline__ static int lane_chunk(int lane) { return lane & (HD / 8 - 1); }
+  __device__ __forceinline__ static int run_row(int run) {
+    return HD == 128 ? ((run & 3) << 2) | ((run >> 2) & 3) : ((run >> 2) & 1) + ((run & 3) << 2);
+  }
+  __device__ __forceinline__ static int row_off(int r) {  // byte offset of tile row r
+    return HD == 128 ? (((r & 3) << 2) | ((r >> 2) & 3)) * RUNB + (r >> 4) * 256
+                     : (((r & 1) << 2) | ((r >> 2) & 3)) * RUNB + ((r >> 1) & 1) * 128 + (r >> 4) * 256;
+  }
+  // MFMA operand of 32 rows: + (row0 / 16) * 256 + 32 s (columns 16 s + 8 (lane / 32))
+  __device__ __forceinline__ static uint32_t rows_lane(int lane) {
+    return (uint32_t)(row_off(lane & 31) + (lane >> 5) * 16);
+  }
+  // MFMA operand of 32 columns in an accumulator's row order (frag_cols_x)
+  __device__ __forceinline__ static uint32_t cols_lane(int lane) {
+    const int i16 = lane & 15, hf = lane >> 5, b4 = (lane >> 4) & 1;
+    return (uint32_t)(row_off(4 * hf + (i16 >> 2)) + (16 * b4 + 4 * (i16 & 3)) * 2);
+  }
+};
+
+template <typename VT>
+__device__ __forceinline__ VT frag_at(const lds_t *t) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) VT *>(t);
+}
+
+// A [64][HD] block of rows from row r0 of a matrix on (fewer at its end: rows past the last
+// read as zero), one buffer per block, so that offsets stay 32-bit in matrices of any size
+template <int HD>
+__device__ __forceinline__ i32x4_v block_rsrc(const void *base, int64_t ld, int col0, int r0, int T) {
+  const int rows = min(KB, T - r0);
+  return make_rsrc(static_cast<const char *>(base) + ((int64_t)r0 * ld + col0) * 2,
+                   (uint32_t)(((int64_t)(rows - 1) * ld + HD) * 2));
+}
 
 struct WinP {
-  const void *q, *k, *v, *dout;
-  void *o, *dq, *dk, *dv;
-  float *lse, *D;
+  const void *q, *k, *v;
+  __bf16 *o;
+  float *lse;
+  const __bf16 *dout;
+  __bf16 *dq, *dk, *dv;
+  const __bf16 *qb, *kb, *vb;  // bf16 rows for the gradient products (copies for fp16 inputs)
+  __bf16 *qb_w, *kb_w, *vb_w;  // where the copies are written (null: none)
+  float *D, *nl2;              // [H, T]: rowsum(dO * O) and -lse log2(e)
+  float *share, *slots;
   const int32_t *off;
-  int64_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
-  int T, B, H, Hkv, G, hd, window, n_sink, dt, o_dt;
+  int64_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv, ld_qb, ld_kb, ld_vb;
+  int T, B, S, H, Hkv, G, window, n_sink;
+  int gh, nq;                  // forward, dQ: heads per workgroup, blocks of query rows
+  int GP, parts;               // dK/dV: query heads per workgroup
+  int chunk, chunks;
+  int nmain, nsplit, nkb;      // dK/dV workgroups; 128-key blocks that hold a sequence's sinks
   float scale;
 };
 
-__device__ __forceinline__ float ld1(const void *base, int64_t i, int dt) {
-  if (dt == LC_FP32) return static_cast<const float *>(base)[i];
-  if (dt == LC_BF16) return (float)static_cast<const __bf16 *>(base)[i];
-  return (float)static_cast<const _Float16 *>(base)[i];
-}
-__device__ __forceinline__ void st1(void *base, int64_t i, int dt, float v) {
-  if (dt == LC_FP32) static_cast<float *>(base)[i] = v;
-  else static_cast<__bf16 *>(base)[i] = (__bf16)v;
+// Workgroups are handed to the 8 XCDs in turn; each XCD gets a consecutive run of the n
+// tasks (neighbouring row blocks of the same heads read the same keys: one L2 holds them).
+// -1: no task.
+__device__ __forceinline__ int xcd_task(int i, int n) {
+  const int per = (n + 7) >> 3, t = (i & 7) * per + (i >> 3);
+  return (i >> 3) < per && t < n ? t : -1;
 }
 
-__device__ __forceinline__ int offset_at(const WinP &p, int b) {
-  return p.off ? min(max(p.off[b], 0), p.T) : b * (p.T / p.B);
+__device__ __forceinline__ int wave_min32(int x) {  // over lanes alike in both halves
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o, 64));
+  return __builtin_amdgcn_readfirstlane(x);
 }
-// the rows [start, end) of the sequence that holds row i (start = end: none)
-__device__ __forceinline__ void sequence_of(const WinP &p, int i, int &start, int &end) {
-  int lo = 0, hi = p.B;  // offset_at(lo) <= i < offset_at(hi) once narrowed
-  start = end = 0;
-  if (i < offset_at(p, 0) || i >= offset_at(p, p.B)) return;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (offset_at(p, mid) <= i) lo = mid;
-    else hi = mid;
-  }
-  start = offset_at(p, lo);
-  end = offset_at(p, hi);
+__device__ __forceinline__ int wave_max32(int x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o, 64));
+  return __builtin_amdgcn_readfirstlane(x);
 }
 
-struct Row2 { float a, b; };
-__device__ __forceinline__ Row2 row2(const void *base, int64_t at, int dt, int hd, int lane) {
-  Row2 r = {0.0f, 0.0f};
-  if (lane < hd) r.a = ld1(base, at + lane, dt);
-  if (lane + 64 < hd) r.b = ld1(base, at + lane + 64, dt);
-  return r;
-}
-__device__ __forceinline__ void put2(void *base, int64_t at, int dt, int hd, int lane, Row2 r) {
-  if (lane < hd) st1(base, at + lane, dt, r.a);
-  if (lane + 64 < hd) st1(base, at + lane + 64, dt, r.b);
-}
-__device__ __forceinline__ float dot2(Row2 x, Row2 y) { return wave_sum(x.a * y.a + x.b * y.b); }
-
-// calls f(j) for every key that row i sees
-template <typename F>
-__device__ __forceinline__ void keys_of(const WinP &p, int i, int start, F f) {
-  const int w0 = max(start, i - p.window + 1 > i ? start : i - p.window + 1);
-  for (int j = start; j < w0 && j - start < p.n_sink; ++j) f(j);
-  for (int j = w0; j <= i; ++j) f(j);
+// whether some accumulator is infinite or NaN
+template <int NI>
+__device__ __forceinline__ bool not_finite(const f32x16_v (&a)[NI]) {
+  float t = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t = __builtin_fmaf(a[i][r], 0.0f, t);
+  return t != t;
 }
 
-template <bool DQ>
-__global__ __launch_bounds__(NTH) void window_rows_kernel(WinP p) {
-  const int lane = threadIdx.x & 63, h = blockIdx.y, kvh = h / p.G;
-  const int i = (int)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= p.T) return;
-  int start, end;
-  sequence_of(p, i, start, end);
-  if (start == end) return;
-  const int64_t hq = (int64_t)h * p.hd, hk = (int64_t)kvh * p.hd;
-  const Row2 q = row2(p.q, i * p.ld_q + hq, p.dt, p.hd, lane);
-  const int64_t si = (int64_t)h * p.T + i;
-  Row2 acc = {0.0f, 0.0f};
-  if constexpr (!DQ) {
-    float m = -INFINITY, l = 0.0f;
-    keys_of(p, i, start, [&](int j) {
-      const float s = dot2(q, row2(p.k, j * p.ld_k + hk, p.dt, p.hd, lane)) * p.scale;
-      const Row2 v = row2(p.v, j * p.ld_v + hk, p.dt, p.hd, lane);
-      const float mn = fmaxf(m, s), mu = mn == -INFINITY ? 0.0f : mn;
-      const float alpha = expf(m - mu), w = expf(s - mu);
-      acc.a = acc.a * alpha + w * v.a;
-      acc.b = acc.b * alpha + w * v.b;
-      l = l * alpha + w;
-      m = mn;
-    });
-    acc.a /= l;
-    acc.b /= l;
-    put2(p.o, i * p.ld_o + hq, p.o_dt, p.hd, lane, acc);
-    if (lane == 0) p.lse[si] = m + logf(l);
-  } else {
-    const Row2 d = row2(p.dout, i * p.ld_do + hq, p.o_dt, p.hd, lane);
-    const float D = dot2(d, row2(p.o, i * p.ld_o + hq, p.o_dt, p.hd, lane)), L = p.lse[si];
-    if (lane == 0) p.D[si] = D;
-    keys_of(p, i, start, [&](int j) {
-      const Row2 k = row2(p.k, j * p.ld_k + hk, p.dt, p.hd, lane);
-      const float s = dot2(q, k) * p.scale, dp = dot2(d, row2(p.v, j * p.ld_v + hk, p.dt, p.hd, lane));
-      const float ds = expf(s - L) * (dp - D) * p.scale;
-      acc.a += ds * k.a;
-      acc.b += ds * k.b;
-    });
-    put2(p.dq, i * p.ld_dq + hq, p.o_dt, p.hd, lane, acc);
+// acc[column e of the tile][lane] += w[row][lane] * tile[row][e] over 32 NJ rows from row0 on
+// that vis(row - row0) lets the lane see, pair by pair. w: the score registers (rows in
+// accumulator order), rounded to E as the product rounds them.
+template <typename E, int HD, int NJ, typename F>
+__device__ __forceinline__ void add_pairs(f32x16_v (&acc)[HD / 32], const f32x16_v (&w)[NJ], const lds_t *tile,
+                                          int row0, int hf, F vis) {
+#pragma unroll 1
+  for (int n = 0; n < 32 * NJ; ++n) {
+    const int reg = (n & 3) + 4 * ((n >> 3) & 3), j = n >> 5;
+    float mine = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NJ; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (u == j && e == reg) mine = w[u][e];
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mine), __float_as_uint(mine), false, false);
+    const float wv = (float)(E)__uint_as_float((n >> 2) & 1 ? both[1] : both[0]);
+    const bool on = vis(n);
+    const lds_t *row = tile + Tile<HD>::row_off(row0 + n) + 8 * hf;
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        typedef __attribute__((ext_vector_type(4))) E e4;
+        const e4 x = frag_at<e4>(row + (32 * i + 8 * g) * 2);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          acc[i][4 * g + u] = on ? acc[i][4 * g + u] + wv * (float)x[u] : acc[i][4 * g + u];
+      }
   }
 }
 
-__global__ __launch_bounds__(NTH) void window_keys_kernel(WinP p) {
-  const int lane = threadIdx.x & 63, kvh = blockIdx.y;
-  const int j = (int)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (j >= p.T) return;
-  int start, end;
-  sequence_of(p, j, start, end);
-  if (start == end) return;
-  const int64_t hk = (int64_t)kvh * p.hd;
-  const Row2 k = row2(p.k, j * p.ld_k + hk, p.dt, p.hd, lane), v = row2(p.v, j * p.ld_v + hk, p.dt, p.hd, lane);
-  Row2 dk = {0.0f, 0.0f}, dv = {0.0f, 0.0f};
-  const int last = j - start < p.n_sink || p.window >= end - j ? end : j + p.window;
-  for (int g = 0; g < p.G; ++g) {
-    const int h = kvh * p.G + g;
-    const int64_t hq = (int64_t)h * p.hd;
-    for (int i = j; i < last; ++i) {
-      const Row2 q = row2(p.q, i * p.ld_q + hq, p.dt, p.hd, lane), d = row2(p.dout, i * p.ld_do + hq, p.o_dt, p.hd, lane);
-      const int64_t si = (int64_t)h * p.T + i;
-      const float P = expf(dot2(q, k) * p.scale - p.lse[si]);
-      const float ds = P * (dot2(d, v) - p.D[si]) * p.scale;
-      dk.a += ds * q.a;
-      dk.b += ds * q.b;
-      dv.a += P * d.a;
-      dv.b += P * d.b;
+// ---------------------------------------------------------------- query blocks
+// A workgroup of NW waves of 32 queries: gh heads of one key/value head x 32 NW / gh rows
+// (wave w: head w % gh, rows 32 (w / gh) ..). What its rows see:
+struct Rows {
+  int row, start, wlo, nwin, ns;  // this lane's query (nwin = 0: of no sequence)
+  int wmin, wmax, smin, rmax, r0; // this wave's: window starts, first start, last row, first row
+  int sb0, nsb, wb0, nit;         // the workgroup's blocks: sink blocks sb0 .., then wb0 ..
+  __device__ __forceinline__ int block(int it) const { return it < nsb ? sb0 + it : wb0 + it - nsb; }
+  __device__ __forceinline__ bool active() const { return rmax >= 0; }
+  // whether the wave sees some key of the block at k0, whether one of them may be a sink before a
+  // window, and whether every row sees all of it
+  __device__ __forceinline__ bool sinks(int k0, int n_sink) const { return k0 + KB > smin && k0 - smin < n_sink; }
+  __device__ __forceinline__ bool any(int k0, int n_sink) const {
+    return active() && k0 <= rmax && (k0 + KB > wmin || sinks(k0, n_sink));
+  }
+  __device__ __forceinline__ bool all(int k0) const { return k0 >= wmax && k0 + KB - 1 <= r0; }
+  __device__ __forceinline__ bool sees(int key) const {
+    return (uint32_t)(key - wlo) < (uint32_t)nwin || (uint32_t)(key - start) < (uint32_t)ns;
+  }
+};
+
+// false: no row of the workgroup belongs to a sequence
+template <int NW>
+__device__ __forceinline__ bool rows_of(const WinP &p, int qb, int w, int lane, Rows &R) {
+  const int qrows = 32 * NW / p.gh;
+  const int first = offset_of(p.off, p.S, p.T, 0), last = offset_of(p.off, p.S, p.T, p.B);
+  const int g0 = qb * qrows, r0 = max(g0, first), r1 = min(g0 + qrows, last) - 1;
+  int b0, s0, e0;
+  if (r0 > r1 || !wave_sequence(p.off, p.S, p.T, p.B, r0, lane, b0, s0, e0)) return false;
+  const int W = p.window;
+  R.wb0 = max(s0, r0 - W + 1) >> 6;
+  const int lr = min(r1, e0 - 1), cnt = min(p.n_sink, max(s0, lr - W + 1) - s0);
+  R.sb0 = s0 >> 6;
+  R.nsb = cnt > 0 ? max(0, min((s0 + cnt - 1) >> 6, R.wb0 - 1) - R.sb0 + 1) : 0;
+  R.nit = max(0, R.nsb + (r1 >> 6) - R.wb0 + 1);
+  R.r0 = g0 + 32 * (w / p.gh);
+  R.row = R.r0 + (lane & 31);
+  bool ok = R.row >= r0 && R.row <= r1;
+  int end = e0;
+  R.start = s0;
+  if (ok && R.row >= e0) ok = lane_sequence(p.off, p.S, p.T, p.B, R.row, b0, R.start, end);
+  R.wlo = max(R.start, R.row - W + 1);
+  R.nwin = ok ? max(0, R.row - R.wlo + 1) : 0;
+  R.ns = ok ? min(p.n_sink, R.wlo - R.start) : 0;
+  constexpr int NONE = 0x7FFFFFFF;
+  R.wmin = wave_min32(ok ? R.wlo : NONE);
+  R.wmax = wave_max32(ok ? R.wlo : NONE);
+  R.smin = wave_min32(ok ? R.start : NONE);
+  R.rmax = wave_max32(ok ? R.row : -1);
+  return true;
+}
+
+// The workgroup's block of rows and first head, neighbouring blocks of a head next to each other
+__device__ __forceinline__ bool place(const WinP &p, int w, int &qb, int &h) {
+  const int t = xcd_task((int)blockIdx.x, p.nq * (p.H / p.gh));
+  if (t < 0) return false;
+  qb = t % p.nq;
+  h = t / p.nq * p.gh + w % p.gh;
+  return true;
+}
+
+// 8 elements of a query row per 16 columns: the product's B operand
+template <typename QV, int HD, typename E>
+__device__ __forceinline__ void load_row(QV (&f)[HD / 16], const E *base, int64_t ld, int row, int T, int hf) {
+  const E *at = base + (int64_t)min(row, T - 1) * ld + hf * 8;
+#pragma unroll
+  for (int es = 0; es < HD / 16; ++es) f[es] = *reinterpret_cast<const QV *>(at + es * 16);
+}
+
+// lane holds acc^T[e][row] for its own row; store that row
+template <int HD>
+__device__ __forceinline__ void store_bf16(__bf16 *row, const f32x16_v (&acc)[HD / 32], float mul, int hf) {
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bf16x4_v wv = {(__bf16)(acc[i][4 * g] * mul), (__bf16)(acc[i][4 * g + 1] * mul),
+                     (__bf16)(acc[i][4 * g + 2] * mul), (__bf16)(acc[i][4 * g + 3] * mul)};
+      *reinterpret_cast<bf16x4_v *>(row + i * 32 + 8 * g + 4 * hf) = wv;
+    }
+}
+template <int HD>
+__device__ __forceinline__ void store_f32(float *row, const f32x16_v (&acc)[HD / 32], int hf) {
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<float4 *>(row + i * 32 + 8 * g + 4 * hf) =
+          make_float4(acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]);
+}
+
+// ---------------------------------------------------------------- forward
+template <typename QE, int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void window_fwd_kernel(WinP p) {
+  typedef typename V8<QE>::type QV;
+  typedef Tile<HD> TL;
+  constexpr int NES = HD / 16, NI = HD / 32, RPW = 2 * TL::NR / NW;
+  __shared__ __align__(16) char smem[2 * 2 * TL::BYTES];  // stage s: K tile | V tile
+  lds_t *const L = LDS_AS(char, smem);
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int qb, h;
+  if (!place(p, w, qb, h)) return;
+  Rows R;
+  if (!rows_of<NW>(p, qb, w, lane, R)) return;
+  const int kvh = h / p.G;
+  const float sc = p.scale * LOG2E;
+  // half of the waves stream K, the other half V, RPW runs each
+  const bool isK = w < NW / 2;
+  const int run0 = RPW * (w % (NW / 2));
+  const int64_t ld = isK ? p.ld_k : p.ld_v;
+  const uint32_t vo = (uint32_t)((TL::lane_row(lane) * ld + 8 * TL::lane_chunk(lane)) * 2);
+  const uint32_t rowb = (uint32_t)(ld * 2);
+  auto load = [&](int kb, lds_t *st) {
+    const i32x4_v rs = block_rsrc<HD>(isK ? p.k : p.v, ld, kvh * HD, kb * KB, p.T);
+#pragma unroll
+    for (int t = 0; t < RPW; ++t)
+      dma16(rs, st + (isK ? 0 : TL::BYTES) + (run0 + t) * RUNB, vo + rowb * (uint32_t)TL::run_row(run0 + t));
+  };
+  f32x16_v o[NI];
+  float m, l;
+  auto pass = [&](auto pairs_) {
+    constexpr bool pairs = decltype(pairs_)::value;
+    QV qf[NES];
+    load_row<QV, HD>(qf, static_cast<const QE *>(p.q) + (int64_t)h * HD, p.ld_q, R.row, p.T, hf);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) o[i] = zero16();
+    m = -INFINITY;
+    l = 0.0f;
+    if (R.nit > 0) load(R.block(0), L);
+    wait_vm0();
+    __syncthreads();
+    for (int it = 0; it < R.nit; ++it) {
+      const lds_t *cur = L + (it & 1) * 2 * TL::BYTES;
+      if (it + 1 < R.nit) load(R.block(it + 1), L + ((it + 1) & 1) * 2 * TL::BYTES);
+      const int k0 = R.block(it) * KB;
+      if (R.any(k0, p.n_sink)) {
+        f32x16_v s[2] = {zero16(), zero16()};
+        // K fragments are read one k-step ahead of the products that use them
+        const lds_t *krow = cur + TL::rows_lane(lane);
+        QV kf[2][2];
+        kf[0][0] = frag_at<QV>(krow);
+        kf[0][1] = frag_at<QV>(krow + 512);
+#pragma unroll
+        for (int es = 0; es < NES; ++es) {
+          if (es + 1 < NES) {
+            kf[(es + 1) & 1][0] = frag_at<QV>(krow + 32 * (es + 1));
+            kf[(es + 1) & 1][1] = frag_at<QV>(krow + 512 + 32 * (es + 1));
+          }
+          __builtin_amdgcn_sched_barrier(0);  // (keeps the reads ahead of the products)
+          s[0] = mfma(kf[es & 1][0], qf[es], s[0]);
+          s[1] = mfma(kf[es & 1][1], qf[es], s[1]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        const bool masked = !R.all(k0);
+        if (masked) {
+          const int kw = k0 - R.wlo + 4 * hf, kst = k0 - R.start + 4 * hf;
+          if (R.sinks(k0, p.n_sink)) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int c = j * 32 + out_row(r, 0);
+                if (!((uint32_t)(kw + c) < (uint32_t)R.nwin || (uint32_t)(kst + c) < (uint32_t)R.ns))
+                  s[j][r] = -INFINITY;
+              }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (!((uint32_t)(kw + j * 32 + out_row(r, 0)) < (uint32_t)R.nwin)) s[j][r] = -INFINITY;
+          }
+        }
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          mx0 = fmaxf(mx0, s[0][r]);
+          mx1 = fmaxf(mx1, s[1][r]);
+        }
+        const float mx = max_with_partner(fmaxf(mx0, mx1)) * sc;
+        // The reference maximum m only moves when a score exceeds it by more than 8
+        // (base-2 exponent units): weights stay <= 2^8, and most blocks skip the rescale.
+        if (__any(mx > m + 8.0f)) {
+          const float mn = fmaxf(m, mx);
+          const float alpha = mn > m ? ex2(m - mn) : 1.0f;
+#pragma unroll
+          for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+          l *= alpha;
+          m = mn;
+        }
+        const float mu = m == -INFINITY ? 0.0f : m;  // (no key seen yet: weights of 0)
+        float ls[4] = {0.0f, 0.0f, 0.0f, 0.0f};      // four independent chains
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float pv = ex2(__builtin_fmaf(s[j][r], sc, -mu));
+            s[j][r] = pv;
+            ls[2 * j + (r & 1)] += pv;
+          }
+        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+        if (masked && pairs) {
+          add_pairs<QE, HD, 2>(o, s, cur + TL::BYTES, 0, hf, [&](int n) { return R.sees(k0 + n); });
+        } else {
+          // V^T fragments of step n (keys 16 n ..) read while step n - 1 multiplies
+          const uint32_t av = (uint32_t)(uintptr_t)(cur + TL::BYTES) + TL::cols_lane(lane);
+          QV vfr[2][NI];
+#pragma unroll
+          for (int i = 0; i < NI; ++i) vfr[0][i] = frag_cols_x<QV>(av, i, 0);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            if (n + 1 < 4) {
+#pragma unroll
+              for (int i = 0; i < NI; ++i) vfr[(n + 1) & 1][i] = frag_cols_x<QV>(av, i, 16 * (n + 1));
+            }
+            const QV pf = pack8<QE>(s[n >> 1], 8 * (n & 1));
+            __builtin_amdgcn_sched_barrier(0);  // (keeps the reads ahead of the products)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) o[i] = mfma(vfr[n & 1][i], pf, o[i]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      wait_vm0();
+      __syncthreads();
+    }
+  };
+  pass(std::false_type{});
+  if (__syncthreads_or(not_finite(o))) pass(std::true_type{});
+  if (R.nwin == 0) return;
+  const float lt = sum_with_partner(l);
+  store_bf16<HD>(p.o + (int64_t)R.row * p.ld_o + (int64_t)h * HD, o, 1.0f / lt, hf);
+  if (hf == 0) p.lse[(int64_t)h * p.T + R.row] = (m + log2f(lt)) * LN2;
+}
+
+// ---------------------------------------------------------------- backward
+// fp16 inputs: bf16 rows of k and v for the gradient products, 8 elements per thread (q's are
+// written by the dQ kernel, which holds them)
+__global__ __launch_bounds__(256) void window_copy_kernel(WinP p, int width) {
+  const int cpr = width / 8;  // chunks per row
+  const int64_t n = (int64_t)p.T * cpr;
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const bool isv = i >= n;
+  if (isv) i -= n;
+  if (i >= n) return;
+  const int64_t r = i / cpr, c = 8 * (i % cpr);
+  const _Float16 *const x = static_cast<const _Float16 *>(isv ? p.v : p.k) + r * (isv ? p.ld_v : p.ld_k) + c;
+  *reinterpret_cast<bf16x8_v *>((isv ? p.vb_w : p.kb_w) + r * width + c) =
+      to_bf16x8<_Float16>(*reinterpret_cast<const uint4 *>(x));
+}
+
+// dQ, D and -lse log2(e): LDS stage = K (QE) | V (bf16), plus the bf16 rows of K for fp16 inputs
+template <typename QE, int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
+  typedef typename V8<QE>::type QV;
+  typedef Tile<HD> TL;
+  constexpr bool SEP = !std::is_same<QE, __bf16>::value;  // separate bf16 K tile
+  constexpr int NT = SEP ? 3 : 2, NES = HD / 16, NI = HD / 32, RPW = NT * TL::NR / NW;
+  __shared__ __align__(16) char smem[2 * NT * TL::BYTES];
+  lds_t *const L = LDS_AS(char, smem);
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int qb, h;
+  if (!place(p, w, qb, h)) return;
+  Rows R;
+  if (!rows_of<NW>(p, qb, w, lane, R)) return;
+  const int kvh = h / p.G;
+  const float sc = p.scale * LOG2E;
+  const bool ok = R.nwin > 0;
+  auto load = [&](int kb, lds_t *st) {
+    const i32x4_v rk = block_rsrc<HD>(p.k, p.ld_k, kvh * HD, kb * KB, p.T);
+    const i32x4_v rv = block_rsrc<HD>(p.vb, p.ld_vb, kvh * HD, kb * KB, p.T);
+    const i32x4_v rb = block_rsrc<HD>(p.kb, p.ld_kb, kvh * HD, kb * KB, p.T);
+#pragma unroll
+    for (int t = 0; t < RPW; ++t) {
+      const int run = RPW * w + t, which = run / TL::NR, r = run % TL::NR;  // (wave-uniform)
+      const int64_t ld = which == 0 ? p.ld_k : which == 1 ? p.ld_vb : p.ld_kb;
+      const uint32_t off = (uint32_t)(((TL::lane_row(lane) + TL::run_row(r)) * ld + 8 * TL::lane_chunk(lane)) * 2);
+      dma16(which == 0 ? rk : which == 1 ? rv : rb, st + run * RUNB, off);
+    }
+  };
+  const int64_t si = (int64_t)h * p.T + min(R.row, p.T - 1);
+  const float lse2 = ok ? p.lse[si] * LOG2E : 0.0f;
+  float Dq = 0.0f;
+  f32x16_v acc[NI];
+  auto pass = [&](auto pairs_) {
+    constexpr bool pairs = decltype(pairs_)::value;
+    if (R.nit > 0) load(R.block(0), L);
+    QV qf[NES];
+    bf16x8_v df[NES];
+    load_row<QV, HD>(qf, static_cast<const QE *>(p.q) + (int64_t)h * HD, p.ld_q, R.row, p.T, hf);
+    load_row<bf16x8_v, HD>(df, p.dout + (int64_t)h * HD, p.ld_do, R.row, p.T, hf);
+    if constexpr (!pairs) {
+      // D of this query (its O row read while the first block streams in), and q's bf16 copy
+      bf16x8_v of[NES];
+      load_row<bf16x8_v, HD>(of, static_cast<const __bf16 *>(p.o) + (int64_t)h * HD, p.ld_o, R.row, p.T, hf);
+#pragma unroll
+      for (int es = 0; es < NES; ++es)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) Dq += (float)df[es][e] * (float)of[es][e];
+      Dq = sum_with_partner(Dq);
+      if (ok && hf == 0) {
+        p.D[si] = Dq;
+        p.nl2[si] = -lse2;
+      }
+      if (SEP && R.row < p.T) {
+#pragma unroll
+        for (int es = 0; es < NES; ++es)
+          *reinterpret_cast<bf16x8_v *>(p.qb_w + R.row * p.ld_qb + (int64_t)h * HD + es * 16 + hf * 8) =
+              to_bf16x8<QE>(__builtin_bit_cast(uint4, qf[es]));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) acc[i] = zero16();
+    wait_vm0();
+    __syncthreads();
+    for (int it = 0; it < R.nit; ++it) {
+      const lds_t *cur = L + (it & 1) * NT * TL::BYTES;
+      if (it + 1 < R.nit) load(R.block(it + 1), L + ((it + 1) & 1) * NT * TL::BYTES);
+      const int k0 = R.block(it) * KB;
+      if (R.any(k0, p.n_sink)) {
+        f32x16_v s[2] = {zero16(), zero16()}, dp[2] = {zero16(), zero16()};
+        // K fragments are read one k-step ahead of their products, V fragments
+        // two products ahead of theirs
+        const lds_t *krow = cur + TL::rows_lane(lane), *vrow = krow + TL::BYTES;
+        QV kf[2][2];
+        kf[0][0] = frag_at<QV>(krow);
+        kf[0][1] = frag_at<QV>(krow + 512);
+#pragma unroll
+        for (int es = 0; es < NES; ++es) {
+          bf16x8_v vf[2];
+          vf[0] = frag_at<bf16x8_v>(vrow + 32 * es);
+          vf[1] = frag_at<bf16x8_v>(vrow + 512 + 32 * es);
+          __builtin_amdgcn_sched_barrier(0);
+          s[0] = mfma(kf[es & 1][0], qf[es], s[0]);
+          s[1] = mfma(kf[es & 1][1], qf[es], s[1]);
+          if (es + 1 < NES) {
+            kf[(es + 1) & 1][0] = frag_at<QV>(krow + 32 * (es + 1));
+            kf[(es + 1) & 1][1] = frag_at<QV>(krow + 512 + 32 * (es + 1));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          dp[0] = mfma(vf[0], df[es], dp[0]);
+          dp[1] = mfma(vf[1], df[es], dp[1]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        const bool masked = !R.all(k0);
+        if (masked) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float pv = ex2(__builtin_fmaf(s[j][r], sc, -lse2));
+              dp[j][r] = R.sees(k0 + j * 32 + out_row(r, hf)) ? pv * (dp[j][r] - Dq) : 0.0f;
+            }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float pv = ex2(__builtin_fmaf(s[j][r], sc, -lse2));
+              dp[j][r] = pv * (dp[j][r] - Dq);
+            }
+        }
+        // K^T fragments: transposing reads of the bf16 K rows in dS's key order
+        const lds_t *kt = cur + (SEP ? 2 * TL::BYTES : 0);
+        if (masked && pairs) {
+          add_pairs<__bf16, HD, 2>(acc, dp, kt, 0, hf, [&](int n) { return R.sees(k0 + n); });
+        } else {
+          uint32_t cl = TL::cols_lane(lane);
+          asm volatile("" : "+v"(cl));  // recomputed each block, not held across the loop
+          const uint32_t ak = (uint32_t)(uintptr_t)kt + cl;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const bf16x8_v sf = pack8<__bf16>(dp[n >> 1], 8 * (n & 1));
+#pragma unroll
+            for (int i = 0; i < NI; ++i) acc[i] = mfma(frag_cols_x<bf16x8_v>(ak, i, 16 * n), sf, acc[i]);
+          }
+        }
+      }
+      wait_vm0();
+      __syncthreads();
+    }
+  };
+  pass(std::false_type{});
+  if (__syncthreads_or(not_finite(acc))) pass(std::true_type{});
+  if (ok) store_bf16<HD>(p.dq + (int64_t)R.row * p.ld_dq + (int64_t)h * HD, acc, p.scale, hf);
+}
+
+// dK, dV. A workgroup of 8 waves owns 128 consecutive key rows of a key/value head and
+// visits, for GP of the head's query heads, the query blocks that see them. Waves w and
+// w + 4 own the same 32 keys (K and V fragments in registers) and take the first and second 32
+// queries of every 64-query block; at the end wave w + 4 hands its sums to wave w, which
+// adds them. LDS stage = Q (QE) | dO | (fp16: bf16 Q) | -lse log2(e) | D of one block.
+//
+// Sinks are seen by their whole sequence, so the workgroup that owns them would visit all
+// of its queries, however long, while every other visits a window's. Where a sequence
+// leaves the chunk of query rows (p.chunk, at least a window) that it starts in, that workgroup
+// stops at limit() and the rest is split by chunk: task (chunk, block of sinks) sums over the
+// queries of the sequence that spans the chunk's first row. Such keys' sums go to fp32 slots,
+// which window_join_kernel adds in chunk order (at most one sequence spans into, and one out
+// of, a chunk, so slots are by chunk).
+//
+// With few keys (p.parts > 1) several workgroups share a key block's query heads and write
+// fp32 shares, which window_sum_kernel adds in head order.
+__device__ __forceinline__ int limit(const WinP &p, int s, int kblk) {
+  return max(kblk * KV_ROWS + KV_ROWS - 1 + p.window, (s / p.chunk + 1) * p.chunk);
+}
+// a slot of [dk | dv], 2 HD floats: set 0 the owner's sums (by the chunk that the sequence
+// starts in), set 1 a chunk's
+template <int HD>
+__device__ __forceinline__ float *slot(const WinP &p, int set, int c, int kvh, int part, int sink) {
+  return p.slots +
+         ((((((int64_t)set * p.chunks + c) * p.Hkv + kvh) * p.parts + part) * p.n_sink) + sink) * (2 * HD);
+}
+
+template <typename QE, int HD> constexpr int dkdv_stage() {
+  return (std::is_same<QE, __bf16>::value ? 2 : 3) * Tile<HD>::BYTES + 512;
+}
+template <typename QE, int HD> constexpr int dkdv_smem() {
+  constexpr int handoff = 4 * HD * 64 * 4;
+  return 2 * dkdv_stage<QE, HD>() > handoff ? 2 * dkdv_stage<QE, HD>() : handoff;
+}
+
+template <typename QE, int HD>
+__global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
+  typedef typename V8<QE>::type QV;
+  typedef Tile<HD> TL;
+  constexpr bool SEP = !std::is_same<QE, __bf16>::value;  // separate bf16 Q tile
+  constexpr int NT = SEP ? 3 : 2, NES = HD / 16, NI = HD / 32;
+  constexpr int RPW = TL::NR / (SEP ? 2 : 4);             // tile runs per wave
+  constexpr int STAGE = dkdv_stage<QE, HD>();
+  __shared__ __align__(256) char smem[dkdv_smem<QE, HD>()];
+  lds_t *const L = LDS_AS(char, smem);
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int pw = w & 3, hq = w >> 2;  // key block of the pair, query half
+  const bool splits = p.chunks > 1;
+
+  // the task: keys kblk, queries [qa, qb) of sequence [s, e) (the one past the block's last key)
+  int kblk, kvh, part, c = -1, b, s, e, qa, qb;
+  {
+    int i = (int)blockIdx.x;
+    const int pad = (p.nsplit + 7) & ~7;  // the long tasks first
+    if (i < pad) {
+      if (i >= p.nsplit) return;
+      const int kbi = i % p.nkb;
+      i /= p.nkb;
+      part = i % p.parts;
+      i /= p.parts;
+      kvh = i % p.Hkv;
+      c = 1 + i / p.Hkv;
+      const int r = c * p.chunk;
+      if (!wave_sequence(p.off, p.S, p.T, p.B, r, lane, b, s, e) || s >= r) return;
+      kblk = s / KV_ROWS + kbi;
+      if (kblk * KV_ROWS >= min(s + p.n_sink, e)) return;
+      qa = max(r, limit(p, s, kblk));
+      qb = min(e, r + p.chunk);
+      if (qa >= qb) return;
+    } else {
+      const int t = xcd_task(i - pad, p.nmain);
+      if (t < 0) return;
+      const int nb = (p.T + KV_ROWS - 1) / KV_ROWS;
+      kblk = t % nb;
+      kvh = t / nb % p.Hkv;
+      part = t / nb / p.Hkv;
+      const int first = offset_of(p.off, p.S, p.T, 0), last = offset_of(p.off, p.S, p.T, p.B);
+      const int k0 = kblk * KV_ROWS, r1 = min(k0 + KV_ROWS, last) - 1;
+      if (r1 < max(k0, first) || !wave_sequence(p.off, p.S, p.T, p.B, r1, lane, b, s, e)) return;
+      qa = k0;
+      qb = p.window < e - r1 ? r1 + p.window : e;
+      if (p.n_sink > 0 && k0 - s < p.n_sink) qb = splits ? min(e, limit(p, s, kblk)) : e;
     }
   }
-  put2(p.dk, j * p.ld_dk + hk, p.o_dt, p.hd, lane, dk);
-  put2(p.dv, j * p.ld_dv + hk, p.o_dt, p.hd, lane, dv);
+  // this lane's key: the queries [lo, lo + cnt) see it
+  const int key = kblk * KV_ROWS + pw * 32 + l32;
+  int lo = key, cnt = 0, ks = s, ke = e;
+  bool later = false;  // its sums are joined from slots
+  if (c >= 0) {
+    if (key >= s && key - s < p.n_sink && key < e) {
+      lo = qa;
+      cnt = qb - qa;
+    }
+  } else {
+    const bool ok = key < p.T && (key >= s ? key < e : lane_sequence(p.off, p.S, p.T, p.B, key, 0, ks, ke));
+    if (ok) {
+      const bool sink = key - ks < p.n_sink;
+      int hi = sink || p.window >= ke - key ? ke : key + p.window;
+      if (splits) {
+        const int lim = limit(p, s, kblk);
+        later = sink && key >= s && e > lim;
+        hi = min(hi, lim);
+      }
+      cnt = max(0, hi - key);
+    }
+  }
+  constexpr int NONE = 0x7FFFFFFF;
+  const int lo_min = wave_min32(cnt ? lo : NONE), lo_max = wave_max32(cnt ? lo : NONE);
+  const int hi_max = wave_max32(cnt ? lo + cnt : -1), hi_min = wave_min32(lo + cnt);
+  const int64_t krow = min(key, p.T - 1);
+  const float sc = p.scale * LOG2E;
+
+  // wave w brings runs RPW sub .. + RPW - 1 of tile tl (Q, dO, bf16 Q; with three tiles waves 6
+  // and 7 bring none); the last wave also brings -lse log2(e) and D (64 floats each)
+  const int tl = SEP ? (w >> 1) : (w >> 2), sub = SEP ? (w & 1) : (w & 3);
+  const bool brings = tl < NT;  // wave-uniform
+  const void *const src = tl == 0 ? p.q : tl == 1 ? static_cast<const void *>(p.dout) : p.qb;
+  const int64_t ld = tl == 0 ? p.ld_q : tl == 1 ? p.ld_do : p.ld_qb;
+  const uint32_t vo = (uint32_t)((TL::lane_row(lane) * ld + 8 * TL::lane_chunk(lane)) * 2);
+  const uint32_t rowb = (uint32_t)(ld * 2);
+  const int h0 = kvh * p.G + part * p.GP;
+  auto load = [&](int g, int qbi, lds_t *st) {
+    if (brings) {
+      const i32x4_v rs = block_rsrc<HD>(src, ld, (h0 + g) * HD, qbi * KB, p.T);
+#pragma unroll
+      for (int t = 0; t < RPW; ++t) {
+        const int run = RPW * sub + t;
+        dma16(rs, st + tl * TL::BYTES + run * RUNB, vo + rowb * (uint32_t)TL::run_row(run));
+      }
+    }
+    if (w == 7) {
+      const int64_t at = (int64_t)(h0 + g) * p.T + qbi * KB;
+      const uint32_t bytes = (uint32_t)min(KB, p.T - qbi * KB) * 4;
+      dma4(make_rsrc(p.nl2 + at, bytes), st + NT * TL::BYTES, lane * 4);
+      dma4(make_rsrc(p.D + at, bytes), st + NT * TL::BYTES + 256, lane * 4);
+    }
+  };
+  const int qfirst = qa / KB, nqb = max(0, (qb + KB - 1) / KB - qfirst), nit = nqb * p.GP;
+  f32x16_v dk[NI], dv[NI];
+  auto pass = [&](auto pairs_) {
+    constexpr bool pairs = decltype(pairs_)::value;
+    if (nit > 0) load(0, qfirst, L);
+    QV kf[NES];
+    bf16x8_v vf[NES];
+#pragma unroll
+    for (int es = 0; es < NES; ++es) {
+      const int col = kvh * HD + es * 16 + hf * 8;
+      kf[es] = *reinterpret_cast<const QV *>(static_cast<const QE *>(p.k) + krow * p.ld_k + col);
+      vf[es] = to_bf16x8<QE>(*reinterpret_cast<const uint4 *>(static_cast<const QE *>(p.v) + krow * p.ld_v + col));
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) dk[i] = dv[i] = zero16();
+    wait_vm0();
+    __syncthreads();
+    int g = 0, qi = 0;  // head and block of this iteration
+    for (int it = 0; it < nit; ++it) {
+      const lds_t *cur = L + (it & 1) * STAGE;
+      int gn = g, qn = qi + 1;
+      if (qn == nqb) {
+        qn = 0;
+        ++gn;
+      }
+      if (it + 1 < nit) load(gn, qfirst + qn, L + ((it + 1) & 1) * STAGE);
+      const int q0 = (qfirst + qi) * KB + 32 * hq;  // this wave's 32 queries
+      if (q0 + 31 >= lo_min && q0 < hi_max) {
+        f32x16_v sv = zero16(), dp = zero16();
+        // fragment rows of this wave's 32 queries: a per-lane base, made opaque
+        // each block (so that it is not held across the loop), plus immediates
+        uint32_t rl = TL::rows_lane(lane) + 512 * hq;
+        asm volatile("" : "+v"(rl));
+        const lds_t *qrow = cur + rl;
+        // each fragment is read one product ahead of the product that uses it
+        QV qv = frag_at<QV>(qrow);
+        bf16x8_v da = frag_at<bf16x8_v>(qrow + TL::BYTES);
+#pragma unroll
+        for (int es = 0; es < NES; ++es) {
+          QV qx{};
+          bf16x8_v dx{};
+          if (es + 1 < NES) qx = frag_at<QV>(qrow + 32 * (es + 1));
+          __builtin_amdgcn_sched_barrier(0);
+          sv = mfma(qv, kf[es], sv);
+          if (es + 1 < NES) dx = frag_at<bf16x8_v>(qrow + TL::BYTES + 32 * (es + 1));
+          __builtin_amdgcn_sched_barrier(0);
+          dp = mfma(da, vf[es], dp);
+          __builtin_amdgcn_sched_barrier(0);
+          qv = qx;
+          da = dx;
+        }
+        const bool masked = !(q0 >= lo_max && q0 + 31 < hi_min);
+        // four rows at a time: their -lse log2(e) and D are 4 consecutive floats each
+        typedef __attribute__((ext_vector_type(4))) float f4_t;
+        const lds_t *const st = cur + NT * TL::BYTES + 128 * hq + 16 * hf;
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq) {
+          const f4_t lc = frag_at<f4_t>(st + 32 * gq), dc = frag_at<f4_t>(st + 256 + 32 * gq);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int r = 4 * gq + x;  // out_row(r, hf) = 8 gq + 4 hf + x
+            const float pv = ex2(__builtin_fmaf(sv[r], sc, lc[x]));
+            sv[r] = pv;
+            dp[r] = pv * (dp[r] - dc[x]);
+          }
+        }
+        if (masked) {
+          const int d = q0 - lo + 4 * hf;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!((uint32_t)(d + out_row(r, 0)) < (uint32_t)cnt)) sv[r] = dp[r] = 0.0f;
+        }
+        if (masked && pairs) {
+          auto vis = [&](int n) { return (uint32_t)(q0 + n - lo) < (uint32_t)cnt; };
+          const f32x16_v w1[1] = {sv}, w2[1] = {dp};
+          add_pairs<__bf16, HD, 1>(dv, w1, cur + TL::BYTES, 32 * hq, hf, vis);
+          add_pairs<__bf16, HD, 1>(dk, w2, cur + (SEP ? 2 * TL::BYTES : 0), 32 * hq, hf, vis);
+        } else {
+          // P and dS rounded to bf16 before the gradient products, so that the
+          // fp32 score registers are free while those run
+          const bf16x8_v pf[2] = {pack8<__bf16>(sv, 0), pack8<__bf16>(sv, 8)};
+          const bf16x8_v sf[2] = {pack8<__bf16>(dp, 0), pack8<__bf16>(dp, 8)};
+          __builtin_amdgcn_sched_barrier(0);
+          // dO^T and Q^T fragments: transposing reads of the dO and bf16 Q rows in P's
+          // query order
+          uint32_t cl = TL::cols_lane(lane);
+          asm volatile("" : "+v"(cl));  // recomputed each block, not held across the loop
+          const uint32_t ac = (uint32_t)(uintptr_t)cur + cl + 512 * hq;
+          const uint32_t aq = ac + (SEP ? 2 * TL::BYTES : 0), ao = ac + TL::BYTES;
+          bf16x8_v fo[2], fq[2];
+          fo[0] = frag_cols_x<bf16x8_v>(ao, 0, 0);
+          fq[0] = frag_cols_x<bf16x8_v>(aq, 0, 0);
+#pragma unroll
+          for (int n = 0; n < 2 * NI; ++n) {
+            const int t = n / NI, i = n % NI;
+            if (n + 1 < 2 * NI) {
+              const int i1 = (n + 1) % NI, k1 = 16 * ((n + 1) / NI);
+              fo[(n + 1) & 1] = frag_cols_x<bf16x8_v>(ao, i1, k1);
+              fq[(n + 1) & 1] = frag_cols_x<bf16x8_v>(aq, i1, k1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            dv[i] = mfma(fo[n & 1], pf[t], dv[i]);
+            dk[i] = mfma(fq[n & 1], sf[t], dk[i]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      g = gn;
+      qi = qn;
+      wait_vm0();
+      __syncthreads();
+    }
+  };
+  pass(std::false_type{});
+  if (__syncthreads_or(not_finite(dk) || not_finite(dv))) pass(std::true_type{});
+  // waves 4-7 hand their sums to waves 0-3 (the stages are free now)
+  typedef __attribute__((address_space(3))) float lds_f;
+  lds_f *const red = reinterpret_cast<lds_f *>(L) + pw * (HD * 64) + lane;
+  if (hq == 1) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        red[(i * 16 + r) * 64] = dk[i][r];
+        red[(HD / 2 + i * 16 + r) * 64] = dv[i][r];
+      }
+  }
+  __syncthreads();
+  if (hq == 1 || cnt == 0) return;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dk[i][r] = (dk[i][r] + red[(i * 16 + r) * 64]) * p.scale;
+      dv[i][r] += red[(HD / 2 + i * 16 + r) * 64];
+    }
+  if (c >= 0 || (later && p.parts == 1)) {
+    float *const to = slot<HD>(p, c >= 0, c >= 0 ? c : s / p.chunk, kvh, part, key - s);
+    store_f32<HD>(to, dk, hf);
+    store_f32<HD>(to + HD, dv, hf);
+  } else if (p.parts > 1) {
+    const int64_t at = ((int64_t)part * p.T + key) * p.Hkv + kvh, n = (int64_t)p.parts * p.T * p.Hkv;
+    store_f32<HD>(p.share + at * HD, dk, hf);
+    store_f32<HD>(p.share + (n + at) * HD, dv, hf);
+  } else {
+    store_bf16<HD>(p.dk + key * p.ld_dk + (int64_t)kvh * HD, dk, 1.0f, hf);
+    store_bf16<HD>(p.dv + key * p.ld_dv + (int64_t)kvh * HD, dv, 1.0f, hf);
+  }
 }
 
-size_t scratch_of(int64_t T, int64_t H) { return T <= 0 || H <= 0 ? 0 : (size_t)T * (size_t)H * sizeof(float); }
+// dk, dv of every key row = the sum of the parts' shares in order, 8 elements per thread
+__global__ __launch_bounds__(256) void window_sum_kernel(WinP p, int width) {
+  const int cpr = width / 8;
+  const int64_t n = (int64_t)p.T * cpr, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= 2 * n) return;
+  const bool isv = i >= n;
+  const int64_t at = isv ? i - n : i, row = at / cpr, col = 8 * (at % cpr);
+  if (row < offset_of(p.off, p.S, p.T, 0) || row >= offset_of(p.off, p.S, p.T, p.B)) return;
+  const float *src = p.share + (isv ? (int64_t)p.parts * p.T * width : 0) + row * width + col;
+  float a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int t = 0; t < p.parts; ++t, src += (int64_t)p.T * width) {
+    const float4 x = *reinterpret_cast<const float4 *>(src), y = *reinterpret_cast<const float4 *>(src + 4);
+    a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w;
+    a[4] += y.x; a[5] += y.y; a[6] += y.z; a[7] += y.w;
+  }
+  store8_dt(isv ? p.dv + row * p.ld_dv : p.dk + row * p.ld_dk, col, LC_BF16, a);
+}
+
+// dk, dv of the sinks whose work was split: workgroup (chunk that the sequence starts in,
+// key/value head, sink), one thread per element
+template <int HD>
+__global__ __launch_bounds__(2 * HD) void window_join_kernel(WinP p) {
+  int i = (int)blockIdx.x;
+  const int sink = i % p.n_sink;
+  i /= p.n_sink;
+  const int kvh = i % p.Hkv, c0 = i / p.Hkv, r = (c0 + 1) * p.chunk, el = threadIdx.x;
+  int b, s, e;
+  if (!wave_sequence(p.off, p.S, p.T, p.B, r, threadIdx.x & 63, b, s, e) || s >= r || s / p.chunk != c0) return;
+  const int key = s + sink;
+  const int lim = limit(p, s, key / KV_ROWS);
+  if (key >= e || e <= lim) return;
+  float sum = 0.0f;
+  for (int part = 0; part < p.parts; ++part) {
+    if (p.parts > 1) {
+      const int64_t at = ((int64_t)part * p.T + key) * p.Hkv + kvh, n = (int64_t)p.parts * p.T * p.Hkv;
+      sum += p.share[((el >= HD ? n : 0) + at) * HD + el % HD];
+    } else {
+      sum += slot<HD>(p, 0, c0, kvh, 0, sink)[el];
+    }
+    for (int c = c0 + 1; c * p.chunk < e; ++c)
+      if (max(c * p.chunk, lim) < min(e, (c + 1) * p.chunk)) sum += slot<HD>(p, 1, c, kvh, part, sink)[el];
+  }
+  __bf16 *const to = el >= HD ? p.dv + key * p.ld_dv : p.dk + key * p.ld_dk;
+  to[(int64_t)kvh * HD + el % HD] = (__bf16)sum;
+}
+
+// ---------------------------------------------------------------- host
+int kv_of(const lc_window_attn_args &a) { return a.Hkv ? a.Hkv : a.H; }
 
 lc_status check(const lc_window_attn_args &a, bool bwd) {
   if (a.T < 0 || a.B < 1 || a.H < 1 || a.hd < 1)
@@ -159,18 +908,18 @@ lc_status check(const lc_window_attn_args &a, bool bwd) {
       return fail(LC_ERR_UNSUPPORTED, "window attention (matrix cores): head_dim must be 64 or 128");
   } else if (a.dtype == LC_FP32) {
     if (a.o_dtype != LC_FP32) return fail(LC_ERR_UNSUPPORTED, "window attention fp32: o must be fp32");
-    if (a.hd > MAXHD || a.hd % 2) return fail(LC_ERR_UNSUPPORTED, "window attention fp32: even head_dim <= 128");
+    if (a.hd > 128 || a.hd % 2) return fail(LC_ERR_UNSUPPORTED, "window attention fp32: even head_dim <= 128");
   } else {
     return fail(LC_ERR_INVALID_ARG, "window attention: unknown dtype");
   }
-  const int64_t qw = (int64_t)a.H * a.hd, kw = (int64_t)(a.Hkv ? a.Hkv : a.H) * a.hd;
-  if (qw > INT32_MAX) return fail(LC_ERR_UNSUPPORTED, "window attention: H * hd of 2^31 or more");
-  const int64_t most = (int64_t)1 << 30;  // (a row's bytes stay below 2^32)
+  const int64_t most = (int64_t)1 << 24;  // (64 rows span less than 2^32 bytes)
+  const int64_t qw = (int64_t)a.H * a.hd, kw = (int64_t)kv_of(a) * a.hd;
+  if (qw > most) return fail(LC_ERR_UNSUPPORTED, "window attention: H * hd larger than 2^24");
   auto ld_bad = [&](int64_t ld, int64_t w) { return ld < w || ld > most || (a.dtype != LC_FP32 && ld % 8); };
   if (ld_bad(a.ld_q, qw) || ld_bad(a.ld_k, kw) || ld_bad(a.ld_v, kw) || ld_bad(a.ld_o, qw) ||
       (bwd && (ld_bad(a.ld_dout, qw) || ld_bad(a.ld_dq, qw) || ld_bad(a.ld_dk, kw) || ld_bad(a.ld_dv, kw))))
     return fail(LC_ERR_INVALID_ARG, "window attention: a leading dimension is smaller than heads * hd, larger "
-                "than 2^30 or (16 bits) not a multiple of 8");
+                "than 2^24 or (16 bits) not a multiple of 8");
   if (a.T == 0) return LC_OK;
   auto bad = [](const void *x) { return !x || !aligned16(x); };
   if (bad(a.q) || bad(a.k) || bad(a.v) || bad(a.o) || bad(a.lse))
@@ -180,55 +929,178 @@ lc_status check(const lc_window_attn_args &a, bool bwd) {
   if (bwd) {
     if (bad(a.dout) || bad(a.dq) || bad(a.dk) || bad(a.dv))
       return fail(LC_ERR_INVALID_ARG, "window attention: null or unaligned gradient pointer");
-    if (bad(a.scratch) || a.scratch_bytes < scratch_of(a.T, a.H))
+    const WindowPlan w = window_plan(a.dtype, a.T, a.H, kv_of(a), a.hd, a.window, a.n_sink);
+    if (bad(a.scratch) || a.scratch_bytes < (size_t)w.total)
       return fail(LC_ERR_WORKSPACE, "window attention: scratch smaller than "
                   "lc_window_attention_scratch_bytes (or unaligned)");
   }
   return LC_OK;
 }
 
-WinP params(const lc_window_attn_args &a) {
+WinP params(const lc_window_attn_args &a, bool bwd) {
   WinP p{};
-  p.q = a.q; p.k = a.k; p.v = a.v; p.dout = a.dout;
-  p.o = a.o; p.dq = a.dq; p.dk = a.dk; p.dv = a.dv;
+  p.q = a.q; p.k = a.k; p.v = a.v;
+  p.o = static_cast<__bf16 *>(a.o);
   p.lse = a.lse;
-  p.D = static_cast<float *>(a.scratch);
+  p.dout = static_cast<const __bf16 *>(a.dout);
+  p.dq = static_cast<__bf16 *>(a.dq);
+  p.dk = static_cast<__bf16 *>(a.dk);
+  p.dv = static_cast<__bf16 *>(a.dv);
   p.off = a.seq_offsets;
   p.ld_q = a.ld_q; p.ld_k = a.ld_k; p.ld_v = a.ld_v; p.ld_o = a.ld_o;
   p.ld_do = a.ld_dout; p.ld_dq = a.ld_dq; p.ld_dk = a.ld_dk; p.ld_dv = a.ld_dv;
   p.T = (int)a.T;
   p.B = a.B;
+  p.S = (int)(a.T / a.B);
   p.H = a.H;
-  p.Hkv = a.Hkv ? a.Hkv : a.H;
+  p.Hkv = kv_of(a);
   p.G = p.H / p.Hkv;
-  p.hd = a.hd;
   p.window = a.window;
   p.n_sink = a.n_sink;
-  p.dt = a.dtype;
-  p.o_dt = a.o_dtype;
   p.scale = 1.0f / sqrtf((float)a.hd);
+  if (!bwd) return p;
+  const WindowPlan w = window_plan(a.dtype, a.T, p.H, p.Hkv, a.hd, a.window, a.n_sink);
+  char *const sc = static_cast<char *>(a.scratch);
+  p.D = reinterpret_cast<float *>(sc + w.D);
+  p.nl2 = reinterpret_cast<float *>(sc + w.nl2);
+  if (a.dtype == LC_FP16) {
+    p.qb = p.qb_w = reinterpret_cast<__bf16 *>(sc + w.qb);
+    p.kb = p.kb_w = reinterpret_cast<__bf16 *>(sc + w.kb);
+    p.vb = p.vb_w = reinterpret_cast<__bf16 *>(sc + w.vb);
+    p.ld_qb = (int64_t)p.H * a.hd;
+    p.ld_kb = p.ld_vb = (int64_t)p.Hkv * a.hd;
+  } else {
+    p.qb = static_cast<const __bf16 *>(a.q);
+    p.kb = static_cast<const __bf16 *>(a.k);
+    p.vb = static_cast<const __bf16 *>(a.v);
+    p.ld_qb = a.ld_q; p.ld_kb = a.ld_k; p.ld_vb = a.ld_v;
+  }
+  p.share = reinterpret_cast<float *>(sc + w.share);
+  p.slots = reinterpret_cast<float *>(sc + w.slots);
+  p.parts = w.parts;
+  p.GP = p.G / w.parts;
+  p.chunk = w.chunk;
+  p.chunks = w.chunks;
+  p.nkb = (p.n_sink + KV_ROWS - 2) / KV_ROWS + 1;
+  p.nmain = (p.T + KV_ROWS - 1) / KV_ROWS * p.Hkv * p.parts;
+  p.nsplit = (p.chunks - 1) * p.Hkv * p.parts * p.nkb;
   return p;
+}
+
+// forward and dQ grids: gh heads of a group (as many of 1, 2, 4, 8 as divide it, at most one
+// per wave) share a workgroup's keys, so that it spans fewer rows and with them fewer keys
+template <int NW>
+lc_status row_grid(WinP &p, unsigned &grid) {
+  p.gh = 1;
+  while (2 * p.gh <= NW && p.G % (2 * p.gh) == 0) p.gh *= 2;
+  const int qrows = 32 * NW / p.gh;
+  p.nq = (p.T + qrows - 1) / qrows;
+  const int64_t n = (int64_t)p.nq * (p.H / p.gh);
+  if (n > 1 << 22) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^22 blocks of rows and heads");
+  grid = (unsigned)((n + 7) / 8 * 8);
+  return LC_OK;
+}
+
+template <typename QE, int HD>
+lc_status fwd(const lc_window_attn_args &a, hipStream_t s) {
+  constexpr int NW = 4;
+  WinP p = params(a, false);
+  unsigned grid = 0;
+  LC_TRY(row_grid<NW>(p, grid));
+  hipLaunchKernelGGL((window_fwd_kernel<QE, HD, NW>), dim3(grid), dim3(64 * NW), 0, s, p);
+  return check_launch("window_fwd_kernel");
+}
+
+template <typename QE, int HD>
+lc_status bwd(const lc_window_attn_args &a, hipStream_t s) {
+  constexpr bool SEP = !std::is_same<QE, __bf16>::value;
+  constexpr int NW = SEP && HD == 128 ? 8 : 4;  // (three tiles of 128: one workgroup per compute unit)
+  WinP p = params(a, true);
+  unsigned grid = 0;
+  LC_TRY(row_grid<NW>(p, grid));
+  const int64_t n = ((int64_t)(p.nsplit + 7) / 8 + ((int64_t)p.nmain + 7) / 8) * 8;
+  if (n > 1 << 22) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^22 blocks of keys and heads");
+  const int width = p.Hkv * HD;
+  const size_t chunks = 2 * (size_t)p.T * width / 8;
+  if (chunks / 256 >= 1u << 24) return fail(LC_ERR_UNSUPPORTED, "window attention: k and v of 2^34 or more elements");
+  if (SEP) {
+    hipLaunchKernelGGL(window_copy_kernel, dim3(ceil_div(chunks, 256)), dim3(256), 0, s, p, width);
+    LC_TRY(check_launch("window_copy_kernel"));
+  }
+  hipLaunchKernelGGL((window_dq_kernel<QE, HD, NW>), dim3(grid), dim3(64 * NW), 0, s, p);
+  LC_TRY(check_launch("window_dq_kernel"));
+  hipLaunchKernelGGL((window_dkdv_kernel<QE, HD>), dim3((unsigned)n), dim3(512), 0, s, p);
+  LC_TRY(check_launch("window_dkdv_kernel"));
+  if (p.parts > 1) {
+    hipLaunchKernelGGL(window_sum_kernel, dim3(ceil_div(chunks, 256)), dim3(256), 0, s, p, width);
+    LC_TRY(check_launch("window_sum_kernel"));
+  }
+  if (p.chunks > 1) {
+    hipLaunchKernelGGL((window_join_kernel<HD>), dim3((unsigned)((p.chunks - 1) * p.Hkv * p.n_sink)), dim3(2 * HD),
+                       0, s, p);
+    LC_TRY(check_launch("window_join_kernel"));
+  }
+  return LC_OK;
 }
 
 lc_status forward(const lc_window_attn_args &a, hipStream_t s) {
   LC_TRY(check(a, false));
   if (a.T == 0) return LC_OK;
-  const WinP p = params(a);
-  hipLaunchKernelGGL(window_rows_kernel<false>, dim3((p.T + 3) / 4, p.H), dim3(NTH), 0, s, p);
-  return check_launch("window_rows_kernel");
+  if (a.dtype == LC_FP32) return window_f32_fwd_launch(a, s);
+  if (a.dtype == LC_FP16) return a.hd == 64 ? fwd<_Float16, 64>(a, s) : fwd<_Float16, 128>(a, s);
+  return a.hd == 64 ? fwd<__bf16, 64>(a, s) : fwd<__bf16, 128>(a, s);
 }
 
 lc_status backward(const lc_window_attn_args &a, hipStream_t s) {
   LC_TRY(check(a, true));
   if (a.T == 0) return LC_OK;
-  const WinP p = params(a);
-  hipLaunchKernelGGL(window_rows_kernel<true>, dim3((p.T + 3) / 4, p.H), dim3(NTH), 0, s, p);
-  LC_TRY(check_launch("window_rows_kernel"));
-  hipLaunchKernelGGL(window_keys_kernel, dim3((p.T + 3) / 4, p.Hkv), dim3(NTH), 0, s, p);
-  return check_launch("window_keys_kernel");
+  if (a.dtype == LC_FP32) return window_f32_bwd_launch(a, s);
+  if (a.dtype == LC_FP16) return a.hd == 64 ? bwd<_Float16, 64>(a, s) : bwd<_Float16, 128>(a, s);
+  return a.hd == 64 ? bwd<__bf16, 64>(a, s) : bwd<__bf16, 128>(a, s);
 }
 
 }  // namespace
+
+WindowPlan window_plan(int dtype, int64_t T, int H, int Hkv, int hd, int window, int n_sink) {
+  WindowPlan w{};
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t x = at;
+    at += (bytes + 255) / 256 * 256;
+    return x;
+  };
+  w.parts = w.chunks = 1;
+  w.D = take(T * H * 4);
+  w.nl2 = w.kb = w.vb = w.qb = w.share = w.slots = 0;
+  if (dtype != LC_FP32) {
+    w.nl2 = take(T * H * 4);
+    if (dtype == LC_FP16) {
+      w.kb = take(T * Hkv * hd * 2);
+      w.vb = take(T * Hkv * hd * 2);
+      w.qb = take(T * H * hd * 2);
+    }
+    const int G = H / Hkv;
+    const int64_t tasks = (T + KV_ROWS - 1) / KV_ROWS * Hkv;
+    for (int n = 1; n <= G; ++n)
+      if (G % n == 0) {
+        w.parts = n;
+        if (tasks * n >= 384) break;
+      }
+    if (w.parts > 1) w.share = take(2 * w.parts * T * Hkv * hd * 4);
+    int64_t chunk = 1024;
+    while (chunk < (int64_t)window + KV_ROWS) chunk *= 2;
+    if (n_sink > 0 && n_sink <= MAXSINK && chunk < T) {
+      w.chunk = (int)chunk;
+      w.chunks = (int)((T + chunk - 1) / chunk);
+      w.slots = take(2ll * w.chunks * Hkv * w.parts * n_sink * 2 * hd * 4);
+    } else {
+      w.chunk = 1 << 30;
+    }
+  }
+  w.total = at;
+  return w;
+}
+
 }  // namespace lc
 
 extern "C" {
@@ -245,8 +1117,10 @@ lc_status lc_window_attention_backward(const lc_window_attn_args *args, void *st
 
 size_t lc_window_attention_scratch_bytes(int32_t dtype, int64_t T, int32_t H, int32_t Hkv, int32_t hd,
                                          int32_t window, int32_t n_sink) {
-  (void)dtype; (void)Hkv; (void)hd; (void)window; (void)n_sink;
-  return lc::scratch_of(T, H);
+  if (T <= 0 || T >= (int64_t)1 << 30 || H < 1 || Hkv < 0 || hd < 1 || hd > 128 || window < 1 || n_sink < 0 ||
+      (Hkv > 0 && H % Hkv) || (int64_t)H * hd > 1 << 24)
+    return 0;
+  return (size_t)lc::window_plan(dtype, T, H, Hkv ? Hkv : H, hd, window, n_sink).total;
 }
 
 }  // extern "C"
