@@ -1,24 +1,46 @@
-// LayerNorm forward and backward.
+// LayerNorm forward and backward (HBM-bound row kernels).
 //
 //   forward:  mu = mean_k x, r = 1/sqrt(mean_k (x - mu)^2 + eps), y = (x - mu) r g + b
 //   backward: xh = (x - mu) r, t = dy g,
 //             dx = dres + r (t - mean_k t - xh mean_k(t xh)),
 //             dg += sum_t dy xh, db += sum_t dy
+//
+// Every tensor is read once and written once: a row stays in registers between its
+// sums and its write (up to 65536 values forward, 16384 backward; longer rows are read
+// again, from L2), the variance is a second sum over the registers, of differences to the
+// mean (sums of squares would lose it in rows far from 0).
+//
+// Rows are read in runs of 8 values at any alignment (the instruction takes any address); the
+// last run of a row whose length is no multiple of 8 begins 8 values before the row's end, and the
+// values that it shares with the run before count once in the sums and are written twice,
+// alike. Whether a tensor has 2 or 4 bytes per value is a template argument (straight-line
+// loads); which 16-bit type is a run-time choice of the conversion.
+//
+// The weight gradients are sums over rows. A backward workgroup keeps its rows' share of
+// its columns in registers over all of its rows (a workgroup per compute unit, so the shares
+// stay a small part of the traffic), adds its row slots through LDS in order, and a second
+// kernel adds the workgroups' shares of each column in order: the same bits every run.
 #include "common.hpp"
+
+#include <algorithm>
 
 namespace lc {
 namespace {
 
-constexpr int NTH = 256;
-constexpr int ROWS = 16;  // rows per block of the weight gradients' partial sums
+constexpr int NTH = 256;        // forward, one to four waves per row
+constexpr int NTB = 1024;       // backward
+constexpr int MAXBLK = 256;     // backward workgroups, one per compute unit
+constexpr int LONG_ROWS = 64;   // rows of a block of the long rows' weight gradients
 
 struct LnP {
   const void *x, *g, *b, *dy, *dres;
   void *y, *dx, *dx_copy;
   float *mean, *rstd;
-  float *pg, *pb;  // partial sums of dg and db, [nblk, d] each
+  float *part;     // shares of dg, then db: [2, nblk, d]
   float *dg, *db;
-  int64_t T, d, ld_x, ld_y, ld_dy, ld_dres, ld_dx;
+  int64_t T, ld_x, ld_y, ld_dy, ld_dres, ld_dx;
+  int64_t first;   // forward, long rows: the launch's first workgroup
+  int d, lpr;      // lpr: lanes per row where several rows share a wave
   float eps;
   int x_dt, w_dt, out_dt, dy_dt, dres_dt, store, nblk;
 };
@@ -41,6 +63,170 @@ __device__ __forceinline__ float scaled(float dy, float g) {
   return dy * g;
 }
 
+// ---------------------------------------------------------------- runs of 8 values
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_v;
+typedef u32x4_v u32x4_any __attribute__((aligned(2)));
+// 8 values of SZ bytes as they lie in memory (SZ = 0: of a size known at run time)
+template <int SZ> struct Raw { u32x4_v v[SZ == 2 ? 1 : 2]; };
+
+template <int SZ>
+__device__ __forceinline__ void load_raw(const void *base, int64_t i, int dt, Raw<SZ> &r) {
+  const bool wide = SZ ? SZ == 4 : dt == LC_FP32;
+  const u32x4_any *at = reinterpret_cast<const u32x4_any *>(static_cast<const char *>(base) + i * (wide ? 4 : 2));
+  r.v[0] = at[0];
+  if constexpr (SZ != 2) {
+    if (wide) r.v[1] = at[1];
+  }
+}
+__device__ __forceinline__ void half_values(u32x4_v v, int dt, float (&x)[8]) {
+  if (dt == LC_BF16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+    }
+  } else {
+    const f16x8_v h = __builtin_bit_cast(f16x8_v, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)h[i];
+  }
+}
+template <int SZ>
+__device__ __forceinline__ void values(const Raw<SZ> &r, int dt, float (&x)[8]) {
+  if constexpr (SZ != 2) {
+    if (SZ == 4 || dt == LC_FP32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r.v[i >> 2][i & 3]);
+      return;
+    }
+  }
+  half_values(r.v[0], dt, x);
+}
+template <int SZ>
+__device__ __forceinline__ void load8(const void *base, int64_t i, int dt, float (&x)[8]) {
+  Raw<SZ> r;
+  load_raw<SZ>(base, i, dt, r);
+  values<SZ>(r, dt, x);
+}
+template <int SZ>
+__device__ __forceinline__ void store8(void *base, int64_t i, int dt, const float (&x)[8]) {
+  const bool wide = SZ ? SZ == 4 : dt == LC_FP32;
+  u32x4_any *at = reinterpret_cast<u32x4_any *>(static_cast<char *>(base) + i * (wide ? 4 : 2));
+  if (wide) {
+    u32x4_v a, b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = __float_as_uint(x[e]);
+      b[e] = __float_as_uint(x[e + 4]);
+    }
+    at[0] = a;
+    at[1] = b;
+    return;
+  }
+  if (dt == LC_BF16) {
+    bf16x8_v h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (__bf16)x[e];
+    at[0] = __builtin_bit_cast(u32x4_v, h);
+  } else {
+    f16x8_v h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)x[e];
+    at[0] = __builtin_bit_cast(u32x4_v, h);
+  }
+}
+
+// run n of a row of d >= 8 values: its first value (d or more: no run), and how many of its
+// values the run before holds already
+__device__ __forceinline__ int run_at(int n, int d, int &skip) {
+  const int c = 8 * n, at = min(c, d - 8);
+  skip = c - at;
+  return c < d ? at : d;
+}
+
+// sum over the lpr lanes of a row (a power of two, aligned)
+__device__ __forceinline__ float row_sum(float v, int lpr) {
+  for (int o = 1; o < lpr; o <<= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// ---------------------------------------------------------------- forward
+// WPR waves per row, each lane U runs; U = 1: 64 / lpr rows per wave (lpr < 64 up to 256 values)
+template <int WPR, int U, int XS, int WS, int YS>
+__global__ __launch_bounds__(WPR > 4 ? 64 * WPR : NTH) void layernorm_fwd_kernel(LnP p) {
+  constexpr int NW = WPR > 4 ? WPR : NTH / 64;
+  __shared__ float red[2][NW];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int lpr = U == 1 ? p.lpr : 64;
+  const int64_t blk = p.first + blockIdx.x;
+  const int64_t row = U == 1 ? (blk * NW + wv) * (64 / lpr) + lane / lpr : blk * (NW / WPR) + wv / WPR;
+  const bool ok = row < p.T;
+  const int l = U == 1 ? lane % lpr : (wv % WPR) * 64 + lane;
+  const void *x = static_cast<const char *>(p.x) + row * p.ld_x * XS;
+  float v[U][8];
+  int at[U], skip[U];
+  float s = 0.0f;
+  Raw<XS> raw[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    at[u] = run_at(l + 64 * WPR * u, p.d, skip[u]);
+    if (!ok) at[u] = p.d;
+    if (at[u] < p.d) load_raw<XS>(x, at[u], p.x_dt, raw[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (at[u] < p.d) {
+      values<XS>(raw[u], p.x_dt, v[u]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += e >= skip[u] ? v[u][e] : 0.0f;
+    }
+  auto total = [&](float t, int which) {
+    if constexpr (U == 1) return row_sum(t, lpr);
+    t = wave_sum(t);
+    if constexpr (WPR > 1) {
+      if (lane == 0) red[which][wv] = t;
+      __syncthreads();
+      t = red[which][wv / WPR * WPR];
+#pragma unroll
+      for (int w = 1; w < WPR; ++w) t += red[which][wv / WPR * WPR + w];
+    }
+    return t;
+  };
+  const float mu = total(s, 0) / (float)p.d;
+  float q = 0.0f;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (at[u] < p.d) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[u][e] -= mu;
+        q += e >= skip[u] ? v[u][e] * v[u][e] : 0.0f;
+      }
+    }
+  const float r = 1.0f / sqrtf(total(q, 1) / (float)p.d + p.eps);
+  if (!ok) return;
+  if (l == 0) {
+    p.mean[row] = mu;
+    p.rstd[row] = r;
+  }
+  void *y = static_cast<char *>(p.y) + row * p.ld_y * YS;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (at[u] < p.d) {
+      float g[8], b[8];
+      load8<WS>(p.g, at[u], p.w_dt, g);
+      if (p.b) {
+        load8<WS>(p.b, at[u], p.w_dt, b);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[u][e] = v[u][e] * r * g[e] + b[e];
+      store8<YS>(y, at[u], p.out_dt, v[u]);
+    }
+}
+
 __device__ __forceinline__ float block_sum(float v, float *red) {
   v = wave_sum(v);
   __syncthreads();
@@ -49,13 +235,14 @@ __device__ __forceinline__ float block_sum(float v, float *red) {
   return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-__global__ __launch_bounds__(NTH) void layernorm_fwd_kernel(LnP p) {
+// rows shorter than a run or longer than registers hold: a workgroup per row, value by value
+__global__ __launch_bounds__(NTH) void layernorm_fwd_any_kernel(LnP p) {
   __shared__ float red[4];
-  const int64_t t = blockIdx.x;
+  const int64_t t = p.first + blockIdx.x;
   float s = 0.0f, v = 0.0f;
-  for (int64_t k = threadIdx.x; k < p.d; k += NTH) s += ld1(p.x, t * p.ld_x + k, p.x_dt);
+  for (int k = threadIdx.x; k < p.d; k += NTH) s += ld1(p.x, t * p.ld_x + k, p.x_dt);
   const float mu = block_sum(s, red) / (float)p.d;
-  for (int64_t k = threadIdx.x; k < p.d; k += NTH) {
+  for (int k = threadIdx.x; k < p.d; k += NTH) {
     const float c = ld1(p.x, t * p.ld_x + k, p.x_dt) - mu;
     v += c * c;
   }
@@ -64,52 +251,202 @@ __global__ __launch_bounds__(NTH) void layernorm_fwd_kernel(LnP p) {
     p.mean[t] = mu;
     p.rstd[t] = r;
   }
-  for (int64_t k = threadIdx.x; k < p.d; k += NTH) {
+  for (int k = threadIdx.x; k < p.d; k += NTH) {
     const float xh = (ld1(p.x, t * p.ld_x + k, p.x_dt) - mu) * r;
     st1(p.y, t * p.ld_y + k, p.out_dt, xh * ld1(p.g, k, p.w_dt) + (p.b ? ld1(p.b, k, p.w_dt) : 0.0f));
   }
 }
 
-// partial sums of the weight gradients over ROWS rows
-__global__ __launch_bounds__(NTH) void layernorm_partial_kernel(LnP p) {
-  const int64_t k = (int64_t)blockIdx.x * NTH + threadIdx.x;
-  if (k >= p.d) return;
-  const int64_t t0 = (int64_t)blockIdx.y * ROWS, t1 = min(p.T, t0 + ROWS);
-  float g = 0.0f, b = 0.0f;
-  for (int64_t t = t0; t < t1; ++t) {
-    const float dy = ld1(p.dy, t * p.ld_dy + k, p.dy_dt);
-    g += dy * ((ld1(p.x, t * p.ld_x + k, p.x_dt) - p.mean[t]) * p.rstd[t]);
-    b += dy;
+// ---------------------------------------------------------------- backward
+// Rows of 8 to 16384 values. A row is held by lpr lanes (a power of two; up to 64 of a wave, or
+// whole waves), lane l of it the runs l and (U = 2, rows over 8192) l + lpr; the workgroup takes
+// NTB / lpr rows at a time and loads the next ones before the sums of these (U = 1: two runs
+// per lane leave no registers for that, nor for the gain). A row's sums
+// over several waves go through LDS, buffered twice, one barrier per step.
+template <int DYS, int XS, int OS, int U>
+__global__ __launch_bounds__(NTB) void layernorm_bwd_kernel(LnP p) {
+  constexpr int RS = OS;
+  constexpr bool AHEAD = U == 1;
+  __shared__ __align__(16) float red[U * NTB * 8];
+  __shared__ float dots[2][2][NTB / 64];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int lpr = p.lpr, slots = NTB / lpr, slot = threadIdx.x / lpr, l = threadIdx.x % lpr;
+  int at[U], skip[U];
+  float g[U][8], ag[U][8], ab[U][8];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    at[u] = run_at(l + lpr * u, p.d, skip[u]);
+    if (AHEAD && at[u] < p.d) load8<0>(p.g, at[u], p.w_dt, g[u]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ag[u][e] = ab[u][e] = 0.0f;
   }
-  p.pg[blockIdx.y * p.d + k] = g;
-  p.pb[blockIdx.y * p.d + k] = b;
+  Raw<DYS> ry[U];
+  Raw<XS> rx[U];
+  Raw<RS> rr[U];
+  float mu = 0.0f, r = 0.0f;
+  auto load = [&](int64_t row) {
+    if (row >= p.T) return;
+    mu = p.mean[row];
+    r = p.rstd[row];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at[u] < p.d) {
+        load_raw<DYS>(p.dy, row * p.ld_dy + at[u], p.dy_dt, ry[u]);
+        load_raw<XS>(p.x, row * p.ld_x + at[u], p.x_dt, rx[u]);
+        if (AHEAD && p.dres) load_raw<RS>(p.dres, row * p.ld_dres + at[u], p.dres_dt, rr[u]);
+      }
+  };
+  const int64_t step = (int64_t)gridDim.x * slots;
+  int64_t row = (int64_t)blockIdx.x * slots + slot;
+  if (AHEAD) load(row);
+#pragma unroll 1
+  for (int64_t r0 = (int64_t)blockIdx.x * slots, it = 0; r0 < p.T; r0 += step, row += step, ++it) {
+    const bool ok = row < p.T;
+    float xh[U][8], t[U][8], o[U][8];
+    float st = 0.0f, sx = 0.0f;
+    if (!AHEAD) load(row);
+    const float rc = r;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (ok && at[u] < p.d) {
+        values<DYS>(ry[u], p.dy_dt, t[u]);
+        values<XS>(rx[u], p.x_dt, xh[u]);
+        if (AHEAD && p.dres) {
+          values<RS>(rr[u], p.dres_dt, o[u]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[u][e] = 0.0f;
+        }
+        if (!AHEAD) load8<0>(p.g, at[u], p.w_dt, g[u]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          xh[u][e] = (xh[u][e] - mu) * rc;
+          ag[u][e] += t[u][e] * xh[u][e];
+          ab[u][e] += t[u][e];
+          t[u][e] = scaled(t[u][e], g[u][e]);
+          st += e >= skip[u] ? t[u][e] : 0.0f;
+          sx += e >= skip[u] ? t[u][e] * xh[u][e] : 0.0f;
+        }
+      }
+    if (AHEAD) load(row + step);
+    if (lpr <= 64) {
+      st = row_sum(st, lpr);
+      sx = row_sum(sx, lpr);
+    } else {
+      st = wave_sum(st);
+      sx = wave_sum(sx);
+      if (lane == 0) {
+        dots[it & 1][0][wv] = st;
+        dots[it & 1][1][wv] = sx;
+      }
+      __syncthreads();
+      const int w0 = slot * (lpr / 64);
+      st = dots[it & 1][0][w0];
+      sx = dots[it & 1][1][w0];
+      for (int w = 1; w < lpr / 64; ++w) {
+        st += dots[it & 1][0][w0 + w];
+        sx += dots[it & 1][1][w0 + w];
+      }
+    }
+    if (!ok) continue;
+    st /= (float)p.d;
+    sx /= (float)p.d;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at[u] < p.d) {
+        if (!AHEAD && p.dres) load8<RS>(p.dres, row * p.ld_dres + at[u], p.dres_dt, o[u]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[u][e] += rc * (t[u][e] - st - xh[u][e] * sx);
+        store8<OS>(p.dx, row * p.ld_dx + at[u], p.out_dt, o[u]);
+        if (p.dx_copy) store8<2>(p.dx_copy, row * p.ld_dx + at[u], LC_BF16, o[u]);
+      }
+  }
+  if (!p.dg && !p.db) return;
+  // the row slots in order, column by column
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    float *const dst = which ? p.db : p.dg;
+    if (!dst) continue;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at[u] < p.d) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e >= skip[u]) red[slot * U * lpr * 8 + at[u] + e] = which ? ab[u][e] : ag[u][e];
+      }
+    __syncthreads();
+    for (int k = threadIdx.x; k < p.d; k += NTB) {
+      float s = red[k];
+      for (int i = 1; i < slots; ++i) s += red[i * U * lpr * 8 + k];
+      if (gridDim.x > 1) p.part[((int64_t)which * p.nblk + blockIdx.x) * p.d + k] = s;
+      else dst[k] = p.store ? s : dst[k] + s;
+    }
+  }
 }
 
-__global__ __launch_bounds__(NTH) void layernorm_final_kernel(LnP p) {
-  const int64_t k = (int64_t)blockIdx.x * NTH + threadIdx.x;
-  if (k >= p.d) return;
-  float g = 0.0f, b = 0.0f;
-  for (int i = 0; i < p.nblk; ++i) {
-    g += p.pg[i * p.d + k];
-    b += p.pb[i * p.d + k];
+// dg, db [k] (+)= the workgroups' shares: sixteen slices of consecutive workgroups, each in
+// order with its loads in flight together, then the slices in order
+constexpr int SLICES = 16;
+__global__ __launch_bounds__(64 * SLICES) void layernorm_final_kernel(LnP p) {
+  __shared__ float sl[SLICES][64];
+  float *const dst = blockIdx.y ? p.db : p.dg;
+  if (!dst) return;
+  const int i = threadIdx.x >> 6, kc = threadIdx.x & 63;
+  const int k = blockIdx.x * 64 + kc;
+  const int per = (p.nblk + SLICES - 1) / SLICES, b0 = i * per, b1 = min(p.nblk, b0 + per);
+  const float *part = p.part + (int64_t)blockIdx.y * p.nblk * p.d + k;
+  float s = 0.0f;
+  if (k < p.d) {
+    int b = b0;
+    for (; b + 8 <= b1; b += 8) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = part[(int64_t)(b + j) * p.d];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += v[j];
+    }
+    for (; b < b1; ++b) s += part[(int64_t)b * p.d];
   }
-  if (p.dg) p.dg[k] = p.store ? g : p.dg[k] + g;
-  if (p.db) p.db[k] = p.store ? b : p.db[k] + b;
+  sl[i][kc] = s;
+  __syncthreads();
+  if (i == 0 && k < p.d) {
+#pragma unroll
+    for (int j = 1; j < SLICES; ++j) s += sl[j][kc];
+    dst[k] = p.store ? s : dst[k] + s;
+  }
 }
 
-__global__ __launch_bounds__(NTH) void layernorm_bwd_kernel(LnP p) {
+// Rows shorter than a run or longer than registers hold: the shares of blocks of LONG_ROWS
+// rows (before dx, which may lie over dy), then a workgroup per row, value by value.
+__global__ __launch_bounds__(NTH) void layernorm_part_any_kernel(LnP p) {
+  const int k = blockIdx.x * NTH + threadIdx.x;
+  if (k >= p.d) return;
+  for (int64_t blk = blockIdx.y; blk < p.nblk; blk += gridDim.y) {
+    const int64_t t0 = blk * LONG_ROWS, t1 = min(p.T, t0 + LONG_ROWS);
+    float g = 0.0f, b = 0.0f;
+    for (int64_t t = t0; t < t1; ++t) {
+      const float dy = ld1(p.dy, t * p.ld_dy + k, p.dy_dt);
+      g += dy * ((ld1(p.x, t * p.ld_x + k, p.x_dt) - p.mean[t]) * p.rstd[t]);
+      b += dy;
+    }
+    p.part[blk * p.d + k] = g;
+    p.part[(p.nblk + blk) * p.d + k] = b;
+  }
+}
+__global__ __launch_bounds__(NTH) void layernorm_bwd_any_kernel(LnP p) {
   __shared__ float red[4];
-  const int64_t t = blockIdx.x;
+  const int64_t t = p.first + blockIdx.x;
   const float mu = p.mean[t], r = p.rstd[t];
   float s = 0.0f, q = 0.0f;
-  for (int64_t k = threadIdx.x; k < p.d; k += NTH) {
+  for (int k = threadIdx.x; k < p.d; k += NTH) {
     const float u = scaled(ld1(p.dy, t * p.ld_dy + k, p.dy_dt), ld1(p.g, k, p.w_dt));
     s += u;
     q += u * ((ld1(p.x, t * p.ld_x + k, p.x_dt) - mu) * r);
   }
   s = block_sum(s, red) / (float)p.d;
   q = block_sum(q, red) / (float)p.d;
-  for (int64_t k = threadIdx.x; k < p.d; k += NTH) {
+  for (int k = threadIdx.x; k < p.d; k += NTH) {
     const float u = scaled(ld1(p.dy, t * p.ld_dy + k, p.dy_dt), ld1(p.g, k, p.w_dt));
     const float xh = (ld1(p.x, t * p.ld_x + k, p.x_dt) - mu) * r;
     float o = r * (u - s - xh * q);
@@ -119,9 +456,22 @@ __global__ __launch_bounds__(NTH) void layernorm_bwd_kernel(LnP p) {
   }
 }
 
-int64_t blocks_of(int64_t T) { return (T + ROWS - 1) / ROWS; }
+// ---------------------------------------------------------------- host
+constexpr int MAXD_FWD = 65536, MAXD_BWD = 16384;
+
+int lanes_of(int64_t d, int most) {  // the power of two of lanes that hold a row, 8 values each
+  int l = 1;
+  while (l < most && 8ll * l < d) l *= 2;
+  return l;
+}
+bool bwd_in_registers(int64_t d) { return d >= 8 && d <= MAXD_BWD; }
+int64_t blocks_of(int64_t T, int64_t d) {
+  if (!bwd_in_registers(d)) return (T + LONG_ROWS - 1) / LONG_ROWS;
+  const int slots = NTB / lanes_of(d, NTB);
+  return std::min<int64_t>(MAXBLK, (T + slots - 1) / slots);
+}
 size_t scratch_of(int64_t T, int64_t d) {
-  return T <= 0 || d <= 0 ? 0 : (size_t)blocks_of(T) * (size_t)d * 2 * sizeof(float);
+  return T <= 0 || d <= 0 ? 0 : (size_t)blocks_of(T, d) * (size_t)d * 2 * sizeof(float);
 }
 
 lc_status check(const lc_layernorm_args &a, bool bwd) {
@@ -159,39 +509,112 @@ LnP params(const lc_layernorm_args &a) {
   p.y = a.y; p.dx = a.dx; p.dx_copy = a.dx_copy;
   p.mean = a.mean; p.rstd = a.rstd;
   p.dg = a.dg_accum; p.db = a.db_accum;
-  p.T = a.T; p.d = a.d;
+  p.T = a.T;
+  p.d = (int)a.d;
   p.ld_x = ld(a.ld_x); p.ld_y = ld(a.ld_y); p.ld_dy = ld(a.ld_dy); p.ld_dres = ld(a.ld_dres); p.ld_dx = ld(a.ld_dx);
   p.eps = a.eps;
   p.x_dt = a.x_dtype; p.w_dt = a.w_dtype; p.out_dt = a.out_dtype; p.dy_dt = a.dy_dtype; p.dres_dt = a.dres_dtype;
   p.store = a.store_dg != 0;
-  p.nblk = (int)blocks_of(a.T);
-  p.pg = static_cast<float *>(a.scratch);
-  p.pb = p.pg ? p.pg + (size_t)p.nblk * a.d : nullptr;
+  p.part = static_cast<float *>(a.scratch);
   return p;
+}
+
+// calls f(sizes...) with each type's size (2 or 4 bytes) as a compile-time constant
+template <typename F> void with_size(int dt, F f) {
+  if (dt == LC_FP32) f(std::integral_constant<int, 4>{});
+  else f(std::integral_constant<int, 2>{});
+}
+
+template <int WPR, int U>
+void fwd_shape(LnP p, hipStream_t s) {
+  constexpr int NW = WPR > 4 ? WPR : NTH / 64;
+  const int64_t rows = U == 1 ? NW * (64 / p.lpr) : NW / WPR;
+  with_size(p.x_dt, [&](auto xs) {
+    with_size(p.w_dt, [&](auto ws) {
+      with_size(p.out_dt, [&](auto ys) {
+        launch_parts((uint32_t)((p.T + rows - 1) / rows), [&](uint32_t first, uint32_t count) {
+          p.first = first;
+          hipLaunchKernelGGL((layernorm_fwd_kernel<WPR, U, decltype(xs)::value, decltype(ws)::value, decltype(ys)::value>),
+                             dim3(count), dim3(64 * NW), 0, s, p);
+        });
+      });
+    });
+  });
 }
 
 lc_status forward(const lc_layernorm_args &a, hipStream_t s) {
   LC_TRY(check(a, false));
   if (a.T == 0) return LC_OK;
-  const LnP p = params(a);
-  hipLaunchKernelGGL(layernorm_fwd_kernel, dim3((unsigned)p.T), dim3(NTH), 0, s, p);
+  LnP p = params(a);
+  p.lpr = lanes_of(a.d, 64);
+  if (p.d < 8 || p.d > MAXD_FWD) {
+    launch_parts((uint32_t)p.T, [&](uint32_t first, uint32_t count) {
+      p.first = first;
+      hipLaunchKernelGGL(layernorm_fwd_any_kernel, dim3(count), dim3(NTH), 0, s, p);
+    });
+  } else if (p.d <= 512) {
+    fwd_shape<1, 1>(p, s);
+  } else if (p.d <= 1024) {
+    fwd_shape<1, 2>(p, s);
+  } else if (p.d <= 2048) {
+    fwd_shape<1, 4>(p, s);
+  } else if (p.d <= 4096) {
+    fwd_shape<1, 8>(p, s);
+  } else if (p.d <= 8192) {
+    fwd_shape<2, 8>(p, s);
+  } else if (p.d <= 16384) {
+    fwd_shape<4, 8>(p, s);
+  } else {
+    fwd_shape<16, 8>(p, s);
+  }
   return check_launch("layernorm_fwd_kernel");
+}
+
+template <int U>
+void bwd_shape(const LnP &p, hipStream_t s) {
+  const dim3 grid((unsigned)p.nblk), block(NTB);
+  // (the residual's gradient of another size than dx: every size at run time)
+  if (p.dres && (p.dres_dt == LC_FP32) != (p.out_dt == LC_FP32)) {
+    hipLaunchKernelGGL((layernorm_bwd_kernel<0, 0, 0, U>), grid, block, 0, s, p);
+    return;
+  }
+  with_size(p.dy_dt, [&](auto ds) {
+    with_size(p.x_dt, [&](auto xs) {
+      with_size(p.out_dt, [&](auto os) {
+        hipLaunchKernelGGL((layernorm_bwd_kernel<decltype(ds)::value, decltype(xs)::value, decltype(os)::value, U>),
+                           grid, block, 0, s, p);
+      });
+    });
+  });
 }
 
 lc_status backward(const lc_layernorm_args &a, hipStream_t s) {
   LC_TRY(check(a, true));
   if (a.T == 0) return LC_OK;
-  const LnP p = params(a);
-  const unsigned cols = ceil_div((size_t)p.d, NTH);
+  LnP p = params(a);
+  p.nblk = (int)blocks_of(a.T, a.d);
+  p.lpr = lanes_of(a.d, NTB);
   const bool sums = p.dg || p.db;
-  if (sums) {  // before dx, which may lie over dy
-    hipLaunchKernelGGL(layernorm_partial_kernel, dim3(cols, (unsigned)p.nblk), dim3(NTH), 0, s, p);
-    LC_TRY(check_launch("layernorm_partial_kernel"));
-    hipLaunchKernelGGL(layernorm_final_kernel, dim3(cols), dim3(NTH), 0, s, p);
-    LC_TRY(check_launch("layernorm_final_kernel"));
+  if (bwd_in_registers(a.d)) {
+    if (p.d <= 8 * NTB) bwd_shape<1>(p, s);
+    else bwd_shape<2>(p, s);
+    LC_TRY(check_launch("layernorm_bwd_kernel"));
+    if (!sums || p.nblk == 1) return LC_OK;
+  } else {
+    if (sums) {
+      const dim3 grid(ceil_div((size_t)p.d, NTH), std::min(p.nblk, 1024));
+      hipLaunchKernelGGL(layernorm_part_any_kernel, grid, dim3(NTH), 0, s, p);
+      LC_TRY(check_launch("layernorm_part_any_kernel"));
+    }
+    launch_parts((uint32_t)p.T, [&](uint32_t first, uint32_t count) {
+      p.first = first;
+      hipLaunchKernelGGL(layernorm_bwd_any_kernel, dim3(count), dim3(NTH), 0, s, p);
+    });
+    LC_TRY(check_launch("layernorm_bwd_any_kernel"));
+    if (!sums) return LC_OK;
   }
-  hipLaunchKernelGGL(layernorm_bwd_kernel, dim3((unsigned)p.T), dim3(NTH), 0, s, p);
-  return check_launch("layernorm_bwd_kernel");
+  hipLaunchKernelGGL(layernorm_final_kernel, dim3(ceil_div((size_t)p.d, 64), 2), dim3(64 * SLICES), 0, s, p);
+  return check_launch("layernorm_final_kernel");
 }
 
 }  // namespace
