@@ -8,6 +8,12 @@
 // under 1e-8 rad at any position. The nearest multiple of a quarter turn is split
 // off in integers too, so sin and cos are taken of at most pi/4, where their Taylor
 // series to x^11 and x^12 are exact to fp32.
+//
+// The rotation is bound by the memory traffic of the head rows (each read and written
+// once). A token's cos and sin are formed once for all of its heads: hd / 2 pairs are
+// RUN = 8 (4, 2, 1) consecutive ones per lane, the lanes of a group hold a head's pairs, and
+// the wave's groups walk the token's heads with the same cos and sin in registers. Few
+// tokens share out their heads over more waves instead, so that the chip is filled.
 #include "common.hpp"
 
 #include <math.h>
@@ -28,6 +34,8 @@ struct RopeP {
   int64_t ld_x, ld_y, T;
   float *cos, *sin;
   int heads, half, x_dt, y_dt;
+  int lpg, share;  // lanes per group; waves that share a token's heads
+  int64_t first;   // the launch's first workgroup
   float sign;  // 1 forward, -1 backward
 };
 
@@ -51,34 +59,132 @@ __device__ __forceinline__ void pair_cos_sin(const RopeP &p, int64_t t, int i, f
   cos_sin((uint64_t)at * p.turn[i], c, s);
 }
 
-__device__ __forceinline__ float ld1(const void *base, int64_t i, int dt) {
-  if (dt == LC_FP32) return static_cast<const float *>(base)[i];
-  if (dt == LC_BF16) return (float)static_cast<const __bf16 *>(base)[i];
-  return (float)static_cast<const _Float16 *>(base)[i];
-}
-__device__ __forceinline__ void st1(void *base, int64_t i, int dt, float v) {
-  if (dt == LC_FP32) static_cast<float *>(base)[i] = v;
-  else if (dt == LC_BF16) static_cast<__bf16 *>(base)[i] = (__bf16)v;
-  else static_cast<_Float16 *>(base)[i] = (_Float16)v;
-}
+// RUN consecutive values of a row at any alignment (the instruction takes any address), as
+// floats and back; SZ bytes per value, the 16-bit type a run-time choice of the conversion
+template <int N> struct Words;
+template <> struct Words<4> { typedef uint32_t type __attribute__((aligned(2))); };
+template <> struct Words<8> { typedef __attribute__((ext_vector_type(2))) uint32_t v; typedef v type __attribute__((aligned(2))); };
+template <> struct Words<16> { typedef __attribute__((ext_vector_type(4))) uint32_t v; typedef v type __attribute__((aligned(2))); };
 
-// one workgroup per token
+template <int SZ, int RUN> struct Vals {
+  static constexpr int BYTES = SZ * RUN;
+  uint32_t w[BYTES < 4 ? 1 : BYTES / 4];
+  __device__ __forceinline__ void load(const char *at) {
+    if constexpr (BYTES >= 16) {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i)
+        __builtin_memcpy(w + 4 * i, reinterpret_cast<const Words<16>::type *>(at) + i, 16);
+    } else if constexpr (BYTES == 8) {
+      __builtin_memcpy(w, reinterpret_cast<const Words<8>::type *>(at), 8);
+    } else if constexpr (BYTES == 4) {
+      w[0] = *reinterpret_cast<const Words<4>::type *>(at);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t *>(at);
+    }
+  }
+  __device__ __forceinline__ void store(char *at) const {
+    if constexpr (BYTES >= 16) {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i)
+        __builtin_memcpy(reinterpret_cast<Words<16>::type *>(at) + i, w + 4 * i, 16);
+    } else if constexpr (BYTES == 8) {
+      __builtin_memcpy(reinterpret_cast<Words<8>::type *>(at), w, 8);
+    } else if constexpr (BYTES == 4) {
+      *reinterpret_cast<Words<4>::type *>(at) = w[0];
+    } else {
+      *reinterpret_cast<uint16_t *>(at) = (uint16_t)w[0];
+    }
+  }
+  __device__ __forceinline__ float get(int i, int dt) const {
+    if constexpr (SZ == 4) return __uint_as_float(w[i]);
+    const uint16_t h = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    return dt == LC_BF16 ? __uint_as_float((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+  }
+  __device__ __forceinline__ void put(const float (&x)[RUN], int dt) {
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) {
+      if constexpr (SZ == 4) {
+        w[i] = __float_as_uint(x[i]);
+      } else {
+        const uint16_t h = dt == LC_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)x[i])
+                                         : __builtin_bit_cast(uint16_t, (_Float16)x[i]);
+        if (i & 1) w[i >> 1] |= (uint32_t)h << 16;
+        else w[i >> 1] = h;
+      }
+    }
+  }
+};
+
+// Groups of p.lpg lanes (a power of two; lane l holds pairs RUN l ..) take a token's heads in
+// turn; a group's heads are h0, h0 + stride, ..., those of `p.share` waves side by side.
+template <int XS, int YS, int RUN>
 __global__ __launch_bounds__(NTH) void rope_axes_kernel(RopeP p) {
-  const int64_t t = blockIdx.x;
-  for (int n = threadIdx.x; n < p.heads * p.half; n += NTH) {
-    const int h = n / p.half, i = n % p.half;
-    float c, s;
-    pair_cos_sin(p, t, i, c, s);
-    s *= p.sign;
-    const int64_t at = (int64_t)h * 2 * p.half + i;
-    const float a = ld1(p.x, t * p.ld_x + at, p.x_dt), b = ld1(p.x, t * p.ld_x + at + p.half, p.x_dt);
-    st1(p.y, t * p.ld_y + at, p.y_dt, a * c - b * s);
-    st1(p.y, t * p.ld_y + at + p.half, p.y_dt, b * c + a * s);
+  const int lane = threadIdx.x & 63, l = lane % p.lpg;
+  const int64_t w = (p.first + blockIdx.x) * (NTH / 64) + (threadIdx.x >> 6);
+  const int64_t t = w / p.share;
+  if (t >= p.T) return;  // (a whole wave)
+  const int groups = 64 / p.lpg, stride = groups * p.share;
+  const int64_t hd = 2 * p.half;
+  const int h0 = (int)(w % p.share) * groups + lane / p.lpg;
+  const char *x = static_cast<const char *>(p.x) + t * p.ld_x * XS;
+  char *y = static_cast<char *>(p.y) + t * p.ld_y * YS;
+  // pairs `lane` and lane + 64
+  float c0 = 1.0f, s0 = 0.0f, c1 = 1.0f, s1 = 0.0f;
+  if (lane < p.half) pair_cos_sin(p, t, lane, c0, s0);
+  if (p.half > 64 && lane + 64 < p.half) pair_cos_sin(p, t, lane + 64, c1, s1);
+  // (RUN = 1: up to 127 pairs on 64 lanes)
+#pragma unroll
+  for (int round = 0; round < (RUN == 1 ? 2 : 1); ++round) {
+    const int i0 = RUN * (l + p.lpg * round);
+    if (round && p.lpg * round >= p.half) break;
+    float c[RUN], s[RUN];
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) {
+      const int from = (i0 + i) & 63;
+      c[i] = __shfl(c0, from, 64);
+      s[i] = __shfl(s0, from, 64);
+      if (p.half > 64) {
+        const float ch = __shfl(c1, from, 64), sh = __shfl(s1, from, 64);
+        c[i] = i0 + i < 64 ? c[i] : ch;
+        s[i] = i0 + i < 64 ? s[i] : sh;
+      }
+      s[i] *= p.sign;
+    }
+    if (i0 >= p.half) continue;
+    Vals<XS, RUN> a, b;
+    int h = h0;
+    if (h < p.heads) {
+      a.load(x + (h * hd + i0) * XS);
+      b.load(x + (h * hd + i0 + p.half) * XS);
+    }
+    while (h < p.heads) {
+      const int hn = h + stride;
+      Vals<XS, RUN> an, bn;
+      if (hn < p.heads) {
+        an.load(x + (hn * hd + i0) * XS);
+        bn.load(x + (hn * hd + i0 + p.half) * XS);
+      }
+      float u[RUN], v[RUN];
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) {
+        const float ai = a.get(i, p.x_dt), bi = b.get(i, p.x_dt);
+        u[i] = ai * c[i] - bi * s[i];
+        v[i] = bi * c[i] + ai * s[i];
+      }
+      Vals<YS, RUN> o;
+      o.put(u, p.y_dt);
+      o.store(y + (h * hd + i0) * YS);
+      o.put(v, p.y_dt);
+      o.store(y + (h * hd + i0 + p.half) * YS);
+      a = an;
+      b = bn;
+      h = hn;
+    }
   }
 }
 
 __global__ __launch_bounds__(NTH) void rope_table_kernel(RopeP p) {
-  const int64_t n = (int64_t)blockIdx.x * NTH + threadIdx.x;
+  const int64_t n = (p.first + blockIdx.x) * NTH + threadIdx.x;
   if (n >= p.T * p.half) return;
   float c, s;
   pair_cos_sin(p, n / p.half, (int)(n % p.half), c, s);
@@ -154,17 +260,47 @@ RopeP params(const lc_rope_axes_args &a, Kind kind) {
   return p;
 }
 
+template <int XS, int YS>
+void rotate(RopeP p, hipStream_t s) {
+  // the longest run that a head's pairs consist of (16-byte accesses at 8 values of 16 bits)
+  const int run = p.half % 8 == 0 ? 8 : p.half % 4 == 0 ? 4 : p.half % 2 == 0 ? 2 : 1;
+  p.lpg = 1;
+  while (p.lpg * run < p.half && p.lpg < 64) p.lpg *= 2;
+  const int groups = 64 / p.lpg;
+  // waves that share a token: up to one per `groups` heads while the tokens' waves are fewer
+  // than 16 per compute unit
+  p.share = 1;
+  while (p.share * groups < p.heads && p.T * p.share < 4096) p.share *= 2;
+  const int64_t wgs = (p.T * p.share + NTH / 64 - 1) / (NTH / 64);
+  launch_parts((uint32_t)wgs, [&](uint32_t first, uint32_t count) {
+    p.first = first;
+    if (run == 8) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 8>), dim3(count), dim3(NTH), 0, s, p);
+    else if (run == 4) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 4>), dim3(count), dim3(NTH), 0, s, p);
+    else if (run == 2) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 2>), dim3(count), dim3(NTH), 0, s, p);
+    else hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 1>), dim3(count), dim3(NTH), 0, s, p);
+  });
+}
+
 lc_status run(const lc_rope_axes_args *args, Kind kind, void *stream) {
   if (!args) return fail(LC_ERR_INVALID_ARG, "rope axes: null args");
   LC_TRY(check(*args, kind));
   if (args->T == 0) return LC_OK;
-  const RopeP p = params(*args, kind);
+  RopeP p = params(*args, kind);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (kind == TABLE) {
-    hipLaunchKernelGGL(rope_table_kernel, dim3(ceil_div((size_t)p.T * p.half, NTH)), dim3(NTH), 0, s, p);
+    launch_parts(ceil_div((size_t)p.T * p.half, NTH), [&](uint32_t first, uint32_t count) {
+      p.first = first;
+      hipLaunchKernelGGL(rope_table_kernel, dim3(count), dim3(NTH), 0, s, p);
+    });
     return check_launch("rope_table_kernel");
   }
-  hipLaunchKernelGGL(rope_axes_kernel, dim3((unsigned)p.T), dim3(NTH), 0, s, p);
+  if (p.x_dt == LC_FP32) {
+    if (p.y_dt == LC_FP32) rotate<4, 4>(p, s);
+    else rotate<4, 2>(p, s);
+  } else {
+    if (p.y_dt == LC_FP32) rotate<2, 4>(p, s);
+    else rotate<2, 2>(p, s);
+  }
   return check_launch("rope_axes_kernel");
 }
 
