@@ -188,10 +188,10 @@ struct Rows {
 template <int NW>
 __device__ __forceinline__ bool rows_of(const WinP &p, int qb, int w, int lane, Rows &R) {
   const int qrows = 32 * NW / p.gh;
-  const int first = offset_of(p.off, p.S, p.T, 0), last = offset_of(p.off, p.S, p.T, p.B);
-  const int g0 = qb * qrows, r0 = max(g0, first), r1 = min(g0 + qrows, last) - 1;
+  const Sequences sq(p.off, p.S, p.T, p.B, lane);
+  const int g0 = qb * qrows, r0 = max(g0, sq.first), r1 = min(g0 + qrows, sq.last) - 1;
   int b0, s0, e0;
-  if (r0 > r1 || !wave_sequence(p.off, p.S, p.T, p.B, r0, lane, b0, s0, e0)) return false;
+  if (r0 > r1 || !sq.of_wave(r0, lane, b0, s0, e0)) return false;
   const int W = p.window;
   R.wb0 = max(s0, r0 - W + 1) >> 6;
   const int lr = min(r1, e0 - 1), cnt = min(p.n_sink, max(s0, lr - W + 1) - s0);
@@ -201,9 +201,11 @@ __device__ __forceinline__ bool rows_of(const WinP &p, int qb, int w, int lane, 
   R.r0 = g0 + 32 * (w / p.gh);
   R.row = R.r0 + (lane & 31);
   bool ok = R.row >= r0 && R.row <= r1;
-  int end = e0;
   R.start = s0;
-  if (ok && R.row >= e0) ok = lane_sequence(p.off, p.S, p.T, p.B, R.row, b0, R.start, end);
+  if (r1 >= e0) {  // (more than one sequence)
+    int end;
+    ok = sq.of_lane(R.row, b0, R.start, end) && ok;
+  }
   R.wlo = max(R.start, R.row - W + 1);
   R.nwin = ok ? max(0, R.row - R.wlo + 1) : 0;
   R.ns = ok ? min(p.n_sink, R.wlo - R.start) : 0;
@@ -605,6 +607,7 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
   const bool splits = p.chunks > 1;
 
   // the task: keys kblk, queries [qa, qb) of sequence [s, e) (the one past the block's last key)
+  const Sequences sq(p.off, p.S, p.T, p.B, lane);
   int kblk, kvh, part, c = -1, b, s, e, qa, qb;
   {
     int i = (int)blockIdx.x;
@@ -618,7 +621,7 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
       kvh = i % p.Hkv;
       c = 1 + i / p.Hkv;
       const int r = c * p.chunk;
-      if (!wave_sequence(p.off, p.S, p.T, p.B, r, lane, b, s, e) || s >= r) return;
+      if (!sq.of_wave(r, lane, b, s, e) || s >= r) return;
       kblk = s / KV_ROWS + kbi;
       if (kblk * KV_ROWS >= min(s + p.n_sink, e)) return;
       qa = max(r, limit(p, s, kblk));
@@ -631,9 +634,8 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
       kblk = t % nb;
       kvh = t / nb % p.Hkv;
       part = t / nb / p.Hkv;
-      const int first = offset_of(p.off, p.S, p.T, 0), last = offset_of(p.off, p.S, p.T, p.B);
-      const int k0 = kblk * KV_ROWS, r1 = min(k0 + KV_ROWS, last) - 1;
-      if (r1 < max(k0, first) || !wave_sequence(p.off, p.S, p.T, p.B, r1, lane, b, s, e)) return;
+      const int k0 = kblk * KV_ROWS, r1 = min(k0 + KV_ROWS, sq.last) - 1;
+      if (r1 < max(k0, sq.first) || !sq.of_wave(r1, lane, b, s, e)) return;
       qa = k0;
       qb = p.window < e - r1 ? r1 + p.window : e;
       if (p.n_sink > 0 && k0 - s < p.n_sink) qb = splits ? min(e, limit(p, s, kblk)) : e;
@@ -649,7 +651,8 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
       cnt = qb - qa;
     }
   } else {
-    const bool ok = key < p.T && (key >= s ? key < e : lane_sequence(p.off, p.S, p.T, p.B, key, 0, ks, ke));
+    bool ok = key < e;
+    if (s > kblk * KV_ROWS) ok = sq.of_lane(key, 0, ks, ke);  // (more than one sequence)
     if (ok) {
       const bool sink = key - ks < p.n_sink;
       int hi = sink || p.window >= ke - key ? ke : key + p.window;
@@ -846,10 +849,10 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
 __global__ __launch_bounds__(256) void window_sum_kernel(WinP p, int width) {
   const int cpr = width / 8;
   const int64_t n = (int64_t)p.T * cpr, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= 2 * n) return;
   const bool isv = i >= n;
   const int64_t at = isv ? i - n : i, row = at / cpr, col = 8 * (at % cpr);
-  if (row < offset_of(p.off, p.S, p.T, 0) || row >= offset_of(p.off, p.S, p.T, p.B)) return;
+  const Sequences sq(p.off, p.S, p.T, p.B, threadIdx.x & 63);
+  if (i >= 2 * n || row < sq.first || row >= sq.last) return;
   const float *src = p.share + (isv ? (int64_t)p.parts * p.T * width : 0) + row * width + col;
   float a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int t = 0; t < p.parts; ++t, src += (int64_t)p.T * width) {
@@ -869,7 +872,8 @@ __global__ __launch_bounds__(2 * HD) void window_join_kernel(WinP p) {
   i /= p.n_sink;
   const int kvh = i % p.Hkv, c0 = i / p.Hkv, r = (c0 + 1) * p.chunk, el = threadIdx.x;
   int b, s, e;
-  if (!wave_sequence(p.off, p.S, p.T, p.B, r, threadIdx.x & 63, b, s, e) || s >= r || s / p.chunk != c0) return;
+  const Sequences sq(p.off, p.S, p.T, p.B, threadIdx.x & 63);
+  if (!sq.of_wave(r, threadIdx.x & 63, b, s, e) || s >= r || s / p.chunk != c0) return;
   const int key = s + sink;
   const int lim = limit(p, s, key / KV_ROWS);
   if (key >= e || e <= lim) return;
