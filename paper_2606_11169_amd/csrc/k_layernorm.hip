@@ -28,8 +28,6 @@ namespace lc {
 namespace {
 
 constexpr int NTH = 256;        // forward, one to four waves per row
-constexpr int NTB = 1024;       // backward
-constexpr int MAXBLK = 256;     // backward workgroups, one per compute unit
 constexpr int LONG_ROWS = 64;   // rows of a block of the long rows' weight gradients
 
 struct LnP {
@@ -61,6 +59,30 @@ __device__ __forceinline__ void st1(void *base, int64_t i, int dt, float v) {
 __device__ __forceinline__ float scaled(float dy, float g) {
 #pragma clang fp contract(off)
   return dy * g;
+}
+
+// sum over the lpr lanes of a row (a power of two up to 64, aligned), in every lane: pairs,
+// quads, halves of 16 and 16 lanes by data-parallel moves, then rows and halves of the wave
+// swapped. (Shuffles, twelve in a row of two sums, go through LDS: 9 x 768 forward 3.4 us, 2.7
+// this way, 500 x 4096 4.7 and 4.4.)
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float row_sum(float v, int lpr) {
+  if (lpr > 1) v += moved<0xB1>(v);   // quad_perm 1 0 3 2
+  if (lpr > 2) v += moved<0x4E>(v);   // quad_perm 2 3 0 1
+  if (lpr > 4) v += moved<0x141>(v);  // row_half_mirror
+  if (lpr > 8) v += moved<0x140>(v);  // row_mirror
+  if (lpr > 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if (lpr > 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
 }
 
 // ---------------------------------------------------------------- runs of 8 values
@@ -144,14 +166,14 @@ __device__ __forceinline__ int run_at(int n, int d, int &skip) {
   return c < d ? at : d;
 }
 
-// sum over the lpr lanes of a row (a power of two, aligned)
-__device__ __forceinline__ float row_sum(float v, int lpr) {
-  for (int o = 1; o < lpr; o <<= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
 
 // ---------------------------------------------------------------- forward
-// WPR waves per row, each lane U runs; U = 1: 64 / lpr rows per wave (lpr < 64 up to 256 values)
+// WPR waves per row, each lane U runs; U = 1: 64 / lpr rows per wave (lpr < 64 up to 256 values).
+// Two runs per lane and as many waves as that takes: few rows of 4096 to 8192 values are held
+// by more of the chip than with eight runs (60 rows of 8192 7.3 -> 3.8 us, 500 of 4096 7.7 ->
+// 4.7), many lose nothing (16411 x 8192 102 -> 98 us, 4096 x 4096 fp32 in, bf16 out 23.8 -> 22.5).
+// Rows of 1025 to 2048 have no barrier with four runs, which many of them gain by (8000 x 2048
+// 15.9 -> 15.1 us; 3001 x 1155 6.1 with two waves, 6.3 with one).
 template <int WPR, int U, int XS, int WS, int YS>
 __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : NTH) void layernorm_fwd_kernel(LnP p) {
   constexpr int NW = WPR > 4 ? WPR : NTH / 64;
@@ -182,7 +204,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : NTH) void layernorm_fwd_kernel
     }
   auto total = [&](float t, int which) {
     if constexpr (U == 1) return row_sum(t, lpr);
-    t = wave_sum(t);
+    t = row_sum(t, 64);
     if constexpr (WPR > 1) {
       if (lane == 0) red[which][wv] = t;
       __syncthreads();
@@ -228,7 +250,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : NTH) void layernorm_fwd_kernel
 }
 
 __device__ __forceinline__ float block_sum(float v, float *red) {
-  v = wave_sum(v);
+  v = row_sum(v, 64);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -260,13 +282,15 @@ __global__ __launch_bounds__(NTH) void layernorm_fwd_any_kernel(LnP p) {
 // ---------------------------------------------------------------- backward
 // Rows of 8 to 16384 values. A row is held by lpr lanes (a power of two; up to 64 of a wave, or
 // whole waves), lane l of it the runs l and (U = 2, rows over 8192) l + lpr; the workgroup takes
-// NTB / lpr rows at a time and loads the next ones before the sums of these (U = 1: two runs
-// per lane leave no registers for that, nor for the gain). A row's sums
-// over several waves go through LDS, buffered twice, one barrier per step.
-template <int DYS, int XS, int OS, int U>
+// NTB / lpr rows at a time. U = 1: the loads run AHEAD = 2 such steps before the sums (one step
+// ahead 16411 x 8192 bf16 take 217 us, two 201; sizes that leave fewer rows per workgroup lie
+// within 3%); two runs per lane leave no registers for that, nor for the gain. A row's
+// sums over several waves go through LDS, buffered twice, one barrier per step.
+template <int DYS, int XS, int OS, int U, int NTB>
 __global__ __launch_bounds__(NTB) void layernorm_bwd_kernel(LnP p) {
   constexpr int RS = OS;
-  constexpr bool AHEAD = U == 1;
+  constexpr int AHEAD = U == 1 ? 2 : 1;
+  constexpr bool HOLD = U == 1;  // the gain in registers
   __shared__ __align__(16) float red[U * NTB * 8];
   __shared__ float dots[2][2][NTB / 64];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
@@ -276,48 +300,49 @@ __global__ __launch_bounds__(NTB) void layernorm_bwd_kernel(LnP p) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     at[u] = run_at(l + lpr * u, p.d, skip[u]);
-    if (AHEAD && at[u] < p.d) load8<0>(p.g, at[u], p.w_dt, g[u]);
+    if (HOLD && at[u] < p.d) load8<0>(p.g, at[u], p.w_dt, g[u]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) ag[u][e] = ab[u][e] = 0.0f;
   }
-  Raw<DYS> ry[U];
-  Raw<XS> rx[U];
-  Raw<RS> rr[U];
-  float mu = 0.0f, r = 0.0f;
-  auto load = [&](int64_t row) {
+  struct In {
+    Raw<DYS> y[U];
+    Raw<XS> x[U];
+    Raw<RS> r[U];
+    float mu, rstd;
+  } in[AHEAD];
+  auto load = [&](In &i, int64_t row) {
     if (row >= p.T) return;
-    mu = p.mean[row];
-    r = p.rstd[row];
+    i.mu = p.mean[row];
+    i.rstd = p.rstd[row];
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (at[u] < p.d) {
-        load_raw<DYS>(p.dy, row * p.ld_dy + at[u], p.dy_dt, ry[u]);
-        load_raw<XS>(p.x, row * p.ld_x + at[u], p.x_dt, rx[u]);
-        if (AHEAD && p.dres) load_raw<RS>(p.dres, row * p.ld_dres + at[u], p.dres_dt, rr[u]);
+        load_raw<DYS>(p.dy, row * p.ld_dy + at[u], p.dy_dt, i.y[u]);
+        load_raw<XS>(p.x, row * p.ld_x + at[u], p.x_dt, i.x[u]);
+        if (HOLD && p.dres) load_raw<RS>(p.dres, row * p.ld_dres + at[u], p.dres_dt, i.r[u]);
       }
   };
   const int64_t step = (int64_t)gridDim.x * slots;
-  int64_t row = (int64_t)blockIdx.x * slots + slot;
-  if (AHEAD) load(row);
-#pragma unroll 1
-  for (int64_t r0 = (int64_t)blockIdx.x * slots, it = 0; r0 < p.T; r0 += step, row += step, ++it) {
+  int64_t r0 = (int64_t)blockIdx.x * slots, row = r0 + slot;
+  int odd = 0;
+  auto one = [&](In &i) {  // the rows of a step, loaded into i
     const bool ok = row < p.T;
     float xh[U][8], t[U][8], o[U][8];
     float st = 0.0f, sx = 0.0f;
-    if (!AHEAD) load(row);
-    const float rc = r;
+    if (!HOLD) load(i, row);
+    const float rc = i.rstd, mu = i.mu;
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (ok && at[u] < p.d) {
-        values<DYS>(ry[u], p.dy_dt, t[u]);
-        values<XS>(rx[u], p.x_dt, xh[u]);
-        if (AHEAD && p.dres) {
-          values<RS>(rr[u], p.dres_dt, o[u]);
+        values<DYS>(i.y[u], p.dy_dt, t[u]);
+        values<XS>(i.x[u], p.x_dt, xh[u]);
+        if (HOLD && p.dres) {
+          values<RS>(i.r[u], p.dres_dt, o[u]);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) o[u][e] = 0.0f;
         }
-        if (!AHEAD) load8<0>(p.g, at[u], p.w_dt, g[u]);
+        if (!HOLD) load8<0>(p.g, at[u], p.w_dt, g[u]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           xh[u][e] = (xh[u][e] - mu) * rc;
@@ -328,38 +353,53 @@ __global__ __launch_bounds__(NTB) void layernorm_bwd_kernel(LnP p) {
           sx += e >= skip[u] ? t[u][e] * xh[u][e] : 0.0f;
         }
       }
-    if (AHEAD) load(row + step);
+    if (HOLD) load(i, row + AHEAD * step);
     if (lpr <= 64) {
       st = row_sum(st, lpr);
       sx = row_sum(sx, lpr);
     } else {
-      st = wave_sum(st);
-      sx = wave_sum(sx);
+      st = row_sum(st, 64);
+      sx = row_sum(sx, 64);
       if (lane == 0) {
-        dots[it & 1][0][wv] = st;
-        dots[it & 1][1][wv] = sx;
+        dots[odd][0][wv] = st;
+        dots[odd][1][wv] = sx;
       }
       __syncthreads();
       const int w0 = slot * (lpr / 64);
-      st = dots[it & 1][0][w0];
-      sx = dots[it & 1][1][w0];
+      st = dots[odd][0][w0];
+      sx = dots[odd][1][w0];
       for (int w = 1; w < lpr / 64; ++w) {
-        st += dots[it & 1][0][w0 + w];
-        sx += dots[it & 1][1][w0 + w];
+        st += dots[odd][0][w0 + w];
+        sx += dots[odd][1][w0 + w];
       }
     }
-    if (!ok) continue;
-    st /= (float)p.d;
-    sx /= (float)p.d;
+    if (ok) {
+      st /= (float)p.d;
+      sx /= (float)p.d;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (at[u] < p.d) {
-        if (!AHEAD && p.dres) load8<RS>(p.dres, row * p.ld_dres + at[u], p.dres_dt, o[u]);
+      for (int u = 0; u < U; ++u)
+        if (at[u] < p.d) {
+          if (!HOLD && p.dres) load8<RS>(p.dres, row * p.ld_dres + at[u], p.dres_dt, o[u]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[u][e] += rc * (t[u][e] - st - xh[u][e] * sx);
-        store8<OS>(p.dx, row * p.ld_dx + at[u], p.out_dt, o[u]);
-        if (p.dx_copy) store8<2>(p.dx_copy, row * p.ld_dx + at[u], LC_BF16, o[u]);
-      }
+          for (int e = 0; e < 8; ++e) o[u][e] += rc * (t[u][e] - st - xh[u][e] * sx);
+          store8<OS>(p.dx, row * p.ld_dx + at[u], p.out_dt, o[u]);
+          if (p.dx_copy) store8<2>(p.dx_copy, row * p.ld_dx + at[u], LC_BF16, o[u]);
+        }
+    }
+    r0 += step;
+    row += step;
+    odd ^= 1;
+  };
+  if (HOLD) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load(in[i], row + i * step);
+  }
+#pragma unroll 1
+  while (r0 < p.T) {
+    one(in[0]);
+    if (AHEAD == 1) continue;
+    if (r0 >= p.T) break;
+    one(in[AHEAD - 1]);
   }
   if (!p.dg && !p.db) return;
   // the row slots in order, column by column
@@ -464,11 +504,17 @@ int lanes_of(int64_t d, int most) {  // the power of two of lanes that hold a ro
   while (l < most && 8ll * l < d) l *= 2;
   return l;
 }
+// Backward: threads per workgroup, and at most one workgroup per compute unit, two for rows of up
+// to 1024 values. More shares cost the final sum more than their rows gain (4096 rows of
+// 4096, fp32: 256 workgroups 54 us with it, 512 57, 1024 60; 20000 x 768 bf16 37, 33 and 37;
+// 30000 x 100 16.4 and 16.6, 1024 22); 512 threads rather than 1024 (100 x 768 9.3 -> 8.1
+// us, 4096 x 4096 56 -> 54) where a row of one run per lane fits them.
+int bwd_threads(int64_t d) { return d <= 4096 ? 512 : 1024; }
 bool bwd_in_registers(int64_t d) { return d >= 8 && d <= MAXD_BWD; }
 int64_t blocks_of(int64_t T, int64_t d) {
   if (!bwd_in_registers(d)) return (T + LONG_ROWS - 1) / LONG_ROWS;
-  const int slots = NTB / lanes_of(d, NTB);
-  return std::min<int64_t>(MAXBLK, (T + slots - 1) / slots);
+  const int nt = bwd_threads(d), slots = nt / lanes_of(d, nt);
+  return std::min<int64_t>(d <= 1024 ? 512 : 256, (T + slots - 1) / slots);
 }
 size_t scratch_of(int64_t T, int64_t d) {
   return T <= 0 || d <= 0 ? 0 : (size_t)blocks_of(T, d) * (size_t)d * 2 * sizeof(float);
@@ -557,31 +603,32 @@ lc_status forward(const lc_layernorm_args &a, hipStream_t s) {
   } else if (p.d <= 1024) {
     fwd_shape<1, 2>(p, s);
   } else if (p.d <= 2048) {
-    fwd_shape<1, 4>(p, s);
+    if (p.T >= 4096) fwd_shape<1, 4>(p, s);
+    else fwd_shape<2, 2>(p, s);
   } else if (p.d <= 4096) {
-    fwd_shape<1, 8>(p, s);
+    fwd_shape<4, 2>(p, s);
   } else if (p.d <= 8192) {
-    fwd_shape<2, 8>(p, s);
+    fwd_shape<8, 2>(p, s);
   } else if (p.d <= 16384) {
-    fwd_shape<4, 8>(p, s);
+    fwd_shape<16, 2>(p, s);
   } else {
     fwd_shape<16, 8>(p, s);
   }
   return check_launch("layernorm_fwd_kernel");
 }
 
-template <int U>
+template <int U, int NTB>
 void bwd_shape(const LnP &p, hipStream_t s) {
   const dim3 grid((unsigned)p.nblk), block(NTB);
   // (the residual's gradient of another size than dx: every size at run time)
   if (p.dres && (p.dres_dt == LC_FP32) != (p.out_dt == LC_FP32)) {
-    hipLaunchKernelGGL((layernorm_bwd_kernel<0, 0, 0, U>), grid, block, 0, s, p);
+    hipLaunchKernelGGL((layernorm_bwd_kernel<0, 0, 0, U, NTB>), grid, block, 0, s, p);
     return;
   }
   with_size(p.dy_dt, [&](auto ds) {
     with_size(p.x_dt, [&](auto xs) {
       with_size(p.out_dt, [&](auto os) {
-        hipLaunchKernelGGL((layernorm_bwd_kernel<decltype(ds)::value, decltype(xs)::value, decltype(os)::value, U>),
+        hipLaunchKernelGGL((layernorm_bwd_kernel<decltype(ds)::value, decltype(xs)::value, decltype(os)::value, U, NTB>),
                            grid, block, 0, s, p);
       });
     });
@@ -593,11 +640,12 @@ lc_status backward(const lc_layernorm_args &a, hipStream_t s) {
   if (a.T == 0) return LC_OK;
   LnP p = params(a);
   p.nblk = (int)blocks_of(a.T, a.d);
-  p.lpr = lanes_of(a.d, NTB);
+  p.lpr = lanes_of(a.d, bwd_threads(a.d));
   const bool sums = p.dg || p.db;
   if (bwd_in_registers(a.d)) {
-    if (p.d <= 8 * NTB) bwd_shape<1>(p, s);
-    else bwd_shape<2>(p, s);
+    if (p.d <= 4096) bwd_shape<1, 512>(p, s);
+    else if (p.d <= 8192) bwd_shape<1, 1024>(p, s);
+    else bwd_shape<2, 1024>(p, s);
     LC_TRY(check_launch("layernorm_bwd_kernel"));
     if (!sums || p.nblk == 1) return LC_OK;
   } else {
