@@ -24,16 +24,18 @@ namespace {
 constexpr int NTH = 256;
 constexpr int MAXPAIR = 128;
 
-struct RopeP {
-  uint64_t turn[MAXPAIR];  // 2^64 f / (2 pi) of every pair
-  uint8_t axis[MAXPAIR];   // (pairs past the sections: turn 0)
+// N: pairs that it has room for (64: up to 128 values per head; the arguments of a launch cost
+// host time by their size)
+template <int N> struct RopeP {
+  uint64_t turn[N];  // 2^64 f / (2 pi) of every pair (past the sections: 0)
+  int32_t end[3];    // first pair past the section of axis 0, 1, 2
   const int32_t *pos;
   int64_t ld_pos;
   const void *x;
   void *y;
   int64_t ld_x, ld_y, T;
   float *cos, *sin;
-  int heads, half, x_dt, y_dt;
+  int heads, half, axes, x_dt, y_dt;
   int lpg, share;  // lanes per group; waves that share a token's heads
   int64_t first;   // the launch's first workgroup
   float sign;  // 1 forward, -1 backward
@@ -54,8 +56,11 @@ __device__ __forceinline__ void cos_sin(uint64_t u, float &c, float &s) {
   s = quarter & 2 ? -b : b;
 }
 
-__device__ __forceinline__ void pair_cos_sin(const RopeP &p, int64_t t, int i, float &c, float &s) {
-  const int64_t at = p.pos[p.axis[i] * p.ld_pos + t];
+// (a pair past the sections takes the last axis' position times 0)
+template <typename P>
+__device__ __forceinline__ void pair_cos_sin(const P &p, int64_t t, int i, float &c, float &s) {
+  const int axis = min((i >= p.end[0]) + (i >= p.end[1]) + (i >= p.end[2]), p.axes - 1);
+  const int64_t at = p.pos[axis * p.ld_pos + t];
   cos_sin((uint64_t)at * p.turn[i], c, s);
 }
 
@@ -117,8 +122,8 @@ template <int SZ, int RUN> struct Vals {
 
 // Groups of p.lpg lanes (a power of two; lane l holds pairs RUN l ..) take a token's heads in
 // turn; a group's heads are h0, h0 + stride, ..., those of `p.share` waves side by side.
-template <int XS, int YS, int RUN>
-__global__ __launch_bounds__(NTH) void rope_axes_kernel(RopeP p) {
+template <int XS, int YS, int RUN, int N>
+__global__ __launch_bounds__(NTH) void rope_axes_kernel(RopeP<N> p) {
   const int lane = threadIdx.x & 63, l = lane % p.lpg;
   const int64_t w = (p.first + blockIdx.x) * (NTH / 64) + (threadIdx.x >> 6);
   const int64_t t = w / p.share;
@@ -128,22 +133,34 @@ __global__ __launch_bounds__(NTH) void rope_axes_kernel(RopeP p) {
   const int h0 = (int)(w % p.share) * groups + lane / p.lpg;
   const char *x = static_cast<const char *>(p.x) + t * p.ld_x * XS;
   char *y = static_cast<char *>(p.y) + t * p.ld_y * YS;
+  // (RUN = 1: up to 127 pairs on 64 lanes)
+  constexpr int ROUNDS = RUN == 1 && N > 64 ? 2 : 1;
+  Vals<XS, RUN> a, b;
+  auto first = [&](int i0) {
+    if (i0 < p.half && h0 < p.heads) {
+      a.load(x + (h0 * hd + i0) * XS);
+      b.load(x + (h0 * hd + i0 + p.half) * XS);
+    }
+  };
+  first(RUN * l);  // (on their way while cos and sin are formed)
   // pairs `lane` and lane + 64
   float c0 = 1.0f, s0 = 0.0f, c1 = 1.0f, s1 = 0.0f;
   if (lane < p.half) pair_cos_sin(p, t, lane, c0, s0);
-  if (p.half > 64 && lane + 64 < p.half) pair_cos_sin(p, t, lane + 64, c1, s1);
-  // (RUN = 1: up to 127 pairs on 64 lanes)
+  if (N > 64 && lane + 64 < p.half) pair_cos_sin(p, t, lane + 64, c1, s1);
 #pragma unroll
-  for (int round = 0; round < (RUN == 1 ? 2 : 1); ++round) {
+  for (int round = 0; round < ROUNDS; ++round) {
     const int i0 = RUN * (l + p.lpg * round);
-    if (round && p.lpg * round >= p.half) break;
+    if (round) {
+      if (p.lpg >= p.half) break;
+      first(i0);
+    }
     float c[RUN], s[RUN];
 #pragma unroll
     for (int i = 0; i < RUN; ++i) {
       const int from = (i0 + i) & 63;
       c[i] = __shfl(c0, from, 64);
       s[i] = __shfl(s0, from, 64);
-      if (p.half > 64) {
+      if (N > 64) {
         const float ch = __shfl(c1, from, 64), sh = __shfl(s1, from, 64);
         c[i] = i0 + i < 64 ? c[i] : ch;
         s[i] = i0 + i < 64 ? s[i] : sh;
@@ -151,12 +168,7 @@ __global__ __launch_bounds__(NTH) void rope_axes_kernel(RopeP p) {
       s[i] *= p.sign;
     }
     if (i0 >= p.half) continue;
-    Vals<XS, RUN> a, b;
     int h = h0;
-    if (h < p.heads) {
-      a.load(x + (h * hd + i0) * XS);
-      b.load(x + (h * hd + i0 + p.half) * XS);
-    }
     while (h < p.heads) {
       const int hn = h + stride;
       Vals<XS, RUN> an, bn;
@@ -183,7 +195,8 @@ __global__ __launch_bounds__(NTH) void rope_axes_kernel(RopeP p) {
   }
 }
 
-__global__ __launch_bounds__(NTH) void rope_table_kernel(RopeP p) {
+template <int N>
+__global__ __launch_bounds__(NTH) void rope_table_kernel(RopeP<N> p) {
   const int64_t n = (p.first + blockIdx.x) * NTH + threadIdx.x;
   if (n >= p.T * p.half) return;
   float c, s;
@@ -230,19 +243,26 @@ lc_status check(const lc_rope_axes_args &a, Kind kind) {
   return LC_OK;
 }
 
-RopeP params(const lc_rope_axes_args &a, Kind kind) {
-  RopeP p{};
-  const long double turns = powl(2.0L, 63) / 3.14159265358979323846264338327950288L;  // 2^64 / (2 pi)
-  int i = 0;
+template <int N>
+RopeP<N> params(const lc_rope_axes_args &a, Kind kind) {
+  RopeP<N> p{};
+  const long double turns = 0x1p63L / 3.14159265358979323846264338327950288L;  // 2^64 / (2 pi)
+  // f goes down by the same factor from pair to pair (over the head, or from 1 in each section)
+  const bool own = a.freq == LC_ROPE_FREQ_AXIS;
+  long double f = 1.0L, step = 1.0L;
+  int i = 0, run = 0;
   for (int ax = 0; ax < a.n_axes; ++ax) {
-    const int n = a.freq == LC_ROPE_FREQ_AXIS ? a.sections[ax] : a.hd / 2;
-    const long double step = n > 0 ? powl((long double)a.base, -1.0L / n) : 1.0L;
-    long double f = a.freq == LC_ROPE_FREQ_AXIS ? 1.0L : powl((long double)a.base, -(long double)i / n);
-    for (int j = 0; j < a.sections[ax]; ++j, ++i, f *= step) {
-      p.turn[i] = (uint64_t)llroundl(f * turns);  // (at most 2^62)
-      p.axis[i] = (uint8_t)ax;
+    const int n = own ? a.sections[ax] : a.hd / 2;
+    if (n > 0 && n != run) {
+      step = powl((long double)a.base, -1.0L / n);
+      run = n;
     }
+    if (own) f = 1.0L;
+    for (int j = 0; j < a.sections[ax]; ++j, ++i, f *= step) p.turn[i] = (uint64_t)llroundl(f * turns);  // (under 2^62)
+    if (ax < 3) p.end[ax] = i;
   }
+  for (int ax = a.n_axes; ax < 3; ++ax) p.end[ax] = N;
+  p.axes = a.n_axes;
   p.pos = a.pos;
   p.ld_pos = a.ld_pos;
   p.x = a.x;
@@ -260,8 +280,8 @@ RopeP params(const lc_rope_axes_args &a, Kind kind) {
   return p;
 }
 
-template <int XS, int YS>
-void rotate(RopeP p, hipStream_t s) {
+template <int XS, int YS, int N>
+void rotate(RopeP<N> p, hipStream_t s) {
   // the longest run that a head's pairs consist of (16-byte accesses at 8 values of 16 bits)
   const int run = p.half % 8 == 0 ? 8 : p.half % 4 == 0 ? 4 : p.half % 2 == 0 ? 2 : 1;
   p.lpg = 1;
@@ -274,34 +294,39 @@ void rotate(RopeP p, hipStream_t s) {
   const int64_t wgs = (p.T * p.share + NTH / 64 - 1) / (NTH / 64);
   launch_parts((uint32_t)wgs, [&](uint32_t first, uint32_t count) {
     p.first = first;
-    if (run == 8) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 8>), dim3(count), dim3(NTH), 0, s, p);
-    else if (run == 4) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 4>), dim3(count), dim3(NTH), 0, s, p);
-    else if (run == 2) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 2>), dim3(count), dim3(NTH), 0, s, p);
-    else hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 1>), dim3(count), dim3(NTH), 0, s, p);
+    if (run == 8) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 8, N>), dim3(count), dim3(NTH), 0, s, p);
+    else if (run == 4) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 4, N>), dim3(count), dim3(NTH), 0, s, p);
+    else if (run == 2) hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 2, N>), dim3(count), dim3(NTH), 0, s, p);
+    else hipLaunchKernelGGL((rope_axes_kernel<XS, YS, 1, N>), dim3(count), dim3(NTH), 0, s, p);
   });
+}
+
+template <int N>
+lc_status launch(const lc_rope_axes_args &a, Kind kind, hipStream_t s) {
+  RopeP<N> p = params<N>(a, kind);
+  if (kind == TABLE) {
+    launch_parts(ceil_div((size_t)p.T * p.half, NTH), [&](uint32_t first, uint32_t count) {
+      p.first = first;
+      hipLaunchKernelGGL(rope_table_kernel<N>, dim3(count), dim3(NTH), 0, s, p);
+    });
+    return check_launch("rope_table_kernel");
+  }
+  if (p.x_dt == LC_FP32) {
+    if (p.y_dt == LC_FP32) rotate<4, 4, N>(p, s);
+    else rotate<4, 2, N>(p, s);
+  } else {
+    if (p.y_dt == LC_FP32) rotate<2, 4, N>(p, s);
+    else rotate<2, 2, N>(p, s);
+  }
+  return check_launch("rope_axes_kernel");
 }
 
 lc_status run(const lc_rope_axes_args *args, Kind kind, void *stream) {
   if (!args) return fail(LC_ERR_INVALID_ARG, "rope axes: null args");
   LC_TRY(check(*args, kind));
   if (args->T == 0) return LC_OK;
-  RopeP p = params(*args, kind);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (kind == TABLE) {
-    launch_parts(ceil_div((size_t)p.T * p.half, NTH), [&](uint32_t first, uint32_t count) {
-      p.first = first;
-      hipLaunchKernelGGL(rope_table_kernel, dim3(count), dim3(NTH), 0, s, p);
-    });
-    return check_launch("rope_table_kernel");
-  }
-  if (p.x_dt == LC_FP32) {
-    if (p.y_dt == LC_FP32) rotate<4, 4>(p, s);
-    else rotate<4, 2>(p, s);
-  } else {
-    if (p.y_dt == LC_FP32) rotate<2, 4>(p, s);
-    else rotate<2, 2>(p, s);
-  }
-  return check_launch("rope_axes_kernel");
+  return args->hd <= 128 ? launch<64>(*args, kind, s) : launch<MAXPAIR>(*args, kind, s);
 }
 
 }  // namespace
