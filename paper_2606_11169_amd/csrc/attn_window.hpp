@@ -6,11 +6,11 @@
 
 namespace lc {
 
-// Where the backward's scratch holds what (bytes from its start; -1: not needed), and the
-// split of its work that this follows from (k_attn_window.hip)
+// Where the backward's scratch holds what (bytes from its start), and the split of its work
+// that this follows from (k_attn_window.hip)
 struct WindowPlan {
   int64_t D, nl2;          // fp32 [H, T] each
-  int64_t kb, vb, qb;      // fp16 inputs: bf16 rows of k, v [T, Hkv hd] and q [T, H hd]
+  int64_t inv;             // fp16 inputs: fp32 [H, T]
   int64_t share;           // fp32 dk, then dv [parts, T, Hkv hd]
   int64_t slots;           // fp32 sums of sinks: [2, chunks, Hkv, parts, n_sink, 2, hd]
   int64_t total;

@@ -5,7 +5,16 @@
 // The products, the online softmax and the LDS row tiles are those of causal attention
 // (k_attn.hip): S^T = K Q^T with one query per lane pair, O^T += V^T P^T with the score
 // registers as operand; backward dQ^T += K^T dS^T over keys, dV^T += dO^T P and dK^T += Q^T dS
-// over queries, P recomputed from the log-sum-exp, gradient products in bf16.
+// over queries, P recomputed from the log-sum-exp. P and dS are rounded once, to the type of
+// the product that takes them.
+//
+// fp16 q, k, v: a gradient's range does not fit fp16, its rows' do. A query's dO is multiplied by
+// the power of two that brings its largest value into [1, 2) (row_scale), which makes dP = dO V^T
+// and dQ = dS K fp16 products of the caller's own k and v, exact but for dS's rounding, undone
+// in fp32. dV and dK sum over queries, so P and dS are bf16 there, and q's rows are rounded to
+// bf16 on their way from LDS. (With bf16 copies of q, k and v for every gradient product the
+// gradients were 1.85 times as far from 64 bits as their last rounding alone, now 1.4, like those
+// of bf16 inputs.)
 //
 // Work is laid over the packed rows, not over the sequences: a workgroup owns consecutive
 // rows whatever sequences they belong to, each row knows its sequence's start (a search
@@ -31,7 +40,8 @@ namespace lc {
 namespace {
 
 constexpr int KB = 64;         // keys (or queries) per inner block
-constexpr int KV_ROWS = 128;   // keys per dK/dV workgroup
+constexpr int NP = 2;          // dK/dV: pairs of waves of a workgroup
+constexpr int KROWS = 32 * NP; // and the keys that they own
 constexpr int MAXSINK = 256;   // sinks whose dK/dV work is split over chunks of queries
 
 // ---------------------------------------------------------------- row tiles
@@ -67,6 +77,19 @@ template <int HD> struct Tile {
   }
 };
 
+// The lane's number, with head_dim 128 formed anew where it is used: what depends on it need not be
+// held across a loop whose registers are full. (The reload of a spilled register also waits for
+// every load that is on its way to LDS: dK/dV of 32768 tokens, 16/4 heads, window 4096 2456 us with
+// one such reload per block, 2169 without. head_dim 64 has registers to spare: 8192 x 32/8 heads 190
+// us, 210 this way.)
+template <int HD>
+__device__ __forceinline__ int lane_again(int lane) {
+  if (HD == 64) return lane;
+  uint32_t zero = 0;
+  asm volatile("" : "+v"(zero));
+  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
+}
+
 template <typename VT>
 __device__ __forceinline__ VT frag_at(const lds_t *t) {
   return *reinterpret_cast<const __attribute__((address_space(3))) VT *>(t);
@@ -87,15 +110,14 @@ struct WinP {
   float *lse;
   const __bf16 *dout;
   __bf16 *dq, *dk, *dv;
-  const __bf16 *qb, *kb, *vb;  // bf16 rows for the gradient products (copies for fp16 inputs)
-  __bf16 *qb_w, *kb_w, *vb_w;  // where the copies are written (null: none)
-  float *D, *nl2;              // [H, T]: rowsum(dO * O) and -lse log2(e)
+  float *D, *nl2;              // [H, T]: rowsum(dO * O) (fp16: scaled) and -lse log2(e)
+  float *inv;                  // fp16 inputs: the inverses of dO's row scales, [H, T]
   float *share, *slots;
   const int32_t *off;
-  int64_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv, ld_qb, ld_kb, ld_vb;
+  int64_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
   int T, B, S, H, Hkv, G, window, n_sink;
   int gh, nq;                  // forward, dQ: heads per workgroup, blocks of query rows
-  int GP, parts;               // dK/dV: query heads per workgroup
+  int GP, parts, period;       // dK/dV: query heads per workgroup, blocks of a window (see the walk; 0: none)
   int chunk, chunks;
   int nmain, nsplit, nkb;      // dK/dV workgroups; 128-key blocks that hold a sequence's sinks
   float scale;
@@ -133,8 +155,8 @@ __device__ __forceinline__ bool not_finite(const f32x16_v (&a)[NI]) {
 
 // acc[column e of the tile][lane] += w[row][lane] * tile[row][e] over 32 NJ rows from row0 on
 // that vis(row - row0) lets the lane see, pair by pair. w: the score registers (rows in
-// accumulator order), rounded to E as the product rounds them.
-template <typename E, int HD, int NJ, typename F>
+// accumulator order), rounded to E as the product rounds them; TE: the tile's type.
+template <typename E, typename TE, int HD, int NJ, typename F>
 __device__ __forceinline__ void add_pairs(f32x16_v (&acc)[HD / 32], const f32x16_v (&w)[NJ], const lds_t *tile,
                                           int row0, int hf, F vis) {
 #pragma unroll 1
@@ -154,7 +176,7 @@ __device__ __forceinline__ void add_pairs(f32x16_v (&acc)[HD / 32], const f32x16
     for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        typedef __attribute__((ext_vector_type(4))) E e4;
+        typedef __attribute__((ext_vector_type(4))) TE e4;
         const e4 x = frag_at<e4>(row + (32 * i + 8 * g) * 2);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -370,7 +392,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_fwd_kernel(WinP p) {
           }
         l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
         if (masked && pairs) {
-          add_pairs<QE, HD, 2>(o, s, cur + TL::BYTES, 0, hf, [&](int n) { return R.sees(k0 + n); });
+          add_pairs<QE, QE, HD, 2>(o, s, cur + TL::BYTES, 0, hf, [&](int n) { return R.sees(k0 + n); });
         } else {
           // V^T fragments of step n (keys 16 n ..) read while step n - 1 multiplies
           const uint32_t av = (uint32_t)(uintptr_t)(cur + TL::BYTES) + TL::cols_lane(lane);
@@ -404,29 +426,22 @@ __global__ __launch_bounds__(64 * NW, 2) void window_fwd_kernel(WinP p) {
 }
 
 // ---------------------------------------------------------------- backward
-// fp16 inputs: bf16 rows of k and v for the gradient products, 8 elements per thread (q's are
-// written by the dQ kernel, which holds them)
-__global__ __launch_bounds__(256) void window_copy_kernel(WinP p, int width) {
-  const int cpr = width / 8;  // chunks per row
-  const int64_t n = (int64_t)p.T * cpr;
-  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const bool isv = i >= n;
-  if (isv) i -= n;
-  if (i >= n) return;
-  const int64_t r = i / cpr, c = 8 * (i % cpr);
-  const _Float16 *const x = static_cast<const _Float16 *>(isv ? p.v : p.k) + r * (isv ? p.ld_v : p.ld_k) + c;
-  *reinterpret_cast<bf16x8_v *>((isv ? p.vb_w : p.kb_w) + r * width + c) =
-      to_bf16x8<_Float16>(*reinterpret_cast<const uint4 *>(x));
+// the power of two that brings a row's largest absolute value x into [1, 2) (1 for a row of zeros,
+// at most 2^100)
+__device__ __forceinline__ float row_scale(float x) {
+  const int e = (int)(__float_as_uint(x) >> 23);
+  return x > 0.0f ? __uint_as_float((uint32_t)(254 - min(max(e, 27), 253)) << 23) : 1.0f;
 }
 
-// dQ, D and -lse log2(e): LDS stage = K (QE) | V (bf16), plus the bf16 rows of K for fp16 inputs
+// dQ, and what dK/dV needs of every query: D, -lse log2(e) and, for fp16 inputs, the inverse of its dO
+// row's scale. LDS stage = K | V.
 template <typename QE, int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
   typedef typename V8<QE>::type QV;
   typedef Tile<HD> TL;
-  constexpr bool SEP = !std::is_same<QE, __bf16>::value;  // separate bf16 K tile
-  constexpr int NT = SEP ? 3 : 2, NES = HD / 16, NI = HD / 32, RPW = NT * TL::NR / NW;
-  __shared__ __align__(16) char smem[2 * NT * TL::BYTES];
+  constexpr bool F16 = !std::is_same<QE, __bf16>::value;
+  constexpr int NES = HD / 16, NI = HD / 32, RPW = 2 * TL::NR / NW;
+  __shared__ __align__(16) char smem[2 * 2 * TL::BYTES];
   lds_t *const L = LDS_AS(char, smem);
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -437,56 +452,70 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
   const int kvh = h / p.G;
   const float sc = p.scale * LOG2E;
   const bool ok = R.nwin > 0;
+  // half of the waves stream K, the other half V, RPW runs each
+  const bool isK = w < NW / 2;
+  const int run0 = RPW * (w % (NW / 2));
+  const int64_t ld = isK ? p.ld_k : p.ld_v;
+  const uint32_t vo = (uint32_t)((TL::lane_row(lane) * ld + 8 * TL::lane_chunk(lane)) * 2);
+  const uint32_t rowb = (uint32_t)(ld * 2);
   auto load = [&](int kb, lds_t *st) {
-    const i32x4_v rk = block_rsrc<HD>(p.k, p.ld_k, kvh * HD, kb * KB, p.T);
-    const i32x4_v rv = block_rsrc<HD>(p.vb, p.ld_vb, kvh * HD, kb * KB, p.T);
-    const i32x4_v rb = block_rsrc<HD>(p.kb, p.ld_kb, kvh * HD, kb * KB, p.T);
+    const i32x4_v rs = block_rsrc<HD>(isK ? p.k : p.v, ld, kvh * HD, kb * KB, p.T);
 #pragma unroll
-    for (int t = 0; t < RPW; ++t) {
-      const int run = RPW * w + t, which = run / TL::NR, r = run % TL::NR;  // (wave-uniform)
-      const int64_t ld = which == 0 ? p.ld_k : which == 1 ? p.ld_vb : p.ld_kb;
-      const uint32_t off = (uint32_t)(((TL::lane_row(lane) + TL::run_row(r)) * ld + 8 * TL::lane_chunk(lane)) * 2);
-      dma16(which == 0 ? rk : which == 1 ? rv : rb, st + run * RUNB, off);
-    }
+    for (int t = 0; t < RPW; ++t)
+      dma16(rs, st + (isK ? 0 : TL::BYTES) + (run0 + t) * RUNB, vo + rowb * (uint32_t)TL::run_row(run0 + t));
   };
   const int64_t si = (int64_t)h * p.T + min(R.row, p.T - 1);
   const float lse2 = ok ? p.lse[si] * LOG2E : 0.0f;
-  float Dq = 0.0f;
+  float Dq = 0.0f, scale = 1.0f;  // (D, and with it dP and dS, in units of 1 / scale)
   f32x16_v acc[NI];
   auto pass = [&](auto pairs_) {
     constexpr bool pairs = decltype(pairs_)::value;
     if (R.nit > 0) load(R.block(0), L);
-    QV qf[NES];
-    bf16x8_v df[NES];
+    QV qf[NES], df[NES];
     load_row<QV, HD>(qf, static_cast<const QE *>(p.q) + (int64_t)h * HD, p.ld_q, R.row, p.T, hf);
-    load_row<bf16x8_v, HD>(df, p.dout + (int64_t)h * HD, p.ld_do, R.row, p.T, hf);
+    bf16x8_v d16[NES];
+    load_row<bf16x8_v, HD>(d16, p.dout + (int64_t)h * HD, p.ld_do, R.row, p.T, hf);
     if constexpr (!pairs) {
-      // D of this query (its O row read while the first block streams in), and q's bf16 copy
+      // D of this query (its O row read while the first block streams in)
       bf16x8_v of[NES];
       load_row<bf16x8_v, HD>(of, static_cast<const __bf16 *>(p.o) + (int64_t)h * HD, p.ld_o, R.row, p.T, hf);
+      float mx = 0.0f;
 #pragma unroll
       for (int es = 0; es < NES; ++es)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) Dq += (float)df[es][e] * (float)of[es][e];
+        for (int e = 0; e < 8; ++e) {
+          Dq += (float)d16[es][e] * (float)of[es][e];
+          if (F16) mx = fmaxf(mx, fabsf((float)d16[es][e]));
+        }
       Dq = sum_with_partner(Dq);
-      if (ok && hf == 0) {
-        p.D[si] = Dq;
-        p.nl2[si] = -lse2;
-      }
-      if (SEP && R.row < p.T) {
+      if constexpr (F16) scale = row_scale(max_with_partner(mx));
+    } else if constexpr (F16) {
+      // (dS over the range of fp16, with a |v| of some thousands, is one reason to be here)
+      scale *= 0x1p-12f;
+      Dq *= 0x1p-12f;
+    }
+    if constexpr (F16) {
 #pragma unroll
-        for (int es = 0; es < NES; ++es)
-          *reinterpret_cast<bf16x8_v *>(p.qb_w + R.row * p.ld_qb + (int64_t)h * HD + es * 16 + hf * 8) =
-              to_bf16x8<QE>(__builtin_bit_cast(uint4, qf[es]));
-      }
+      for (int es = 0; es < NES; ++es)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) df[es][e] = (QE)((float)d16[es][e] * scale);
+      if constexpr (!pairs) Dq *= scale;
+    } else {
+#pragma unroll
+      for (int es = 0; es < NES; ++es) df[es] = __builtin_bit_cast(QV, d16[es]);
+    }
+    if (!pairs && ok && hf == 0) {
+      p.D[si] = Dq;
+      p.nl2[si] = -lse2;
+      if (F16) p.inv[si] = 1.0f / scale;
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) acc[i] = zero16();
     wait_vm0();
     __syncthreads();
     for (int it = 0; it < R.nit; ++it) {
-      const lds_t *cur = L + (it & 1) * NT * TL::BYTES;
-      if (it + 1 < R.nit) load(R.block(it + 1), L + ((it + 1) & 1) * NT * TL::BYTES);
+      const lds_t *cur = L + (it & 1) * 2 * TL::BYTES;
+      if (it + 1 < R.nit) load(R.block(it + 1), L + ((it + 1) & 1) * 2 * TL::BYTES);
       const int k0 = R.block(it) * KB;
       if (R.any(k0, p.n_sink)) {
         f32x16_v s[2] = {zero16(), zero16()}, dp[2] = {zero16(), zero16()};
@@ -498,9 +527,9 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
         kf[0][1] = frag_at<QV>(krow + 512);
 #pragma unroll
         for (int es = 0; es < NES; ++es) {
-          bf16x8_v vf[2];
-          vf[0] = frag_at<bf16x8_v>(vrow + 32 * es);
-          vf[1] = frag_at<bf16x8_v>(vrow + 512 + 32 * es);
+          QV vf[2];
+          vf[0] = frag_at<QV>(vrow + 32 * es);
+          vf[1] = frag_at<QV>(vrow + 512 + 32 * es);
           __builtin_amdgcn_sched_barrier(0);
           s[0] = mfma(kf[es & 1][0], qf[es], s[0]);
           s[1] = mfma(kf[es & 1][1], qf[es], s[1]);
@@ -531,19 +560,16 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
               dp[j][r] = pv * (dp[j][r] - Dq);
             }
         }
-        // K^T fragments: transposing reads of the bf16 K rows in dS's key order
-        const lds_t *kt = cur + (SEP ? 2 * TL::BYTES : 0);
+        // K^T fragments: transposing reads of the K rows in dS's key order
         if (masked && pairs) {
-          add_pairs<__bf16, HD, 2>(acc, dp, kt, 0, hf, [&](int n) { return R.sees(k0 + n); });
+          add_pairs<QE, QE, HD, 2>(acc, dp, cur, 0, hf, [&](int n) { return R.sees(k0 + n); });
         } else {
-          uint32_t cl = TL::cols_lane(lane);
-          asm volatile("" : "+v"(cl));  // recomputed each block, not held across the loop
-          const uint32_t ak = (uint32_t)(uintptr_t)kt + cl;
+          const uint32_t ak = (uint32_t)(uintptr_t)cur + TL::cols_lane(lane_again<HD>(lane));
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
-            const bf16x8_v sf = pack8<__bf16>(dp[n >> 1], 8 * (n & 1));
+            const QV sf = pack8<QE>(dp[n >> 1], 8 * (n & 1));
 #pragma unroll
-            for (int i = 0; i < NI; ++i) acc[i] = mfma(frag_cols_x<bf16x8_v>(ak, i, 16 * n), sf, acc[i]);
+            for (int i = 0; i < NI; ++i) acc[i] = mfma(frag_cols_x<QV>(ak, i, 16 * n), sf, acc[i]);
           }
         }
       }
@@ -553,14 +579,14 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
   };
   pass(std::false_type{});
   if (__syncthreads_or(not_finite(acc))) pass(std::true_type{});
-  if (ok) store_bf16<HD>(p.dq + (int64_t)R.row * p.ld_dq + (int64_t)h * HD, acc, p.scale, hf);
+  if (ok) store_bf16<HD>(p.dq + (int64_t)R.row * p.ld_dq + (int64_t)h * HD, acc, p.scale / scale, hf);
 }
 
-// dK, dV. A workgroup of 8 waves owns 128 consecutive key rows of a key/value head and
+// dK, dV. A workgroup of 2 NP waves owns 32 NP consecutive key rows of a key/value head and
 // visits, for GP of the head's query heads, the query blocks that see them. Waves w and
-// w + 4 own the same 32 keys (K and V fragments in registers) and take the first and second 32
-// queries of every 64-query block; at the end wave w + 4 hands its sums to wave w, which
-// adds them. LDS stage = Q (QE) | dO | (fp16: bf16 Q) | -lse log2(e) | D of one block.
+// w + NP own the same 32 keys (K and V fragments in registers) and take the first and second 32
+// queries of every 64-query block; at the end wave w + NP hands its sums to wave w, which
+// adds them. LDS stage = Q | dO | -lse log2(e) | D | (fp16: the scales' inverses) of one block.
 //
 // Sinks are seen by their whole sequence, so the workgroup that owns them would visit all
 // of its queries, however long, while every other visits a window's. Where a sequence
@@ -573,7 +599,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
 // With few keys (p.parts > 1) several workgroups share a key block's query heads and write
 // fp32 shares, which window_sum_kernel adds in head order.
 __device__ __forceinline__ int limit(const WinP &p, int s, int kblk) {
-  return max(kblk * KV_ROWS + KV_ROWS - 1 + p.window, (s / p.chunk + 1) * p.chunk);
+  return max((kblk + 1) * KROWS - 1 + p.window, (s / p.chunk + 1) * p.chunk);
 }
 // a slot of [dk | dv], 2 HD floats: set 0 the owner's sums (by the chunk that the sequence
 // starts in), set 1 a chunk's
@@ -583,27 +609,45 @@ __device__ __forceinline__ float *slot(const WinP &p, int set, int c, int kvh, i
          ((((((int64_t)set * p.chunks + c) * p.Hkv + kvh) * p.parts + part) * p.n_sink) + sink) * (2 * HD);
 }
 
+// fp16 inputs: 8 values of a dO row times its scale, as fp16. c: the scale as (e - 15) << 7 in both
+// halves, e the exponent of the row's largest value in bf16's terms, so that exponents fall by
+// e - 15 and fp16's bias is 15. What falls below fp16's range (2^-14 of the row's largest value) is
+// left as a mantissa of the exponent 0, off by less than that.
+__device__ __forceinline__ f16x8_v scaled_row(bf16x8_v x, uint32_t c) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_v;
+  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_v;
+  u32x4_v v = __builtin_bit_cast(u32x4_v, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u16x2_v a = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2_v, v[i] & 0x7FFF7FFFu),
+                                                    __builtin_bit_cast(u16x2_v, c));
+    v[i] = (v[i] & 0x80008000u) | __builtin_bit_cast(uint32_t, a << (uint16_t)3);
+  }
+  return __builtin_bit_cast(f16x8_v, v);
+}
+
 template <typename QE, int HD> constexpr int dkdv_stage() {
-  return (std::is_same<QE, __bf16>::value ? 2 : 3) * Tile<HD>::BYTES + 512;
+  return 2 * Tile<HD>::BYTES + (std::is_same<QE, __bf16>::value ? 512 : 768);
 }
 template <typename QE, int HD> constexpr int dkdv_smem() {
-  constexpr int handoff = 4 * HD * 64 * 4;
+  constexpr int handoff = NP * HD * 64 * 4;
   return 2 * dkdv_stage<QE, HD>() > handoff ? 2 * dkdv_stage<QE, HD>() : handoff;
 }
 
 template <typename QE, int HD>
-__global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
+__global__ __launch_bounds__(128 * NP, 2) void window_dkdv_kernel(WinP p) {
   typedef typename V8<QE>::type QV;
   typedef Tile<HD> TL;
-  constexpr bool SEP = !std::is_same<QE, __bf16>::value;  // separate bf16 Q tile
-  constexpr int NT = SEP ? 3 : 2, NES = HD / 16, NI = HD / 32;
-  constexpr int RPW = TL::NR / (SEP ? 2 : 4);             // tile runs per wave
+  constexpr bool F16 = !std::is_same<QE, __bf16>::value;
+  constexpr int NES = HD / 16, NI = HD / 32;
+  constexpr int RPW = TL::NR / NP;  // tile runs per wave
   constexpr int STAGE = dkdv_stage<QE, HD>();
   __shared__ __align__(256) char smem[dkdv_smem<QE, HD>()];
+  __shared__ int keys[2][KROWS];  // lo and cnt (below) of every key
   lds_t *const L = LDS_AS(char, smem);
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int pw = w & 3, hq = w >> 2;  // key block of the pair, query half
+  const int pw = w % NP, hq = w / NP;  // key block of the pair, query half
   const bool splits = p.chunks > 1;
 
   // the task: keys kblk, queries [qa, qb) of sequence [s, e) (the one past the block's last key)
@@ -622,19 +666,19 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
       c = 1 + i / p.Hkv;
       const int r = c * p.chunk;
       if (!sq.of_wave(r, lane, b, s, e) || s >= r) return;
-      kblk = s / KV_ROWS + kbi;
-      if (kblk * KV_ROWS >= min(s + p.n_sink, e)) return;
+      kblk = s / KROWS + kbi;
+      if (kblk * KROWS >= min(s + p.n_sink, e)) return;
       qa = max(r, limit(p, s, kblk));
       qb = min(e, r + p.chunk);
       if (qa >= qb) return;
     } else {
       const int t = xcd_task(i - pad, p.nmain);
       if (t < 0) return;
-      const int nb = (p.T + KV_ROWS - 1) / KV_ROWS;
+      const int nb = (p.T + KROWS - 1) / KROWS;
       kblk = t % nb;
       kvh = t / nb % p.Hkv;
       part = t / nb / p.Hkv;
-      const int k0 = kblk * KV_ROWS, r1 = min(k0 + KV_ROWS, sq.last) - 1;
+      const int k0 = kblk * KROWS, r1 = min(k0 + KROWS, sq.last) - 1;
       if (r1 < max(k0, sq.first) || !sq.of_wave(r1, lane, b, s, e)) return;
       qa = k0;
       qb = p.window < e - r1 ? r1 + p.window : e;
@@ -642,7 +686,7 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
     }
   }
   // this lane's key: the queries [lo, lo + cnt) see it
-  const int key = kblk * KV_ROWS + pw * 32 + l32;
+  const int key = kblk * KROWS + pw * 32 + l32;
   int lo = key, cnt = 0, ks = s, ke = e;
   bool later = false;  // its sums are joined from slots
   if (c >= 0) {
@@ -652,7 +696,7 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
     }
   } else {
     bool ok = key < e;
-    if (s > kblk * KV_ROWS) ok = sq.of_lane(key, 0, ks, ke);  // (more than one sequence)
+    if (s > kblk * KROWS) ok = sq.of_lane(key, 0, ks, ke);  // (more than one sequence)
     if (ok) {
       const bool sink = key - ks < p.n_sink;
       int hi = sink || p.window >= ke - key ? ke : key + p.window;
@@ -668,68 +712,81 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
   const int lo_min = wave_min32(cnt ? lo : NONE), lo_max = wave_max32(cnt ? lo : NONE);
   const int hi_max = wave_max32(cnt ? lo + cnt : -1), hi_min = wave_min32(lo + cnt);
   const int64_t krow = min(key, p.T - 1);
+  if (hq == 0 && hf == 0) {
+    keys[0][pw * 32 + l32] = lo;
+    keys[1][pw * 32 + l32] = cnt;
+  }
   const float sc = p.scale * LOG2E;
 
-  // wave w brings runs RPW sub .. + RPW - 1 of tile tl (Q, dO, bf16 Q; with three tiles waves 6
-  // and 7 bring none); the last wave also brings -lse log2(e) and D (64 floats each)
-  const int tl = SEP ? (w >> 1) : (w >> 2), sub = SEP ? (w & 1) : (w & 3);
-  const bool brings = tl < NT;  // wave-uniform
-  const void *const src = tl == 0 ? p.q : tl == 1 ? static_cast<const void *>(p.dout) : p.qb;
-  const int64_t ld = tl == 0 ? p.ld_q : tl == 1 ? p.ld_do : p.ld_qb;
-  const uint32_t vo = (uint32_t)((TL::lane_row(lane) * ld + 8 * TL::lane_chunk(lane)) * 2);
+  // half of the waves bring Q, half dO, RPW runs each; the last one also -lse log2(e), D and the
+  // inverses (64 floats each)
+  const int tl = w / NP, sub = w % NP;
+  const void *const src = tl == 0 ? p.q : static_cast<const void *>(p.dout);
+  const int64_t ld = tl == 0 ? p.ld_q : p.ld_do;
   const uint32_t rowb = (uint32_t)(ld * 2);
   const int h0 = kvh * p.G + part * p.GP;
   auto load = [&](int g, int qbi, lds_t *st) {
-    if (brings) {
-      const i32x4_v rs = block_rsrc<HD>(src, ld, (h0 + g) * HD, qbi * KB, p.T);
+    const int ln = lane_again<HD>(lane);
+    const uint32_t vo = (uint32_t)TL::lane_row(ln) * rowb + 16 * TL::lane_chunk(ln);
+    const i32x4_v rs = block_rsrc<HD>(src, ld, (h0 + g) * HD, qbi * KB, p.T);
 #pragma unroll
-      for (int t = 0; t < RPW; ++t) {
-        const int run = RPW * sub + t;
-        dma16(rs, st + tl * TL::BYTES + run * RUNB, vo + rowb * (uint32_t)TL::run_row(run));
-      }
+    for (int t = 0; t < RPW; ++t) {
+      const int run = RPW * sub + t;
+      dma16(rs, st + tl * TL::BYTES + run * RUNB, vo + rowb * (uint32_t)TL::run_row(run));
     }
-    if (w == 7) {
+    if (w == 2 * NP - 1) {
       const int64_t at = (int64_t)(h0 + g) * p.T + qbi * KB;
       const uint32_t bytes = (uint32_t)min(KB, p.T - qbi * KB) * 4;
-      dma4(make_rsrc(p.nl2 + at, bytes), st + NT * TL::BYTES, lane * 4);
-      dma4(make_rsrc(p.D + at, bytes), st + NT * TL::BYTES + 256, lane * 4);
+      dma4(make_rsrc(p.nl2 + at, bytes), st + 2 * TL::BYTES, ln * 4);
+      dma4(make_rsrc(p.D + at, bytes), st + 2 * TL::BYTES + 256, ln * 4);
+      if (F16) dma4(make_rsrc(p.inv + at, bytes), st + 2 * TL::BYTES + 512, ln * 4);
     }
   };
   const int qfirst = qa / KB, nqb = max(0, (qb + KB - 1) / KB - qfirst), nit = nqb * p.GP;
+  // The walk over the blocks begins at the one that comes first in a clock of a window's blocks:
+  // workgroups side by side, whose windows overlap a little further on each, are then at the same
+  // block at the same time, so that it comes from the L2 once for all (4096 tokens x 32 heads, window
+  // 1024: 201 -> 193 us, fp16 287 -> 272). Long windows, whose workgroups follow one another through
+  // them anyway, lose by it (32768 tokens, 16/4 heads, window 4096: 2456 -> 2550 us).
+  int turn = p.period > 0 ? (p.period - qfirst % p.period) % p.period : 0;
+  if (turn >= nqb) turn = 0;
   f32x16_v dk[NI], dv[NI];
   auto pass = [&](auto pairs_) {
     constexpr bool pairs = decltype(pairs_)::value;
-    if (nit > 0) load(0, qfirst, L);
-    QV kf[NES];
-    bf16x8_v vf[NES];
+    if (nit > 0) load(0, qfirst + turn, L);
+    QV kf[NES], vf[NES];
 #pragma unroll
     for (int es = 0; es < NES; ++es) {
       const int col = kvh * HD + es * 16 + hf * 8;
       kf[es] = *reinterpret_cast<const QV *>(static_cast<const QE *>(p.k) + krow * p.ld_k + col);
-      vf[es] = to_bf16x8<QE>(*reinterpret_cast<const uint4 *>(static_cast<const QE *>(p.v) + krow * p.ld_v + col));
+      vf[es] = *reinterpret_cast<const QV *>(static_cast<const QE *>(p.v) + krow * p.ld_v + col);
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) dk[i] = dv[i] = zero16();
     wait_vm0();
     __syncthreads();
-    int g = 0, qi = 0;  // head and block of this iteration
+    int g = 0, qi = turn;  // head and block of this iteration
     for (int it = 0; it < nit; ++it) {
       const lds_t *cur = L + (it & 1) * STAGE;
-      int gn = g, qn = qi + 1;
-      if (qn == nqb) {
-        qn = 0;
-        ++gn;
-      }
+      int gn = g, qn = qi + 1 < nqb ? qi + 1 : 0;
+      if (qn == turn) ++gn;
       if (it + 1 < nit) load(gn, qfirst + qn, L + ((it + 1) & 1) * STAGE);
       const int q0 = (qfirst + qi) * KB + 32 * hq;  // this wave's 32 queries
       if (q0 + 31 >= lo_min && q0 < hi_max) {
         f32x16_v sv = zero16(), dp = zero16();
-        // fragment rows of this wave's 32 queries: a per-lane base, made opaque
-        // each block (so that it is not held across the loop), plus immediates
-        uint32_t rl = TL::rows_lane(lane) + 512 * hq;
-        asm volatile("" : "+v"(rl));
-        const lds_t *qrow = cur + rl;
+        // fragment rows of this wave's 32 queries: a per-lane base plus immediates
+        const int ln = lane_again<HD>(lane), lh = ln >> 5;
+        const lds_t *qrow = cur + TL::rows_lane(ln) + 512 * hq;
         // each fragment is read one product ahead of the product that uses it
+        uint32_t rs = 0;  // this fragment row's scale
+        if constexpr (F16) {
+          rs = (frag_at<uint32_t>(cur + 2 * TL::BYTES + 512 + 128 * hq + 4 * (ln & 31)) >> 23) - 15;
+          rs = rs << 7 | rs << 23;
+        }
+        auto scaled = [&](bf16x8_v x) -> QV {
+          if constexpr (F16) return scaled_row(x, rs);
+          else return x;
+        };
         QV qv = frag_at<QV>(qrow);
         bf16x8_v da = frag_at<bf16x8_v>(qrow + TL::BYTES);
 #pragma unroll
@@ -741,7 +798,7 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
           sv = mfma(qv, kf[es], sv);
           if (es + 1 < NES) dx = frag_at<bf16x8_v>(qrow + TL::BYTES + 32 * (es + 1));
           __builtin_amdgcn_sched_barrier(0);
-          dp = mfma(da, vf[es], dp);
+          dp = mfma(scaled(da), vf[es], dp);
           __builtin_amdgcn_sched_barrier(0);
           qv = qx;
           da = dx;
@@ -749,55 +806,55 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
         const bool masked = !(q0 >= lo_max && q0 + 31 < hi_min);
         // four rows at a time: their -lse log2(e) and D are 4 consecutive floats each
         typedef __attribute__((ext_vector_type(4))) float f4_t;
-        const lds_t *const st = cur + NT * TL::BYTES + 128 * hq + 16 * hf;
+        const lds_t *const st = cur + 2 * TL::BYTES + 128 * hq + 16 * lh;
 #pragma unroll
         for (int gq = 0; gq < 4; ++gq) {
           const f4_t lc = frag_at<f4_t>(st + 32 * gq), dc = frag_at<f4_t>(st + 256 + 32 * gq);
+          f4_t ic{};
+          if (F16) ic = frag_at<f4_t>(st + 512 + 32 * gq);
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const int r = 4 * gq + x;  // out_row(r, hf) = 8 gq + 4 hf + x
             const float pv = ex2(__builtin_fmaf(sv[r], sc, lc[x]));
             sv[r] = pv;
-            dp[r] = pv * (dp[r] - dc[x]);
+            dp[r] = (F16 ? pv * ic[x] : pv) * (dp[r] - dc[x]);
           }
         }
         if (masked) {
-          const int d = q0 - lo + 4 * hf;
+          const int at = pw * 32 + (ln & 31), d = q0 - keys[0][at] + 4 * lh;
+          const uint32_t n = keys[1][at];
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (!((uint32_t)(d + out_row(r, 0)) < (uint32_t)cnt)) sv[r] = dp[r] = 0.0f;
+            if (!((uint32_t)(d + out_row(r, 0)) < n)) sv[r] = dp[r] = 0.0f;
         }
         if (masked && pairs) {
           auto vis = [&](int n) { return (uint32_t)(q0 + n - lo) < (uint32_t)cnt; };
           const f32x16_v w1[1] = {sv}, w2[1] = {dp};
-          add_pairs<__bf16, HD, 1>(dv, w1, cur + TL::BYTES, 32 * hq, hf, vis);
-          add_pairs<__bf16, HD, 1>(dk, w2, cur + (SEP ? 2 * TL::BYTES : 0), 32 * hq, hf, vis);
+          add_pairs<__bf16, __bf16, HD, 1>(dv, w1, cur + TL::BYTES, 32 * hq, hf, vis);
+          add_pairs<__bf16, QE, HD, 1>(dk, w2, cur, 32 * hq, hf, vis);
         } else {
           // P and dS rounded to bf16 before the gradient products, so that the
           // fp32 score registers are free while those run
           const bf16x8_v pf[2] = {pack8<__bf16>(sv, 0), pack8<__bf16>(sv, 8)};
           const bf16x8_v sf[2] = {pack8<__bf16>(dp, 0), pack8<__bf16>(dp, 8)};
           __builtin_amdgcn_sched_barrier(0);
-          // dO^T and Q^T fragments: transposing reads of the dO and bf16 Q rows in P's
-          // query order
-          uint32_t cl = TL::cols_lane(lane);
-          asm volatile("" : "+v"(cl));  // recomputed each block, not held across the loop
-          const uint32_t ac = (uint32_t)(uintptr_t)cur + cl + 512 * hq;
-          const uint32_t aq = ac + (SEP ? 2 * TL::BYTES : 0), ao = ac + TL::BYTES;
-          bf16x8_v fo[2], fq[2];
+          // dO^T and Q^T fragments: transposing reads of the dO and Q rows in P's query order
+          const uint32_t aq = (uint32_t)(uintptr_t)cur + TL::cols_lane(lane_again<HD>(lane)) + 512 * hq, ao = aq + TL::BYTES;
+          bf16x8_v fo[2];
+          uint4 fq[2];
           fo[0] = frag_cols_x<bf16x8_v>(ao, 0, 0);
-          fq[0] = frag_cols_x<bf16x8_v>(aq, 0, 0);
+          fq[0] = frag_cols_x<uint4>(aq, 0, 0);
 #pragma unroll
           for (int n = 0; n < 2 * NI; ++n) {
             const int t = n / NI, i = n % NI;
             if (n + 1 < 2 * NI) {
               const int i1 = (n + 1) % NI, k1 = 16 * ((n + 1) / NI);
               fo[(n + 1) & 1] = frag_cols_x<bf16x8_v>(ao, i1, k1);
-              fq[(n + 1) & 1] = frag_cols_x<bf16x8_v>(aq, i1, k1);
+              fq[(n + 1) & 1] = frag_cols_x<uint4>(aq, i1, k1);
             }
             __builtin_amdgcn_sched_barrier(0);
             dv[i] = mfma(fo[n & 1], pf[t], dv[i]);
-            dk[i] = mfma(fq[n & 1], sf[t], dk[i]);
+            dk[i] = mfma(to_bf16x8<QE>(fq[n & 1]), sf[t], dk[i]);
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -810,7 +867,7 @@ __global__ __launch_bounds__(512, 2) void window_dkdv_kernel(WinP p) {
   };
   pass(std::false_type{});
   if (__syncthreads_or(not_finite(dk) || not_finite(dv))) pass(std::true_type{});
-  // waves 4-7 hand their sums to waves 0-3 (the stages are free now)
+  // the upper waves hand their sums to the lower ones (the stages are free now)
   typedef __attribute__((address_space(3))) float lds_f;
   lds_f *const red = reinterpret_cast<lds_f *>(L) + pw * (HD * 64) + lane;
   if (hq == 1) {
@@ -875,7 +932,7 @@ __global__ __launch_bounds__(2 * HD) void window_join_kernel(WinP p) {
   const Sequences sq(p.off, p.S, p.T, p.B, threadIdx.x & 63);
   if (!sq.of_wave(r, threadIdx.x & 63, b, s, e) || s >= r || s / p.chunk != c0) return;
   const int key = s + sink;
-  const int lim = limit(p, s, key / KV_ROWS);
+  const int lim = limit(p, s, key / KROWS);
   if (key >= e || e <= lim) return;
   float sum = 0.0f;
   for (int part = 0; part < p.parts; ++part) {
@@ -967,26 +1024,16 @@ WinP params(const lc_window_attn_args &a, bool bwd) {
   char *const sc = static_cast<char *>(a.scratch);
   p.D = reinterpret_cast<float *>(sc + w.D);
   p.nl2 = reinterpret_cast<float *>(sc + w.nl2);
-  if (a.dtype == LC_FP16) {
-    p.qb = p.qb_w = reinterpret_cast<__bf16 *>(sc + w.qb);
-    p.kb = p.kb_w = reinterpret_cast<__bf16 *>(sc + w.kb);
-    p.vb = p.vb_w = reinterpret_cast<__bf16 *>(sc + w.vb);
-    p.ld_qb = (int64_t)p.H * a.hd;
-    p.ld_kb = p.ld_vb = (int64_t)p.Hkv * a.hd;
-  } else {
-    p.qb = static_cast<const __bf16 *>(a.q);
-    p.kb = static_cast<const __bf16 *>(a.k);
-    p.vb = static_cast<const __bf16 *>(a.v);
-    p.ld_qb = a.ld_q; p.ld_kb = a.ld_k; p.ld_vb = a.ld_v;
-  }
+  p.inv = reinterpret_cast<float *>(sc + w.inv);
   p.share = reinterpret_cast<float *>(sc + w.share);
   p.slots = reinterpret_cast<float *>(sc + w.slots);
   p.parts = w.parts;
   p.GP = p.G / w.parts;
   p.chunk = w.chunk;
   p.chunks = w.chunks;
-  p.nkb = (p.n_sink + KV_ROWS - 2) / KV_ROWS + 1;
-  p.nmain = (p.T + KV_ROWS - 1) / KV_ROWS * p.Hkv * p.parts;
+  p.period = p.window <= 2048 ? (p.window + KROWS - 1 + KB - 1) / KB : 0;
+  p.nkb = (p.n_sink + KROWS - 2) / KROWS + 1;
+  p.nmain = (p.T + KROWS - 1) / KROWS * p.Hkv * p.parts;
   p.nsplit = (p.chunks - 1) * p.Hkv * p.parts * p.nkb;
   return p;
 }
@@ -1017,8 +1064,7 @@ lc_status fwd(const lc_window_attn_args &a, hipStream_t s) {
 
 template <typename QE, int HD>
 lc_status bwd(const lc_window_attn_args &a, hipStream_t s) {
-  constexpr bool SEP = !std::is_same<QE, __bf16>::value;
-  constexpr int NW = SEP && HD == 128 ? 8 : 4;  // (three tiles of 128: one workgroup per compute unit)
+  constexpr int NW = 4;
   WinP p = params(a, true);
   unsigned grid = 0;
   LC_TRY(row_grid<NW>(p, grid));
@@ -1027,13 +1073,9 @@ lc_status bwd(const lc_window_attn_args &a, hipStream_t s) {
   const int width = p.Hkv * HD;
   const size_t chunks = 2 * (size_t)p.T * width / 8;
   if (chunks / 256 >= 1u << 24) return fail(LC_ERR_UNSUPPORTED, "window attention: k and v of 2^34 or more elements");
-  if (SEP) {
-    hipLaunchKernelGGL(window_copy_kernel, dim3(ceil_div(chunks, 256)), dim3(256), 0, s, p, width);
-    LC_TRY(check_launch("window_copy_kernel"));
-  }
   hipLaunchKernelGGL((window_dq_kernel<QE, HD, NW>), dim3(grid), dim3(64 * NW), 0, s, p);
   LC_TRY(check_launch("window_dq_kernel"));
-  hipLaunchKernelGGL((window_dkdv_kernel<QE, HD>), dim3((unsigned)n), dim3(512), 0, s, p);
+  hipLaunchKernelGGL((window_dkdv_kernel<QE, HD>), dim3((unsigned)n), dim3(256), 0, s, p);
   LC_TRY(check_launch("window_dkdv_kernel"));
   if (p.parts > 1) {
     hipLaunchKernelGGL(window_sum_kernel, dim3(ceil_div(chunks, 256)), dim3(256), 0, s, p, width);
@@ -1075,16 +1117,12 @@ WindowPlan window_plan(int dtype, int64_t T, int H, int Hkv, int hd, int window,
   };
   w.parts = w.chunks = 1;
   w.D = take(T * H * 4);
-  w.nl2 = w.kb = w.vb = w.qb = w.share = w.slots = 0;
+  w.nl2 = w.inv = w.share = w.slots = 0;
   if (dtype != LC_FP32) {
     w.nl2 = take(T * H * 4);
-    if (dtype == LC_FP16) {
-      w.kb = take(T * Hkv * hd * 2);
-      w.vb = take(T * Hkv * hd * 2);
-      w.qb = take(T * H * hd * 2);
-    }
+    if (dtype == LC_FP16) w.inv = take(T * H * 4);
     const int G = H / Hkv;
-    const int64_t tasks = (T + KV_ROWS - 1) / KV_ROWS * Hkv;
+    const int64_t tasks = (T + KROWS - 1) / KROWS * Hkv;
     for (int n = 1; n <= G; ++n)
       if (G % n == 0) {
         w.parts = n;
@@ -1092,7 +1130,7 @@ WindowPlan window_plan(int dtype, int64_t T, int H, int Hkv, int hd, int window,
       }
     if (w.parts > 1) w.share = take(2 * w.parts * T * Hkv * hd * 4);
     int64_t chunk = 1024;
-    while (chunk < (int64_t)window + KV_ROWS) chunk *= 2;
+    while (chunk < (int64_t)window + KROWS) chunk *= 2;
     if (n_sink > 0 && n_sink <= MAXSINK && chunk < T) {
       w.chunk = (int)chunk;
       w.chunks = (int)((T + chunk - 1) / chunk);
