@@ -14,7 +14,7 @@ struct WindowPlan {
   int64_t share;           // fp32 dk, then dv [parts, T, Hkv hd]
   int64_t slots;           // fp32 sums of sinks: [2, chunks, Hkv, parts, n_sink, 2, hd]
   int64_t total;
-  int parts;               // workgroups that share a key block's query heads
+  int krows, parts;        // keys per dK/dV workgroup; workgroups that share their query heads
   int chunk, chunks;       // query rows of a chunk; chunks of T (1: sinks are not split)
 };
 WindowPlan window_plan(int dtype, int64_t T, int H, int Hkv, int hd, int window, int n_sink);

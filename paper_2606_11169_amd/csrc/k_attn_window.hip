@@ -40,8 +40,6 @@ namespace lc {
 namespace {
 
 constexpr int KB = 64;         // keys (or queries) per inner block
-constexpr int NP = 2;          // dK/dV: pairs of waves of a workgroup
-constexpr int KROWS = 32 * NP; // and the keys that they own
 constexpr int MAXSINK = 256;   // sinks whose dK/dV work is split over chunks of queries
 
 // ---------------------------------------------------------------- row tiles
@@ -117,7 +115,7 @@ struct WinP {
   int64_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
   int T, B, S, H, Hkv, G, window, n_sink;
   int gh, nq;                  // forward, dQ: heads per workgroup, blocks of query rows
-  int GP, parts, period;       // dK/dV: query heads per workgroup, blocks of a window (see the walk; 0: none)
+  int krows, GP, parts, period;       // dK/dV: keys, query heads per workgroup, blocks of a window (see the walk; 0: none)
   int chunk, chunks;
   int nmain, nsplit, nkb;      // dK/dV workgroups; 128-key blocks that hold a sequence's sinks
   float scale;
@@ -186,7 +184,7 @@ __device__ __forceinline__ void add_pairs(f32x16_v (&acc)[HD / 32], const f32x16
 }
 
 // ---------------------------------------------------------------- query blocks
-// A workgroup of NW waves of 32 queries: gh heads of one key/value head x 32 NW / gh rows
+// A workgroup's (group's) QW waves of 32 queries: gh heads of one key/value head x 32 QW / gh rows
 // (wave w: head w % gh, rows 32 (w / gh) ..). What its rows see:
 struct Rows {
   int row, start, wlo, nwin, ns;  // this lane's query (nwin = 0: of no sequence)
@@ -207,9 +205,9 @@ struct Rows {
 };
 
 // false: no row of the workgroup belongs to a sequence
-template <int NW>
+template <int QW>
 __device__ __forceinline__ bool rows_of(const WinP &p, int qb, int w, int lane, Rows &R) {
-  const int qrows = 32 * NW / p.gh;
+  const int qrows = 32 * QW / p.gh;
   const Sequences sq(p.off, p.S, p.T, p.B, lane);
   const int g0 = qb * qrows, r0 = max(g0, sq.first), r1 = min(g0 + qrows, sq.last) - 1;
   int b0, s0, e0;
@@ -239,11 +237,12 @@ __device__ __forceinline__ bool rows_of(const WinP &p, int qb, int w, int lane, 
   return true;
 }
 
-// The workgroup's block of rows and first head, neighbouring blocks of a head next to each other
+// The workgroup's block of rows and first head, neighbouring blocks of a head next to each other, the last
+// ones (under a window longer than the sequences the heaviest) first
 __device__ __forceinline__ bool place(const WinP &p, int w, int &qb, int &h) {
   const int t = xcd_task((int)blockIdx.x, p.nq * (p.H / p.gh));
   if (t < 0) return false;
-  qb = t % p.nq;
+  qb = p.nq - 1 - t % p.nq;
   h = t / p.nq * p.gh + w % p.gh;
   return true;
 }
@@ -279,32 +278,53 @@ __device__ __forceinline__ void store_f32(float *row, const f32x16_v (&acc)[HD /
 }
 
 // ---------------------------------------------------------------- forward
-template <typename QE, int HD, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void window_fwd_kernel(WinP p) {
+// KG groups of QW waves own the same 32 QW queries (or 32 QW / gh of gh heads) and take the key blocks in
+// turn, each with a ring of its own; their sums are joined at the end in group order, scaled to the
+// common maximum. See row_shape for which.
+template <int HD, int KG> constexpr int ring_stages() { return KG * 4 * Tile<HD>::BYTES <= 140 * 1024 ? 2 : 1; }
+
+// A group's loads of K and V blocks: QW waves bring 2 NR / QW runs each
+template <int HD, int QW>
+__device__ __forceinline__ void load_kv(const WinP &p, int kvh, int kb, lds_t *st, int qw, int lane) {
+  typedef Tile<HD> TL;
+  constexpr int RPW = 2 * TL::NR / QW;
+#pragma unroll
+  for (int half = 0; half < (QW == 1 ? 2 : 1); ++half) {
+    const int first = QW == 1 ? half * TL::NR : RPW * qw;
+    const bool isK = QW == 1 ? half == 0 : qw < QW / 2;
+    const int64_t ld = isK ? p.ld_k : p.ld_v;
+    const uint32_t vo = (uint32_t)((TL::lane_row(lane) * ld + 8 * TL::lane_chunk(lane)) * 2);
+    const uint32_t rowb = (uint32_t)(ld * 2);
+    const i32x4_v rs = block_rsrc<HD>(isK ? p.k : p.v, ld, kvh * HD, kb * KB, p.T);
+#pragma unroll
+    for (int t = 0; t < (QW == 1 ? TL::NR : RPW); ++t)
+      dma16(rs, st + (first + t) * RUNB, vo + rowb * (uint32_t)TL::run_row((first + t) % TL::NR));
+  }
+}
+
+template <typename QE, int HD, int QW, int KG>
+__global__ __launch_bounds__(64 * QW * KG, 2) void window_fwd_kernel(WinP p) {
   typedef typename V8<QE>::type QV;
   typedef Tile<HD> TL;
-  constexpr int NES = HD / 16, NI = HD / 32, RPW = 2 * TL::NR / NW;
-  __shared__ __align__(16) char smem[2 * 2 * TL::BYTES];  // stage s: K tile | V tile
-  lds_t *const L = LDS_AS(char, smem);
+  constexpr int NES = HD / 16, NI = HD / 32, ST = ring_stages<HD, KG>();
+  __shared__ __align__(16) char smem[KG * ST * 2 * TL::BYTES];  // per group, stage s: K tile | V tile
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6), w = w8 % QW, kg = w8 / QW;
+  lds_t *const L = LDS_AS(char, smem) + kg * ST * 2 * TL::BYTES;
   int qb, h;
   if (!place(p, w, qb, h)) return;
   Rows R;
-  if (!rows_of<NW>(p, qb, w, lane, R)) return;
+  if (!rows_of<QW>(p, qb, w, lane, R)) return;
   const int kvh = h / p.G;
   const float sc = p.scale * LOG2E;
-  // half of the waves stream K, the other half V, RPW runs each
-  const bool isK = w < NW / 2;
-  const int run0 = RPW * (w % (NW / 2));
-  const int64_t ld = isK ? p.ld_k : p.ld_v;
-  const uint32_t vo = (uint32_t)((TL::lane_row(lane) * ld + 8 * TL::lane_chunk(lane)) * 2);
-  const uint32_t rowb = (uint32_t)(ld * 2);
-  auto load = [&](int kb, lds_t *st) {
-    const i32x4_v rs = block_rsrc<HD>(isK ? p.k : p.v, ld, kvh * HD, kb * KB, p.T);
-#pragma unroll
-    for (int t = 0; t < RPW; ++t)
-      dma16(rs, st + (isK ? 0 : TL::BYTES) + (run0 + t) * RUNB, vo + rowb * (uint32_t)TL::run_row(run0 + t));
+  auto load = [&](int it, lds_t *st) { load_kv<HD, QW>(p, kvh, R.block(it), st, w, lane); };
+  auto next_stage = [&](int it) {  // after the block of step `it`
+    if (ST == 1) {
+      __syncthreads();
+      if (it + KG < R.nit) load(it + KG, L);
+    }
+    wait_vm0();
+    __syncthreads();
   };
   f32x16_v o[NI];
   float m, l;
@@ -316,14 +336,14 @@ __global__ __launch_bounds__(64 * NW, 2) void window_fwd_kernel(WinP p) {
     for (int i = 0; i < NI; ++i) o[i] = zero16();
     m = -INFINITY;
     l = 0.0f;
-    if (R.nit > 0) load(R.block(0), L);
+    if (kg < R.nit) load(kg, L);
     wait_vm0();
     __syncthreads();
-    for (int it = 0; it < R.nit; ++it) {
-      const lds_t *cur = L + (it & 1) * 2 * TL::BYTES;
-      if (it + 1 < R.nit) load(R.block(it + 1), L + ((it + 1) & 1) * 2 * TL::BYTES);
+    for (int it = kg, i0 = 0; i0 < R.nit; it += KG, i0 += KG) {  // (as many steps in every group)
+      const lds_t *cur = L + (ST == 2 ? (i0 / KG & 1) * 2 * TL::BYTES : 0);
+      if (ST == 2 && it + KG < R.nit) load(it + KG, L + ((i0 / KG + 1) & 1) * 2 * TL::BYTES);
       const int k0 = R.block(it) * KB;
-      if (R.any(k0, p.n_sink)) {
+      if (it < R.nit && R.any(k0, p.n_sink)) {
         f32x16_v s[2] = {zero16(), zero16()};
         // K fragments are read one k-step ahead of the products that use them
         const lds_t *krow = cur + TL::rows_lane(lane);
@@ -413,12 +433,41 @@ __global__ __launch_bounds__(64 * NW, 2) void window_fwd_kernel(WinP p) {
           }
         }
       }
-      wait_vm0();
-      __syncthreads();
+      next_stage(it);
     }
   };
   pass(std::false_type{});
   if (__syncthreads_or(not_finite(o))) pass(std::true_type{});
+  if constexpr (KG > 1) {
+    // (a group that saw no key of a row has m = -inf: weight 0)
+    typedef __attribute__((address_space(3))) float lds_f;
+    constexpr int N = HD / 2 + 2;
+    lds_f *const red = reinterpret_cast<lds_f *>(LDS_AS(char, smem)) + w * (N * 64) + lane;
+    constexpr int STEP = QW * N * 64;  // to the next group's
+    if (kg > 0) {
+      lds_f *const to = red + (kg - 1) * STEP;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[(i * 16 + r) * 64] = o[i][r];
+      to[(N - 2) * 64] = m;
+      to[(N - 1) * 64] = l;
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int x = 0; x < KG - 1; ++x) {
+      const lds_f *const from = red + x * STEP;
+      const float m1 = from[(N - 2) * 64], mt = fmaxf(m, m1), mu = mt == -INFINITY ? 0.0f : mt;
+      const float a0 = ex2(m - mu), a1 = ex2(m1 - mu);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = o[i][r] * a0 + from[(i * 16 + r) * 64] * a1;
+      l = l * a0 + from[(N - 1) * 64] * a1;
+      m = mt;
+    }
+  }
   if (R.nwin == 0) return;
   const float lt = sum_with_partner(l);
   store_bf16<HD>(p.o + (int64_t)R.row * p.ld_o + (int64_t)h * HD, o, 1.0f / lt, hf);
@@ -435,34 +484,32 @@ __device__ __forceinline__ float row_scale(float x) {
 
 // dQ, and what dK/dV needs of every query: D, -lse log2(e) and, for fp16 inputs, the inverse of its dO
 // row's scale. LDS stage = K | V.
-template <typename QE, int HD, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
+// QW, KG as in the forward.
+template <typename QE, int HD, int QW, int KG>
+__global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
   typedef typename V8<QE>::type QV;
   typedef Tile<HD> TL;
   constexpr bool F16 = !std::is_same<QE, __bf16>::value;
-  constexpr int NES = HD / 16, NI = HD / 32, RPW = 2 * TL::NR / NW;
-  __shared__ __align__(16) char smem[2 * 2 * TL::BYTES];
-  lds_t *const L = LDS_AS(char, smem);
+  constexpr int NES = HD / 16, NI = HD / 32, ST = ring_stages<HD, KG>();
+  __shared__ __align__(16) char smem[KG * ST * 2 * TL::BYTES];
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6), w = w8 % QW, kg = w8 / QW;
+  lds_t *const L = LDS_AS(char, smem) + kg * ST * 2 * TL::BYTES;
   int qb, h;
   if (!place(p, w, qb, h)) return;
   Rows R;
-  if (!rows_of<NW>(p, qb, w, lane, R)) return;
+  if (!rows_of<QW>(p, qb, w, lane, R)) return;
   const int kvh = h / p.G;
   const float sc = p.scale * LOG2E;
   const bool ok = R.nwin > 0;
-  // half of the waves stream K, the other half V, RPW runs each
-  const bool isK = w < NW / 2;
-  const int run0 = RPW * (w % (NW / 2));
-  const int64_t ld = isK ? p.ld_k : p.ld_v;
-  const uint32_t vo = (uint32_t)((TL::lane_row(lane) * ld + 8 * TL::lane_chunk(lane)) * 2);
-  const uint32_t rowb = (uint32_t)(ld * 2);
-  auto load = [&](int kb, lds_t *st) {
-    const i32x4_v rs = block_rsrc<HD>(isK ? p.k : p.v, ld, kvh * HD, kb * KB, p.T);
-#pragma unroll
-    for (int t = 0; t < RPW; ++t)
-      dma16(rs, st + (isK ? 0 : TL::BYTES) + (run0 + t) * RUNB, vo + rowb * (uint32_t)TL::run_row(run0 + t));
+  auto load = [&](int it, lds_t *st) { load_kv<HD, QW>(p, kvh, R.block(it), st, w, lane); };
+  auto next_stage = [&](int it) {  // after the block of step `it`
+    if (ST == 1) {
+      __syncthreads();
+      if (it + KG < R.nit) load(it + KG, L);
+    }
+    wait_vm0();
+    __syncthreads();
   };
   const int64_t si = (int64_t)h * p.T + min(R.row, p.T - 1);
   const float lse2 = ok ? p.lse[si] * LOG2E : 0.0f;
@@ -470,7 +517,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
   f32x16_v acc[NI];
   auto pass = [&](auto pairs_) {
     constexpr bool pairs = decltype(pairs_)::value;
-    if (R.nit > 0) load(R.block(0), L);
+    if (kg < R.nit) load(kg, L);
     QV qf[NES], df[NES];
     load_row<QV, HD>(qf, static_cast<const QE *>(p.q) + (int64_t)h * HD, p.ld_q, R.row, p.T, hf);
     bf16x8_v d16[NES];
@@ -504,7 +551,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
 #pragma unroll
       for (int es = 0; es < NES; ++es) df[es] = __builtin_bit_cast(QV, d16[es]);
     }
-    if (!pairs && ok && hf == 0) {
+    if (!pairs && ok && hf == 0 && kg == 0) {
       p.D[si] = Dq;
       p.nl2[si] = -lse2;
       if (F16) p.inv[si] = 1.0f / scale;
@@ -513,11 +560,11 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
     for (int i = 0; i < NI; ++i) acc[i] = zero16();
     wait_vm0();
     __syncthreads();
-    for (int it = 0; it < R.nit; ++it) {
-      const lds_t *cur = L + (it & 1) * 2 * TL::BYTES;
-      if (it + 1 < R.nit) load(R.block(it + 1), L + ((it + 1) & 1) * 2 * TL::BYTES);
+    for (int it = kg, i0 = 0; i0 < R.nit; it += KG, i0 += KG) {  // (as many steps in every group)
+      const lds_t *cur = L + (ST == 2 ? (i0 / KG & 1) * 2 * TL::BYTES : 0);
+      if (ST == 2 && it + KG < R.nit) load(it + KG, L + ((i0 / KG + 1) & 1) * 2 * TL::BYTES);
       const int k0 = R.block(it) * KB;
-      if (R.any(k0, p.n_sink)) {
+      if (it < R.nit && R.any(k0, p.n_sink)) {
         f32x16_v s[2] = {zero16(), zero16()}, dp[2] = {zero16(), zero16()};
         // K fragments are read one k-step ahead of their products, V fragments
         // two products ahead of theirs
@@ -573,12 +620,30 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
           }
         }
       }
-      wait_vm0();
-      __syncthreads();
+      next_stage(it);
     }
   };
   pass(std::false_type{});
   if (__syncthreads_or(not_finite(acc))) pass(std::true_type{});
+  if constexpr (KG > 1) {
+    typedef __attribute__((address_space(3))) float lds_f;
+    lds_f *const red = reinterpret_cast<lds_f *>(LDS_AS(char, smem)) + w * (HD / 2 * 64) + lane;
+    constexpr int STEP = QW * (HD / 2) * 64;  // to the next group's
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) red[(kg - 1) * STEP + (i * 16 + r) * 64] = acc[i][r];
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int x = 0; x < KG - 1; ++x)
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][r] += red[x * STEP + (i * 16 + r) * 64];
+  }
   if (ok) store_bf16<HD>(p.dq + (int64_t)R.row * p.ld_dq + (int64_t)h * HD, acc, p.scale / scale, hf);
 }
 
@@ -586,7 +651,9 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
 // visits, for GP of the head's query heads, the query blocks that see them. Waves w and
 // w + NP own the same 32 keys (K and V fragments in registers) and take the first and second 32
 // queries of every 64-query block; at the end wave w + NP hands its sums to wave w, which
-// adds them. LDS stage = Q | dO | -lse log2(e) | D | (fp16: the scales' inverses) of one block.
+// adds them. QG groups of such waves own the same keys and take the (head, query block) units in
+// turn, each with a ring of its own (QG = 2: key_rows). LDS stage = Q | dO | -lse log2(e) | D |
+// (fp16: the scales' inverses) of one block.
 //
 // Sinks are seen by their whole sequence, so the workgroup that owns them would visit all
 // of its queries, however long, while every other visits a window's. Where a sequence
@@ -599,7 +666,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_dq_kernel(WinP p) {
 // With few keys (p.parts > 1) several workgroups share a key block's query heads and write
 // fp32 shares, which window_sum_kernel adds in head order.
 __device__ __forceinline__ int limit(const WinP &p, int s, int kblk) {
-  return max((kblk + 1) * KROWS - 1 + p.window, (s / p.chunk + 1) * p.chunk);
+  return max((kblk + 1) * p.krows - 1 + p.window, (s / p.chunk + 1) * p.chunk);
 }
 // a slot of [dk | dv], 2 HD floats: set 0 the owner's sums (by the chunk that the sequence
 // starts in), set 1 a chunk's
@@ -629,24 +696,24 @@ __device__ __forceinline__ f16x8_v scaled_row(bf16x8_v x, uint32_t c) {
 template <typename QE, int HD> constexpr int dkdv_stage() {
   return 2 * Tile<HD>::BYTES + (std::is_same<QE, __bf16>::value ? 512 : 768);
 }
-template <typename QE, int HD> constexpr int dkdv_smem() {
-  constexpr int handoff = NP * HD * 64 * 4;
-  return 2 * dkdv_stage<QE, HD>() > handoff ? 2 * dkdv_stage<QE, HD>() : handoff;
+template <typename QE, int HD, int NP, int QG> constexpr int dkdv_smem() {
+  constexpr int handoff = QG * NP * HD * 64 * 4, stages = QG * 2 * dkdv_stage<QE, HD>();
+  return stages > handoff ? stages : handoff;
 }
 
-template <typename QE, int HD>
-__global__ __launch_bounds__(128 * NP, 2) void window_dkdv_kernel(WinP p) {
+template <typename QE, int HD, int NP, int QG>
+__global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
   typedef typename V8<QE>::type QV;
   typedef Tile<HD> TL;
   constexpr bool F16 = !std::is_same<QE, __bf16>::value;
   constexpr int NES = HD / 16, NI = HD / 32;
-  constexpr int RPW = TL::NR / NP;  // tile runs per wave
+  constexpr int KROWS = 32 * NP, RPW = TL::NR / NP;  // keys; tile runs per wave
   constexpr int STAGE = dkdv_stage<QE, HD>();
-  __shared__ __align__(256) char smem[dkdv_smem<QE, HD>()];
+  __shared__ __align__(256) char smem[dkdv_smem<QE, HD, NP, QG>()];
   __shared__ int keys[2][KROWS];  // lo and cnt (below) of every key
-  lds_t *const L = LDS_AS(char, smem);
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6), w = w8 % (2 * NP), kg = w8 / (2 * NP);
+  lds_t *const L = LDS_AS(char, smem) + kg * 2 * STAGE;
   const int pw = w % NP, hq = w / NP;  // key block of the pair, query half
   const bool splits = p.chunks > 1;
 
@@ -712,7 +779,7 @@ __global__ __launch_bounds__(128 * NP, 2) void window_dkdv_kernel(WinP p) {
   const int lo_min = wave_min32(cnt ? lo : NONE), lo_max = wave_max32(cnt ? lo : NONE);
   const int hi_max = wave_max32(cnt ? lo + cnt : -1), hi_min = wave_min32(lo + cnt);
   const int64_t krow = min(key, p.T - 1);
-  if (hq == 0 && hf == 0) {
+  if (w8 == pw && hf == 0) {
     keys[0][pw * 32 + l32] = lo;
     keys[1][pw * 32 + l32] = cnt;
   }
@@ -753,7 +820,14 @@ __global__ __launch_bounds__(128 * NP, 2) void window_dkdv_kernel(WinP p) {
   f32x16_v dk[NI], dv[NI];
   auto pass = [&](auto pairs_) {
     constexpr bool pairs = decltype(pairs_)::value;
-    if (nit > 0) load(0, qfirst + turn, L);
+    // head and block of this group's unit; the walk's next one
+    int g = 0, qi = turn;
+    auto next = [&](int &gn, int &qn) {
+      qn = qn + 1 < nqb ? qn + 1 : 0;
+      if (qn == turn) ++gn;
+    };
+    if (kg == 1) next(g, qi);
+    if (kg < nit) load(g, qfirst + qi, L);
     QV kf[NES], vf[NES];
 #pragma unroll
     for (int es = 0; es < NES; ++es) {
@@ -765,14 +839,14 @@ __global__ __launch_bounds__(128 * NP, 2) void window_dkdv_kernel(WinP p) {
     for (int i = 0; i < NI; ++i) dk[i] = dv[i] = zero16();
     wait_vm0();
     __syncthreads();
-    int g = 0, qi = turn;  // head and block of this iteration
-    for (int it = 0; it < nit; ++it) {
-      const lds_t *cur = L + (it & 1) * STAGE;
-      int gn = g, qn = qi + 1 < nqb ? qi + 1 : 0;
-      if (qn == turn) ++gn;
-      if (it + 1 < nit) load(gn, qfirst + qn, L + ((it + 1) & 1) * STAGE);
+    for (int it = kg, i0 = 0; i0 < nit; it += QG, i0 += QG) {  // (as many steps in every group)
+      const lds_t *cur = L + (i0 / QG & 1) * STAGE;
+      int gn = g, qn = qi;
+#pragma unroll
+      for (int u = 0; u < QG; ++u) next(gn, qn);
+      if (it + QG < nit) load(gn, qfirst + qn, L + ((i0 / QG + 1) & 1) * STAGE);
       const int q0 = (qfirst + qi) * KB + 32 * hq;  // this wave's 32 queries
-      if (q0 + 31 >= lo_min && q0 < hi_max) {
+      if (it < nit && q0 + 31 >= lo_min && q0 < hi_max) {
         f32x16_v sv = zero16(), dp = zero16();
         // fragment rows of this wave's 32 queries: a per-lane base plus immediates
         const int ln = lane_again<HD>(lane), lh = ln >> 5;
@@ -867,10 +941,34 @@ __global__ __launch_bounds__(128 * NP, 2) void window_dkdv_kernel(WinP p) {
   };
   pass(std::false_type{});
   if (__syncthreads_or(not_finite(dk) || not_finite(dv))) pass(std::true_type{});
-  // the upper waves hand their sums to the lower ones (the stages are free now)
+  // the second group hands its sums to the first, then the upper waves theirs to the lower ones (the
+  // stages are free now)
   typedef __attribute__((address_space(3))) float lds_f;
-  lds_f *const red = reinterpret_cast<lds_f *>(L) + pw * (HD * 64) + lane;
-  if (hq == 1) {
+  if constexpr (QG > 1) {
+    lds_f *const red = reinterpret_cast<lds_f *>(LDS_AS(char, smem)) + w * (HD * 64) + lane;
+    if (kg == 1) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          red[(i * 16 + r) * 64] = dk[i][r];
+          red[(HD / 2 + i * 16 + r) * 64] = dv[i][r];
+        }
+    }
+    __syncthreads();
+    if (kg == 0) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dk[i][r] += red[(i * 16 + r) * 64];
+          dv[i][r] += red[(HD / 2 + i * 16 + r) * 64];
+        }
+    }
+    __syncthreads();
+  }
+  lds_f *const red = reinterpret_cast<lds_f *>(LDS_AS(char, smem)) + pw * (HD * 64) + lane;
+  if (hq == 1 && kg == 0) {
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -880,7 +978,7 @@ __global__ __launch_bounds__(128 * NP, 2) void window_dkdv_kernel(WinP p) {
       }
   }
   __syncthreads();
-  if (hq == 1 || cnt == 0) return;
+  if (hq == 1 || kg == 1 || cnt == 0) return;
 #pragma unroll
   for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -932,7 +1030,7 @@ __global__ __launch_bounds__(2 * HD) void window_join_kernel(WinP p) {
   const Sequences sq(p.off, p.S, p.T, p.B, threadIdx.x & 63);
   if (!sq.of_wave(r, threadIdx.x & 63, b, s, e) || s >= r || s / p.chunk != c0) return;
   const int key = s + sink;
-  const int lim = limit(p, s, key / KROWS);
+  const int lim = limit(p, s, key / p.krows);
   if (key >= e || e <= lim) return;
   float sum = 0.0f;
   for (int part = 0; part < p.parts; ++part) {
@@ -950,6 +1048,11 @@ __global__ __launch_bounds__(2 * HD) void window_join_kernel(WinP p) {
 }
 
 // ---------------------------------------------------------------- host
+// Keys per dK/dV workgroup: 64, or 32 and two groups of waves where that leaves a compute unit to
+// every two workgroups of 64 (1024 tokens in 4 sequences, 8 heads, window 256: 21 -> 16 us; one
+// sequence of 1500, 4 heads, causal: 38 -> 27. With 160 of them, 300 tokens x 32 heads: 16 -> 21)
+int key_rows(int64_t T, int H) { return (T + 63) / 64 * H <= 128 ? 32 : 64; }
+
 int kv_of(const lc_window_attn_args &a) { return a.Hkv ? a.Hkv : a.H; }
 
 lc_status check(const lc_window_attn_args &a, bool bwd) {
@@ -1031,20 +1134,35 @@ WinP params(const lc_window_attn_args &a, bool bwd) {
   p.GP = p.G / w.parts;
   p.chunk = w.chunk;
   p.chunks = w.chunks;
-  p.period = p.window <= 2048 ? (p.window + KROWS - 1 + KB - 1) / KB : 0;
-  p.nkb = (p.n_sink + KROWS - 2) / KROWS + 1;
-  p.nmain = (p.T + KROWS - 1) / KROWS * p.Hkv * p.parts;
+  p.krows = w.krows;
+  p.period = p.window <= 2048 ? (p.window + p.krows - 1 + KB - 1) / KB : 0;
+  p.nkb = (p.n_sink + p.krows - 2) / p.krows + 1;
+  p.nmain = (p.T + p.krows - 1) / p.krows * p.Hkv * p.parts;
   p.nsplit = (p.chunks - 1) * p.Hkv * p.parts * p.nkb;
   return p;
 }
 
-// forward and dQ grids: gh heads of a group (as many of 1, 2, 4, 8 as divide it, at most one
-// per wave) share a workgroup's keys, so that it spans fewer rows and with them fewer keys
-template <int NW>
-lc_status row_grid(WinP &p, unsigned &grid) {
+// Forward and dQ: 32 QW rows (of one head) per workgroup and KG groups of waves, by the number of
+// workgroups that 128 rows each would make.
+// Up to 64: 32 rows and four groups, so that four times as many compute units share the work and a
+// chain of blocks is a quarter as long (1024 tokens in 4 sequences, 8 heads, window 256: forward 17.0 ->
+// 13.2 us, dQ 21.3 -> 15.4; one sequence of 1500, 4 heads, causal: 41 -> 23 and 51 -> 25). With 96
+// workgroups the chip is full (300 tokens, 32 heads: 12.8 -> 18.5).
+// Up to 256, one per compute unit, and chains of 8 blocks or more: two groups (3000 tokens, 10 heads,
+// window 1000: 33.3 -> 28.6 and 41.2 -> 37.0; with chains of up to 5 blocks 12.8 -> 13.1, 16.1 -> 18.4).
+struct Shape { int QW, KG; };
+Shape row_shape(const WinP &p) {
+  const int64_t n = (p.T + 127ll) / 128 * p.H;
+  if (n <= 64) return {1, 4};
+  return n <= 256 && p.window >= 512 && p.T / p.B >= 512 ? Shape{4, 2} : Shape{4, 1};
+}
+
+// Forward and dQ grids. gh heads of a group (as many of 1, 2, 4 as divide it, at most one per wave) share
+// a workgroup's keys, so that it spans fewer rows and with them fewer keys.
+lc_status row_grid(WinP &p, int QW, unsigned &grid) {
   p.gh = 1;
-  while (2 * p.gh <= NW && p.G % (2 * p.gh) == 0) p.gh *= 2;
-  const int qrows = 32 * NW / p.gh;
+  while (2 * p.gh <= QW && p.G % (2 * p.gh) == 0) p.gh *= 2;
+  const int qrows = 32 * QW / p.gh;
   p.nq = (p.T + qrows - 1) / qrows;
   const int64_t n = (int64_t)p.nq * (p.H / p.gh);
   if (n > 1 << 22) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^22 blocks of rows and heads");
@@ -1054,28 +1172,33 @@ lc_status row_grid(WinP &p, unsigned &grid) {
 
 template <typename QE, int HD>
 lc_status fwd(const lc_window_attn_args &a, hipStream_t s) {
-  constexpr int NW = 4;
   WinP p = params(a, false);
+  const Shape sh = row_shape(p);
   unsigned grid = 0;
-  LC_TRY(row_grid<NW>(p, grid));
-  hipLaunchKernelGGL((window_fwd_kernel<QE, HD, NW>), dim3(grid), dim3(64 * NW), 0, s, p);
+  LC_TRY(row_grid(p, sh.QW, grid));
+  if (sh.QW == 1) hipLaunchKernelGGL((window_fwd_kernel<QE, HD, 1, 4>), dim3(grid), dim3(256), 0, s, p);
+  else if (sh.KG == 2) hipLaunchKernelGGL((window_fwd_kernel<QE, HD, 4, 2>), dim3(grid), dim3(512), 0, s, p);
+  else hipLaunchKernelGGL((window_fwd_kernel<QE, HD, 4, 1>), dim3(grid), dim3(256), 0, s, p);
   return check_launch("window_fwd_kernel");
 }
 
 template <typename QE, int HD>
 lc_status bwd(const lc_window_attn_args &a, hipStream_t s) {
-  constexpr int NW = 4;
   WinP p = params(a, true);
+  const Shape sh = row_shape(p);
   unsigned grid = 0;
-  LC_TRY(row_grid<NW>(p, grid));
+  LC_TRY(row_grid(p, sh.QW, grid));
   const int64_t n = ((int64_t)(p.nsplit + 7) / 8 + ((int64_t)p.nmain + 7) / 8) * 8;
   if (n > 1 << 22) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^22 blocks of keys and heads");
   const int width = p.Hkv * HD;
   const size_t chunks = 2 * (size_t)p.T * width / 8;
   if (chunks / 256 >= 1u << 24) return fail(LC_ERR_UNSUPPORTED, "window attention: k and v of 2^34 or more elements");
-  hipLaunchKernelGGL((window_dq_kernel<QE, HD, NW>), dim3(grid), dim3(64 * NW), 0, s, p);
+  if (sh.QW == 1) hipLaunchKernelGGL((window_dq_kernel<QE, HD, 1, 4>), dim3(grid), dim3(256), 0, s, p);
+  else if (sh.KG == 2) hipLaunchKernelGGL((window_dq_kernel<QE, HD, 4, 2>), dim3(grid), dim3(512), 0, s, p);
+  else hipLaunchKernelGGL((window_dq_kernel<QE, HD, 4, 1>), dim3(grid), dim3(256), 0, s, p);
   LC_TRY(check_launch("window_dq_kernel"));
-  hipLaunchKernelGGL((window_dkdv_kernel<QE, HD>), dim3((unsigned)n), dim3(256), 0, s, p);
+  if (p.krows == 32) hipLaunchKernelGGL((window_dkdv_kernel<QE, HD, 1, 2>), dim3((unsigned)n), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((window_dkdv_kernel<QE, HD, 2, 1>), dim3((unsigned)n), dim3(256), 0, s, p);
   LC_TRY(check_launch("window_dkdv_kernel"));
   if (p.parts > 1) {
     hipLaunchKernelGGL(window_sum_kernel, dim3(ceil_div(chunks, 256)), dim3(256), 0, s, p, width);
@@ -1122,7 +1245,8 @@ WindowPlan window_plan(int dtype, int64_t T, int H, int Hkv, int hd, int window,
     w.nl2 = take(T * H * 4);
     if (dtype == LC_FP16) w.inv = take(T * H * 4);
     const int G = H / Hkv;
-    const int64_t tasks = (T + KROWS - 1) / KROWS * Hkv;
+    w.krows = key_rows(T, H);
+    const int64_t tasks = (T + w.krows - 1) / w.krows * Hkv;
     for (int n = 1; n <= G; ++n)
       if (G % n == 0) {
         w.parts = n;
@@ -1130,7 +1254,7 @@ WindowPlan window_plan(int dtype, int64_t T, int H, int Hkv, int hd, int window,
       }
     if (w.parts > 1) w.share = take(2 * w.parts * T * Hkv * hd * 4);
     int64_t chunk = 1024;
-    while (chunk < (int64_t)window + KROWS) chunk *= 2;
+    while (chunk < (int64_t)window + w.krows) chunk *= 2;
     if (n_sink > 0 && n_sink <= MAXSINK && chunk < T) {
       w.chunk = (int)chunk;
       w.chunks = (int)((T + chunk - 1) / chunk);
