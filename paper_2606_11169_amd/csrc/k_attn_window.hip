@@ -188,13 +188,13 @@ __device__ __forceinline__ void add_pairs(f32x16_v (&acc)[HD / 32], const f32x16
 // (wave w: head w % gh, rows 32 (w / gh) ..). What its rows see:
 struct Rows {
   int row, start, wlo, nwin, ns;  // this lane's query (nwin = 0: of no sequence)
-  int wmin, wmax, smin, rmax, r0; // this wave's: window starts, first start, last row, first row
+  int wmin, wmax, smin, smax, rmax, r0; // this wave's: window starts, sequence starts, last row, first row
   int sb0, nsb, wb0, nit;         // the workgroup's blocks: sink blocks sb0 .., then wb0 ..
   __device__ __forceinline__ int block(int it) const { return it < nsb ? sb0 + it : wb0 + it - nsb; }
   __device__ __forceinline__ bool active() const { return rmax >= 0; }
   // whether the wave sees some key of the block at k0, whether one of them may be a sink before a
   // window, and whether every row sees all of it
-  __device__ __forceinline__ bool sinks(int k0, int n_sink) const { return k0 + KB > smin && k0 - smin < n_sink; }
+  __device__ __forceinline__ bool sinks(int k0, int n_sink) const { return k0 + KB > smin && k0 - smax < n_sink; }
   __device__ __forceinline__ bool any(int k0, int n_sink) const {
     return active() && k0 <= rmax && (k0 + KB > wmin || sinks(k0, n_sink));
   }
@@ -233,6 +233,7 @@ __device__ __forceinline__ bool rows_of(const WinP &p, int qb, int w, int lane, 
   R.wmin = wave_min32(ok ? R.wlo : NONE);
   R.wmax = wave_max32(ok ? R.wlo : NONE);
   R.smin = wave_min32(ok ? R.start : NONE);
+  R.smax = wave_max32(ok ? R.start : -1);
   R.rmax = wave_max32(ok ? R.row : -1);
   return true;
 }
@@ -1136,9 +1137,7 @@ WinP params(const lc_window_attn_args &a, bool bwd) {
   p.chunks = w.chunks;
   p.krows = w.krows;
   p.period = p.window <= 2048 ? (p.window + p.krows - 1 + KB - 1) / KB : 0;
-  p.nkb = (p.n_sink + p.krows - 2) / p.krows + 1;
-  p.nmain = (p.T + p.krows - 1) / p.krows * p.Hkv * p.parts;
-  p.nsplit = (p.chunks - 1) * p.Hkv * p.parts * p.nkb;
+  p.nkb = p.chunks > 1 ? (p.n_sink + p.krows - 2) / p.krows + 1 : 0;
   return p;
 }
 
@@ -1188,7 +1187,11 @@ lc_status bwd(const lc_window_attn_args &a, hipStream_t s) {
   const Shape sh = row_shape(p);
   unsigned grid = 0;
   LC_TRY(row_grid(p, sh.QW, grid));
-  const int64_t n = ((int64_t)(p.nsplit + 7) / 8 + ((int64_t)p.nmain + 7) / 8) * 8;
+  const int64_t nmain = ((int64_t)p.T + p.krows - 1) / p.krows * p.Hkv * p.parts;
+  const int64_t nsplit = (int64_t)(p.chunks - 1) * p.Hkv * p.parts * p.nkb;
+  const int64_t n = ((nsplit + 7) / 8 + (nmain + 7) / 8) * 8;
+  p.nmain = (int)nmain;
+  p.nsplit = (int)nsplit;
   if (n > 1 << 22) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^22 blocks of keys and heads");
   const int width = p.Hkv * HD;
   const size_t chunks = 2 * (size_t)p.T * width / 8;

@@ -314,3 +314,78 @@ def test_no_rows():
     banner("window attention T=0")
     lc.lc_window_attention_forward(BF16, BF16, 0, 1, None, 2, 2, 64, 4, 0, None, 128, None, 128, None, 128, None, 128, None)
     torch.cuda.synchronize()
+
+
+# What a call's number of rows and heads chooses: 128 rows per workgroup, its waves over one or two
+# groups of keys, 64 keys per dK/dV workgroup, a group's query heads over some workgroups and sinks
+# over chunks of queries (few rows, as in most tests above: 32 rows, 32 keys, every head of its own)
+WIDE = [([700, 1, 0, 333, 466], 100, 5, 24, 24),    # 128 rows; 64 keys, sinks split
+        ([65, 200, 63, 64, 129, 1200, 31], 64, 70, 24, 24),
+        ([1000, 0, 1000], 300, 4, 32, 8),           # a group's four heads over two workgroups
+        ([900, 511, 589], 1500, 0, 32, 8),
+        ([1500, 1501], 600, 3, 10, 5),              # two groups of keys
+        ([2999], 5000, 0, 10, 2),
+        ([2500, 100], 513, 1000, 12, 12),
+        ([1, 1, 3, 2, 200, 77, 1800], 33, 2, 32, 16)]
+SOME = [WIDE[0], WIDE[4], WIDE[2]]
+
+
+@pytest.mark.parametrize("dt,hd", [(BF16, 128), (BF16, 64), (F16, 128), (F16, 64), (F32, 40)])
+@pytest.mark.parametrize("lens,W,S,H,Hkv", WIDE, ids=[f"{'_'.join(map(str, a[0]))}w{a[1]}s{a[2]}h{a[3]}" for a in WIDE])
+def test_many_heads(lens, W, S, H, Hkv, dt, hd):
+    banner(f"window attention wide {lens} W={W} S={S} {dt} {H}/{Hkv} x {hd}")
+    m = make(lens, H, Hkv, hd, dt, seed=W, first=3, tail=70)
+    a = run(m, W, S)
+    verify(m, W, S, a)
+    assert all(torch.equal(x, y) for x, y in zip(a, run(m, W, S)))
+
+
+@pytest.mark.parametrize("dt,hd", [(BF16, 128), (BF16, 64), (F16, 128)])
+@pytest.mark.parametrize("lens,W,S,H,Hkv", SOME, ids=[f"w{a[1]}s{a[2]}h{a[3]}" for a in SOME])
+def test_many_heads_masked_places(lens, W, S, H, Hkv, dt, hd):
+    banner(f"window attention wide masked places {lens} W={W} S={S} {dt} {H}/{Hkv} x {hd}")
+    at = lens[0] // 2
+    for what, bad in (("k", math.inf), ("v", math.nan), ("q", math.nan), ("dout", -math.inf)):
+        m = make(lens, H, Hkv, hd, dt, tail=30, seed=6)
+        clean = {x: m[x].clone() for x in ("q", "k", "v", "dout")}
+        m[what][at, ::3] = bad
+        for x in ("q", "k", "v", "dout"):
+            m[x][sum(lens):] = bad
+        got = run(m, W, S)
+        m.update(clean)
+        see = seen(lens, 0, m["T"], W, S)
+        rows = ~see[:, at] if what in ("k", "v") else torch.arange(m["T"], device=DEV) != at
+        verify(m, W, S, got, rows=rows, keys=~see[~rows].any(0))
+
+
+MANY = [(64, 40, 16, 2), (100, 30, 7, 3), (63, 35, 9, 1), (1000, 9, 4, 1), (5000, 3, 2, 1), (4097, 1, 1, 0),
+        (129, 60, 200, 4)]
+
+
+@pytest.mark.parametrize("dt,H,Hkv,hd", [(BF16, 4, 2, 64), (F16, 2, 2, 128), (F32, 2, 1, 32), (BF16, 16, 16, 128)])
+@pytest.mark.parametrize("B,most,W,S", MANY)
+def test_many_sequences(B, most, W, S, dt, H, Hkv, hd):
+    """Sequence counts at and past what one load of a wave holds, lengths from 0 to `most`."""
+    banner(f"window attention {B} sequences of up to {most} W={W} S={S} {dt} {H}/{Hkv} x {hd}")
+    g = torch.Generator()
+    g.manual_seed(B)
+    lens = torch.randint(0, most + 1, (B,), generator=g).tolist()
+    lens[-1] = lens[-1] or 1
+    m = make(lens, H, Hkv, hd, dt, seed=B, first=2, tail=5)
+    verify(m, W, S, run(m, W, S))
+
+
+def test_many_long_sequences_with_split_sinks():
+    banner("window attention 70 sequences of which some are long")
+    lens = [3000, 1, 2048, 0] + [30] * 65 + [1500]
+    m = make(lens, 4, 2, 64, BF16, seed=4)
+    verify(m, 50, 6, run(m, 50, 6))
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_many_equal_sequences_without_offsets(dt):
+    banner(f"window attention 200 sequences without offsets {dt}")
+    m = make([17] * 200, 4, 2, 64, dt)
+    a, b = run(m, 6, 2), run(m, 6, 2, offsets=False)
+    verify(m, 6, 2, b)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
