@@ -382,7 +382,15 @@ __global__ __launch_bounds__(NTB) void layernorm_bwd_kernel(LnP p) {
           if (!HOLD && p.dres) load8<RS>(p.dres, row * p.ld_dres + at[u], p.dres_dt, o[u]);
 #pragma unroll
           for (int e = 0; e < 8; ++e) o[u][e] += rc * (t[u][e] - st - xh[u][e] * sx);
-          store8<OS>(p.dx, row * p.ld_dx + at[u], p.out_dt, o[u]);
+          if (skip[u] && p.dres && lpr > 64) {
+            // (dx may lie over dres, and the shared values belong to another wave, which may not have
+            // read them: they are left to it)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e >= skip[u]) st1(p.dx, row * p.ld_dx + at[u] + e, p.out_dt, o[u][e]);
+          } else {
+            store8<OS>(p.dx, row * p.ld_dx + at[u], p.out_dt, o[u]);
+          }
           if (p.dx_copy) store8<2>(p.dx_copy, row * p.ld_dx + at[u], LC_BF16, o[u]);
         }
     }

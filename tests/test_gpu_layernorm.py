@@ -239,3 +239,20 @@ def test_no_rows():
                              F32, F32)
     torch.cuda.synchronize()
     assert bool((dg == 2.0).all())
+
+
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("T,d", [(300, 1155), (40, 2049), (40, 4099), (300, 8195), (20, 9001), (20, 12289), (20, 16383)])
+def test_dx_over_dres_in_rows_of_no_whole_runs(T, d, out):
+    """The last run of such a row shares values with the one before, which other lanes hold."""
+    banner(f"layernorm dx over dres T={T} d={d} {out}")
+    g = torch.Generator(device=DEV)
+    g.manual_seed(d)
+    x, dy, dres = rows(g, T, d, BF16, d), rows(g, T, d, BF16, d), rows(g, T, d, out, d)
+    gain = rows(g, 1, d, F32, d)[0]
+    types = (BF16, F32, BF16, BF16, out, out)
+    want = run(T, d, x, gain, None, dy, dres, types)[3]
+    for _ in range(3):
+        over = dres.clone()
+        run(T, d, x, gain, None, dy, over, types, dx=over)
+        assert torch.equal(over, want)
