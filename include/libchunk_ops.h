@@ -179,9 +179,7 @@ lc_status lc_rmsnorm_backward_noalloc(const lc_norm_args *args, void *stream);
  * fp32; the variance is summed from differences to the mean. The weight
  * gradients are fixed-order reductions (partial sums of row blocks in `scratch`,
  * lc_layernorm_scratch_bytes, needed only for them, then one ordered sum):
- * run-to-run deterministic. Any T >= 0 (0: nothing happens) and d >= 1; rows
- * that are whole 16-byte runs (d and the leading dimensions multiples of 8)
- * are read and written in such runs.
+ * run-to-run deterministic. 0 <= T < 2^31 (0: nothing happens), 1 <= d <= 2^24.
  * Overlap: y may lie over x, and dx over dy or dres, element for element (the
  * same type and leading dimension); no other output may overlap a tensor that
  * the call reads.
@@ -287,8 +285,10 @@ size_t lc_attention_scratch_bytes_kv(int32_t B, int32_t S, int32_t H, int32_t Hk
  * No output may overlap a tensor that the call reads.
  * Types: matrix-core path: q, k, v LC_FP16 or LC_BF16 (`dtype`; forward
  * products in that type), o, dout, dq, dk, dv LC_BF16 (gradient products in
- * bf16), head_dim 64 or 128, leading dimensions multiples of 8. fp32 path:
- * everything LC_FP32, even head_dim <= 128. Leading dimensions up to 2^24.
+ * bf16; with LC_FP16 inputs those of dO with v and of dS with k in fp16, dO's
+ * rows scaled by powers of two), head_dim 64 or 128, leading dimensions
+ * multiples of 8. fp32 path: everything LC_FP32, even head_dim <= 128.
+ * Leading dimensions up to 2^24.
  */
 typedef struct lc_window_attn_args {
   int32_t dtype;       /* q, k, v */

@@ -770,7 +770,7 @@ __global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
       int hi = sink || p.window >= ke - key ? ke : key + p.window;
       if (splits) {
         const int lim = limit(p, s, kblk);
-        later = sink && key >= s && e > lim;
+        later = sink && key >= s && key - s < p.n_sink && e > lim;
         hi = min(hi, lim);
       }
       cnt = max(0, hi - key);
@@ -1194,8 +1194,6 @@ lc_status bwd(const lc_window_attn_args &a, hipStream_t s) {
   p.nsplit = (int)nsplit;
   if (n > 1 << 22) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^22 blocks of keys and heads");
   const int width = p.Hkv * HD;
-  const size_t chunks = 2 * (size_t)p.T * width / 8;
-  if (chunks / 256 >= 1u << 24) return fail(LC_ERR_UNSUPPORTED, "window attention: k and v of 2^34 or more elements");
   if (sh.QW == 1) hipLaunchKernelGGL((window_dq_kernel<QE, HD, 1, 4>), dim3(grid), dim3(256), 0, s, p);
   else if (sh.KG == 2) hipLaunchKernelGGL((window_dq_kernel<QE, HD, 4, 2>), dim3(grid), dim3(512), 0, s, p);
   else hipLaunchKernelGGL((window_dq_kernel<QE, HD, 4, 1>), dim3(grid), dim3(256), 0, s, p);
@@ -1204,7 +1202,8 @@ lc_status bwd(const lc_window_attn_args &a, hipStream_t s) {
   else hipLaunchKernelGGL((window_dkdv_kernel<QE, HD, 2, 1>), dim3((unsigned)n), dim3(256), 0, s, p);
   LC_TRY(check_launch("window_dkdv_kernel"));
   if (p.parts > 1) {
-    hipLaunchKernelGGL(window_sum_kernel, dim3(ceil_div(chunks, 256)), dim3(256), 0, s, p, width);
+    // (fewer than 384 blocks of keys and heads: window_plan)
+    hipLaunchKernelGGL(window_sum_kernel, dim3(ceil_div(2 * (size_t)p.T * width / 8, 256)), dim3(256), 0, s, p, width);
     LC_TRY(check_launch("window_sum_kernel"));
   }
   if (p.chunks > 1) {
@@ -1258,7 +1257,8 @@ WindowPlan window_plan(int dtype, int64_t T, int H, int Hkv, int hd, int window,
     if (w.parts > 1) w.share = take(2 * w.parts * T * Hkv * hd * 4);
     int64_t chunk = 1024;
     while (chunk < (int64_t)window + w.krows) chunk *= 2;
-    if (n_sink > 0 && n_sink <= MAXSINK && chunk < T) {
+    const int64_t joins = (T + chunk - 1) / chunk * Hkv * n_sink;  // (workgroups of window_join_kernel)
+    if (n_sink > 0 && n_sink <= MAXSINK && chunk < T && joins <= 1 << 23) {
       w.chunk = (int)chunk;
       w.chunks = (int)((T + chunk - 1) / chunk);
       w.slots = take(2ll * w.chunks * Hkv * w.parts * n_sink * 2 * hd * 4);

@@ -12,8 +12,8 @@
 //
 // Rows are read in runs of 8 values at any alignment (the instruction takes any address); the
 // last run of a row whose length is no multiple of 8 begins 8 values before the row's end, and the
-// values that it shares with the run before count once in the sums and are written twice,
-// alike. Whether a tensor has 2 or 4 bytes per value is a template argument (straight-line
+// values that it shares with the run before count once in the sums and are written twice, alike
+// (but where dx may lie over dres: there once). Whether a tensor has 2 or 4 bytes per value is a template argument (straight-line
 // loads); which 16-bit type is a run-time choice of the conversion.
 //
 // The weight gradients are sums over rows. A backward workgroup keeps its rows' share of
@@ -165,7 +165,6 @@ __device__ __forceinline__ int run_at(int n, int d, int &skip) {
   skip = c - at;
   return c < d ? at : d;
 }
-
 
 // ---------------------------------------------------------------- forward
 // WPR waves per row, each lane U runs; U = 1: 64 / lpr rows per wave (lpr < 64 up to 256 values).
@@ -505,7 +504,8 @@ __global__ __launch_bounds__(NTH) void layernorm_bwd_any_kernel(LnP p) {
 }
 
 // ---------------------------------------------------------------- host
-constexpr int MAXD_FWD = 65536, MAXD_BWD = 16384;
+constexpr int MAXD_FWD = 65536, MAXD_BWD = 16384;  // in registers
+constexpr int MAXD = 1 << 24;
 
 int lanes_of(int64_t d, int most) {  // the power of two of lanes that hold a row, 8 values each
   int l = 1;
@@ -525,12 +525,13 @@ int64_t blocks_of(int64_t T, int64_t d) {
   return std::min<int64_t>(d <= 1024 ? 512 : 256, (T + slots - 1) / slots);
 }
 size_t scratch_of(int64_t T, int64_t d) {
-  return T <= 0 || d <= 0 ? 0 : (size_t)blocks_of(T, d) * (size_t)d * 2 * sizeof(float);
+  return T <= 0 || T > INT32_MAX || d <= 0 || d > MAXD ? 0 : (size_t)blocks_of(T, d) * (size_t)d * 2 * sizeof(float);
 }
 
 lc_status check(const lc_layernorm_args &a, bool bwd) {
   if (a.T < 0 || a.d <= 0) return fail(LC_ERR_INVALID_ARG, "layernorm: T must be 0 or more, d positive");
-  if (a.d > INT32_MAX || a.T > INT32_MAX) return fail(LC_ERR_UNSUPPORTED, "layernorm: 2^31 or more rows or values");
+  if (a.d > MAXD) return fail(LC_ERR_UNSUPPORTED, "layernorm: rows of more than 2^24 values");
+  if (a.T > INT32_MAX) return fail(LC_ERR_UNSUPPORTED, "layernorm: 2^31 or more rows");
   if (!valid_dtype(a.x_dtype) || !valid_dtype(a.w_dtype) || !valid_dtype(a.out_dtype))
     return fail(LC_ERR_INVALID_ARG, "layernorm: unknown dtype");
   auto ld_ok = [&](int64_t ld) { return ld == 0 || (ld >= a.d && ld <= INT64_MAX / 4 / (a.T + 1)); };

@@ -3,11 +3,12 @@
 //
 // Pair i turns by pos[axis(i)] f_i. In turns that is pos f_i / (2 pi); its fraction
 // is formed exactly in integers: F_i = round(2^64 f_i / (2 pi)) (computed in 80-bit
-// floating point on the host), and pos F_i mod 2^64 is the fraction of a turn in
-// units of 2^-64, off by at most 2^31 (2^-1 + 2^-64 relative of F_i's own rounding),
-// under 1e-8 rad at any position. The nearest multiple of a quarter turn is split
-// off in integers too, so sin and cos are taken of at most pi/4, where their Taylor
-// series to x^11 and x^12 are exact to fp32.
+// floating point on the host, f_i by at most 127 products of 2^-63 each), and pos F_i
+// mod 2^64 is the fraction of a turn in units of 2^-64. At position 2^31 that is off by
+// F_i's half unit, 2^31 2^-65 turns < 1e-9 rad, and by f_i's error, i 2^-63 f_i 2^31 <
+// 2^-25 rad (f_i = 1 throughout; 1e-9 rad with base 10000). The nearest multiple of a
+// quarter turn is split off in integers too, so sin and cos are taken of at most pi/4, where
+// their Taylor series to x^11 and x^12 are exact to fp32.
 //
 // The rotation is bound by the memory traffic of the head rows (each read and written
 // once). A token's cos and sin are formed once for all of its heads: hd / 2 pairs are

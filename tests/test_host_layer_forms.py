@@ -110,6 +110,25 @@ def test_window_attention_backward(over, want):
     assert status_of(lc.lc_window_attention_backward, **{**args, "scratch_bytes": need - 1}) == WS
 
 
+@pytest.mark.parametrize("d,want", [((1 << 24) + 1, UNSUP), (1 << 30, UNSUP)])
+def test_layernorm_long_rows(d, want):
+    assert status_of(lc.lc_layernorm_forward, **{**LN_F, "d": d}) == want
+    assert status_of(lc.lc_layernorm_backward, **{**LN_B, "d": d}) == want
+    assert lc.lc_layernorm_scratch_bytes(16, d) == 0 < lc.lc_layernorm_scratch_bytes(16, 1 << 24)
+
+
+def test_window_attention_of_too_many_workgroups():
+    """2^29 rows of 2^18 heads: refused before a launch, and no workgroup count wraps."""
+    T, H, hd, ld = 1 << 29, 1 << 18, 64, 1 << 24
+    n = lc.lc_window_attention_scratch_bytes(BF16, T, H, H, hd, 100, 4)
+    assert n >= T * H * 8
+    rows = dict(dtype=BF16, o_dtype=BF16, T=T, B=1, seq_offsets=None, H=H, Hkv=H, hd=hd, window=100, n_sink=4, q=A,
+                ld_q=ld, k=B, ld_k=ld, v=C, ld_v=ld, o=D, ld_o=ld, lse=E)
+    assert status_of(lc.lc_window_attention_forward, **rows) == UNSUP
+    assert status_of(lc.lc_window_attention_backward, **rows, dout=F, ld_dout=ld, dq=A, ld_dq=ld, dk=B, ld_dk=ld,
+                     dv=C, ld_dv=ld, scratch=D, scratch_bytes=n) == UNSUP
+
+
 def test_null_argument_structs():
     L = lc.lib()
     for name in ("lc_layernorm_forward", "lc_layernorm_backward", "lc_rope_axes_forward", "lc_rope_axes_backward",
