@@ -13,8 +13,8 @@
 // and dQ = dS K fp16 products of the caller's own k and v, exact but for dS's rounding, undone
 // in fp32. dV and dK sum over queries, so P and dS are bf16 there, and q's rows are rounded to
 // bf16 on their way from LDS. (With bf16 copies of q, k and v for every gradient product the
-// gradients were 1.85 times as far from 64 bits as their last rounding alone, now 1.4, like those
-// of bf16 inputs.)
+// gradients were 1.85 times as far from 64 bits as their last rounding alone, now 1.45, like
+// those of bf16 inputs.)
 //
 // Work is laid over the packed rows, not over the sequences: a workgroup owns consecutive
 // rows whatever sequences they belong to, each row knows its sequence's start (a search
@@ -484,8 +484,13 @@ __device__ __forceinline__ float row_scale(float x) {
 }
 
 // dQ, and what dK/dV needs of every query: D, -lse log2(e) and, for fp16 inputs, the inverse of its dO
-// row's scale. LDS stage = K | V.
-// QW, KG as in the forward.
+// row's scale. LDS stage = K | V. QW, KG as in the forward.
+//
+// D of a row is taken from its o, which is rounded to bf16. With the exact D a row's dS sum to zero,
+// so their sum is what D was off by, and dK's D gets it added (windows of 8: dk 1.62 times as far from
+// 64 bits as its last rounding alone, now 1.41, all three gradients 1.53, now 1.47; sequences of 8
+// tokens, fp16, 1.60 and 1.48; 8100 tokens, 32/8 heads 465 -> 470 us). dQ's own sums have used the other
+// one, which would take another product to put right.
 template <typename QE, int HD, int QW, int KG>
 __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
   typedef typename V8<QE>::type QV;
@@ -515,6 +520,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
   const int64_t si = (int64_t)h * p.T + min(R.row, p.T - 1);
   const float lse2 = ok ? p.lse[si] * LOG2E : 0.0f;
   float Dq = 0.0f, scale = 1.0f;  // (D, and with it dP and dS, in units of 1 / scale)
+  float off[2] = {0.0f, 0.0f};    // the sums of the row's dS
   f32x16_v acc[NI];
   auto pass = [&](auto pairs_) {
     constexpr bool pairs = decltype(pairs_)::value;
@@ -553,7 +559,6 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
       for (int es = 0; es < NES; ++es) df[es] = __builtin_bit_cast(QV, d16[es]);
     }
     if (!pairs && ok && hf == 0 && kg == 0) {
-      p.D[si] = Dq;
       p.nl2[si] = -lse2;
       if (F16) p.inv[si] = 1.0f / scale;
     }
@@ -598,6 +603,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
             for (int r = 0; r < 16; ++r) {
               const float pv = ex2(__builtin_fmaf(s[j][r], sc, -lse2));
               dp[j][r] = R.sees(k0 + j * 32 + out_row(r, hf)) ? pv * (dp[j][r] - Dq) : 0.0f;
+              if (!pairs) off[j] += dp[j][r];
             }
         } else {
 #pragma unroll
@@ -606,6 +612,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
             for (int r = 0; r < 16; ++r) {
               const float pv = ex2(__builtin_fmaf(s[j][r], sc, -lse2));
               dp[j][r] = pv * (dp[j][r] - Dq);
+              if (!pairs) off[j] += dp[j][r];
             }
         }
         // K^T fragments: transposing reads of the K rows in dS's key order
@@ -625,26 +632,32 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
     }
   };
   pass(std::false_type{});
+  float Dk = sum_with_partner(off[0] + off[1]) + (kg == 0 ? Dq : 0.0f);
   if (__syncthreads_or(not_finite(acc))) pass(std::true_type{});
   if constexpr (KG > 1) {
     typedef __attribute__((address_space(3))) float lds_f;
-    lds_f *const red = reinterpret_cast<lds_f *>(LDS_AS(char, smem)) + w * (HD / 2 * 64) + lane;
-    constexpr int STEP = QW * (HD / 2) * 64;  // to the next group's
+    constexpr int N = HD / 2 + 1;
+    lds_f *const red = reinterpret_cast<lds_f *>(LDS_AS(char, smem)) + w * (N * 64) + lane;
+    constexpr int STEP = QW * N * 64;  // to the next group's
     if (kg > 0) {
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) red[(kg - 1) * STEP + (i * 16 + r) * 64] = acc[i][r];
+      red[(kg - 1) * STEP + (N - 1) * 64] = Dk;
     }
     __syncthreads();
     if (kg > 0) return;
 #pragma unroll
-    for (int x = 0; x < KG - 1; ++x)
+    for (int x = 0; x < KG - 1; ++x) {
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][r] += red[x * STEP + (i * 16 + r) * 64];
+      Dk += red[x * STEP + (N - 1) * 64];
+    }
   }
+  if (ok && hf == 0) p.D[si] = Dk;
   if (ok) store_bf16<HD>(p.dq + (int64_t)R.row * p.ld_dq + (int64_t)h * HD, acc, p.scale / scale, hf);
 }
 

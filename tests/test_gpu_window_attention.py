@@ -389,3 +389,18 @@ def test_many_equal_sequences_without_offsets(dt):
     a, b = run(m, 6, 2), run(m, 6, 2, offsets=False)
     verify(m, 6, 2, b)
     assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("lens,W,S,H,Hkv", [([700, 300], 8, 0, 4, 4), ([8] * 50, 100, 0, 4, 4), ([2000], 8, 1, 24, 24),
+                                            ([1000], 100, 2, 4, 2)])
+def test_dk_and_dv_are_two_roundings_off(lens, W, S, H, Hkv, hd):
+    """bf16: the weights (or their gradients) are rounded and the result is; independent
+    roundings of one relative size add up to sqrt(2) of one, which is the exact result's own."""
+    banner(f"window attention roundings {lens[:3]} W={W} S={S} {H}/{Hkv} x {hd}")
+    m = make(lens, H, Hkv, hd, BF16, seed=1)
+    got = run(m, W, S)
+    ref = reference(m["q"], m["k"], m["v"], m["dout"], seen(lens, 0, m["T"], W, S), H, Hkv, hd)
+    for i in (3, 4):
+        one = float((ref[i].to(torch.bfloat16).double() - ref[i]).norm())
+        assert float((got[i].double() - ref[i]).norm()) < 1.05 * math.sqrt(2) * one, i
