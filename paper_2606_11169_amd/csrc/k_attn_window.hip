@@ -725,6 +725,10 @@ __global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
   constexpr int STAGE = dkdv_stage<QE, HD>();
   __shared__ __align__(256) char smem[dkdv_smem<QE, HD, NP, QG>()];
   __shared__ int keys[2][KROWS];  // lo and cnt (below) of every key
+  // fp16 of head_dim 128 has no registers for the first of K's fragments: it is read again for every
+  // block (8100 tokens in 9 sequences, 32/8 heads: 377 -> 333 us; see lane_again)
+  constexpr bool KL = F16 && HD == 128 && NP == 2;
+  __shared__ __align__(16) char first_k[KL ? NP * 1024 : 16];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6), w = w8 % (2 * NP), kg = w8 / (2 * NP);
   lds_t *const L = LDS_AS(char, smem) + kg * 2 * STAGE;
@@ -849,6 +853,7 @@ __global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
       kf[es] = *reinterpret_cast<const QV *>(static_cast<const QE *>(p.k) + krow * p.ld_k + col);
       vf[es] = *reinterpret_cast<const QV *>(static_cast<const QE *>(p.v) + krow * p.ld_v + col);
     }
+    if (KL && hq == 0) *reinterpret_cast<QV *>(first_k + 1024 * pw + 16 * lane) = kf[0];
 #pragma unroll
     for (int i = 0; i < NI; ++i) dk[i] = dv[i] = zero16();
     wait_vm0();
@@ -875,6 +880,8 @@ __global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
           if constexpr (F16) return scaled_row(x, rs);
           else return x;
         };
+        QV k0{};
+        if (KL) k0 = frag_at<QV>(LDS_AS(char, first_k) + 1024 * pw + 16 * ln);
         QV qv = frag_at<QV>(qrow);
         bf16x8_v da = frag_at<bf16x8_v>(qrow + TL::BYTES);
 #pragma unroll
@@ -883,7 +890,7 @@ __global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
           bf16x8_v dx{};
           if (es + 1 < NES) qx = frag_at<QV>(qrow + 32 * (es + 1));
           __builtin_amdgcn_sched_barrier(0);
-          sv = mfma(qv, kf[es], sv);
+          sv = mfma(qv, KL && es == 0 ? k0 : kf[es], sv);
           if (es + 1 < NES) dx = frag_at<bf16x8_v>(qrow + TL::BYTES + 32 * (es + 1));
           __builtin_amdgcn_sched_barrier(0);
           dp = mfma(scaled(da), vf[es], dp);
