@@ -17,8 +17,8 @@
 // loads); which 16-bit type is a run-time choice of the conversion.
 //
 // The weight gradients are sums over rows. A backward workgroup keeps its rows' share of
-// its columns in registers over all of its rows (a workgroup per compute unit, so the shares
-// stay a small part of the traffic), adds its row slots through LDS in order, and a second
+// its columns in registers over all of its rows (one or two workgroups per compute unit, so the
+// shares stay a small part of the traffic), adds its row slots through LDS in order, and a second
 // kernel adds the workgroups' shares of each column in order: the same bits every run.
 #include "common.hpp"
 
@@ -512,20 +512,22 @@ int lanes_of(int64_t d, int most) {  // the power of two of lanes that hold a ro
   while (l < most && 8ll * l < d) l *= 2;
   return l;
 }
-// Backward: threads per workgroup, and at most one workgroup per compute unit, two for rows of up
-// to 1024 values. More shares cost the final sum more than their rows gain (4096 rows of
-// 4096, fp32: 256 workgroups 54 us with it, 512 57, 1024 60; 20000 x 768 bf16 37, 33 and 37;
-// 30000 x 100 16.4 and 16.6, 1024 22); 512 threads rather than 1024 (100 x 768 9.3 -> 8.1
-// us, 4096 x 4096 56 -> 54) where a row of one run per lane fits them.
+// Backward: threads per workgroup (512 rather than 1024 where a row of one run per lane fits
+// them: 100 x 768 9.3 -> 8.1 us, 4096 x 4096 56 -> 54), and at most one workgroup per compute
+// unit: more shares cost the final sum more than their rows gain (4096 rows of 4096, fp32: 256
+// workgroups 54 us with it, 512 57, 1024 60; 20000 x 768 34 and 38). Rows of 16 bits have half the
+// bytes in flight per workgroup; from 4096 of them on two workgroups of 512 threads per unit gain
+// (20000 x 3000 115 -> 85 us, 20000 x 1536 53 -> 44, 8000 x 4096 51 -> 44, 4000 x 1280 18.6 ->
+// 18.1; but 3000 x 2048 17.5 -> 19.4, and with 1024 threads 16411 x 8192 168 -> 177).
 int bwd_threads(int64_t d) { return d <= 4096 ? 512 : 1024; }
 bool bwd_in_registers(int64_t d) { return d >= 8 && d <= MAXD_BWD; }
-int64_t blocks_of(int64_t T, int64_t d) {
+int64_t blocks_of(int64_t T, int64_t d, bool half) {
   if (!bwd_in_registers(d)) return (T + LONG_ROWS - 1) / LONG_ROWS;
   const int nt = bwd_threads(d), slots = nt / lanes_of(d, nt);
-  return std::min<int64_t>(d <= 1024 ? 512 : 256, (T + slots - 1) / slots);
+  return std::min<int64_t>(half && nt == 512 && T >= 4096 ? 512 : 256, (T + slots - 1) / slots);
 }
-size_t scratch_of(int64_t T, int64_t d) {
-  return T <= 0 || T > INT32_MAX || d <= 0 || d > MAXD ? 0 : (size_t)blocks_of(T, d) * (size_t)d * 2 * sizeof(float);
+size_t scratch_of(int64_t T, int64_t d) {  // for any types
+  return T <= 0 || T > INT32_MAX || d <= 0 || d > MAXD ? 0 : (size_t)blocks_of(T, d, true) * (size_t)d * 2 * sizeof(float);
 }
 
 lc_status check(const lc_layernorm_args &a, bool bwd) {
@@ -648,7 +650,7 @@ lc_status backward(const lc_layernorm_args &a, hipStream_t s) {
   LC_TRY(check(a, true));
   if (a.T == 0) return LC_OK;
   LnP p = params(a);
-  p.nblk = (int)blocks_of(a.T, a.d);
+  p.nblk = (int)blocks_of(a.T, a.d, a.x_dtype != LC_FP32 && a.dy_dtype != LC_FP32);
   p.lpr = lanes_of(a.d, bwd_threads(a.d));
   const bool sums = p.dg || p.db;
   if (bwd_in_registers(a.d)) {
