@@ -7,6 +7,12 @@
 // dK/dV: 16 key rows of a key/value head; the waves take (query head, block of 32 queries)
 // in turn, up to the end of the window of the last key or, where a sink is among the keys,
 // of its sequence.
+//
+// Measured: 600 tokens in 4 sequences, 12 heads of 64, window 128: forward 13 us, dQ 18, dK/dV 22, where
+// a single workgroup of one block takes 7.5, 9 and 9.6: a chain of dependent loads (offsets, rows,
+// keys, values) with 0.9 us of products per block. Loads a block ahead cost registers and were
+// slower (14 -> 17; 2000 tokens, 8/2 heads of 128, window 512, dQ 69 -> 96), as was a bound of 256
+// registers (dK/dV there 370 -> 430).
 #include "attn_f32.hpp"
 #include "attn_window.hpp"
 
