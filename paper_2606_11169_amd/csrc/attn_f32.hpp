@@ -132,10 +132,10 @@ __device__ __forceinline__ void accumulate(f32x4_v (&acc)[NI], const f32x4_v (&w
 }
 
 // The waves' accumulators in LDS: feature e of column c of wave w at (w 16 + c) LD + e
-template <int NI>
+template <int NI, int W = NW>
 struct Merge {
   static constexpr int LD = 16 * NI + 4;
-  static constexpr int FLOATS = NW * QR * LD;
+  static constexpr int FLOATS = W * QR * LD;
   __device__ __forceinline__ static void put(float *s, const f32x4_v (&acc)[NI], int w, int lane) {
     float *row = s + (w * QR + (lane & 15)) * LD + 4 * NI * (lane >> 4);
 #pragma unroll
@@ -146,7 +146,7 @@ struct Merge {
   __device__ __forceinline__ static float sum(const float *s, int c, int e) {
     float t = s[c * LD + e];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) t += s[(w * QR + c) * LD + e];
+    for (int w = 1; w < W; ++w) t += s[(w * QR + c) * LD + e];
     return t;
   }
 };

@@ -8,11 +8,11 @@
 // in turn, up to the end of the window of the last key or, where a sink is among the keys,
 // of its sequence.
 //
-// Measured: 600 tokens in 4 sequences, 12 heads of 64, window 128: forward 13 us, dQ 18, dK/dV 22, where
+// Measured: 600 tokens in 4 sequences, 12 heads of 64, window 128: forward 13 us, dQ 17, dK/dV 23, where
 // a single workgroup of one block takes 7.5, 9 and 9.6: a chain of dependent loads (offsets, rows,
-// keys, values) with 0.9 us of products per block. Loads a block ahead cost registers and were
-// slower (14 -> 17; 2000 tokens, 8/2 heads of 128, window 512, dQ 69 -> 96), as was a bound of 256
-// registers (dK/dV there 370 -> 430).
+// keys, values) with 0.9 us of products per block. 2000 causal tokens, 12 heads: of 64 128, 180 and
+// 230 us, 31 to 35% of the fp32 matrix rate, of 128 225, 333 and 420, 36 to 38%: each wave brings its
+// blocks' rows itself, 32 KB per 128 products of head_dim 64, and waits for them.
 #include "attn_f32.hpp"
 #include "attn_window.hpp"
 
@@ -168,9 +168,10 @@ __global__ __launch_bounds__(NTF) void window_f32_fwd_kernel(WinF p) {
   }
 }
 
-// per 16 queries: D (written for the dK/dV kernel) and dQ
+// per 16 queries: D (written for the dK/dV kernel) and dQ. Bound to two waves per SIMD: above
+// head_dim 64 it would take registers of one (2000 causal tokens, 12 heads of 128: 508 -> 333 us)
 template <int NI>
-__global__ __launch_bounds__(NTF) void window_f32_dq_kernel(WinF p) {
+__global__ __launch_bounds__(NTF, 2) void window_f32_dq_kernel(WinF p) {
   __shared__ __align__(16) float sq[Merge<NI>::FLOATS];
   __shared__ int live[QR];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
@@ -226,11 +227,79 @@ __global__ __launch_bounds__(NTF) void window_f32_dq_kernel(WinF p) {
   }
 }
 
+// rows 16 t + 4 g + r of a block at r0 (at most row `last`), features NI c ..: accumulate_rows' operand
+template <int NI>
+__device__ __forceinline__ void load_rows(float (&x)[2][4][NI], const float *x0, int64_t ld, int r0, int last, int hd,
+                                          bool vec, int lane) {
+  const int g = lane >> 4, c = lane & 15;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      load_run<NI>(x0 + (int64_t)min(r0 + 16 * t + 4 * g + r, last) * ld, NI * c, hd, vec, x[t][r]);
+}
+
+// accumulate (attn_f32.hpp) with the rows' values in x, loaded earlier
+template <int NI, typename F>
+__device__ __forceinline__ void accumulate_rows(f32x4_v (&acc)[NI], const f32x4_v (&w)[2], const float (&x)[2][4][NI],
+                                           const float *x0, int64_t ld, int r0, int last, int hd, int lane,
+                                           bool masked, F vis) {
+  const int g = lane >> 4, c = lane & 15;
+  if (masked) {
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) bad |= !(fabsf(x[t][r][i]) < INFINITY);
+    if (__any(bad)) {
+#pragma unroll 1
+      for (int n = 0; n < 32; ++n) {
+        const int row = r0 + n, t = n >> 4, r = n & 3;
+        float mine = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (u == t && e == r) mine = w[u][e];
+        const float wv = __shfl(mine, c + 16 * ((n >> 2) & 3), 64);
+        if (row > last || !vis(row)) continue;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int f = NI * (4 * g + e) + i;
+            if (f < hd) acc[i][e] += wv * x0[(int64_t)row * ld + f];
+          }
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int i = 0; i < NI; ++i) acc[i] = mfma4(x[t][r][i], w[t][r], acc[i]);
+}
+
 // per 16 keys and key/value head: dK, dV summed over the head's query heads (needs D from the
 // kernel above)
+template <int NI> constexpr int dkdv_waves() { return NI == 8 ? 8 : NW; }  // (why: KVL)
+
 template <int NI>
-__global__ __launch_bounds__(NTF) void window_f32_dkdv_kernel(WinF p) {
-  __shared__ __align__(16) float sk[Merge<NI>::FLOATS], sv[Merge<NI>::FLOATS];
+__global__ __launch_bounds__(64 * dkdv_waves<NI>(), 2) void window_f32_dkdv_kernel(WinF p) {
+  // Whether a block's loads are all issued before its products (both halves' fragments, the
+  // second products' rows, lse and D): at head_dim up to 32 the registers are there (2000 tokens,
+  // 12/4 heads of 32, window 700 190 -> 148 us).
+  constexpr bool EARLY = NI < 4;
+  // Above 64 K's and V's fragments, alike in all waves, are read from LDS for every half block, so
+  // that two waves fit a SIMD (2000 causal tokens, 12 heads of 128: 538 -> 410 us), and they are one
+  // workgroup's eight, so that few key/value heads have them too (2000 tokens, 12/4 heads of 80, window
+  // 700: 393 us with four waves of any registers, 284).
+  constexpr bool KVL = NI == 8;
+  __shared__ __align__(16) float sk[Merge<NI, dkdv_waves<NI>()>::FLOATS], sv[Merge<NI, dkdv_waves<NI>()>::FLOATS];
   __shared__ int live[QR];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
   int k0, kvh;
@@ -249,49 +318,99 @@ __global__ __launch_bounds__(NTF) void window_f32_dkdv_kernel(WinF p) {
   if (tid < QR) live[tid] = cnt > 0;
   const int qend = col_max16(kj + cnt), hi_min = col_min(cnt ? kj + cnt : -1);
   const int64_t hk = (int64_t)kvh * p.hd, kr = min(kj, last);
-  float kf[NI][4], vf[NI][4];
-  load_frag<NI>(p.k + kr * p.ld_k + hk, g, p.hd, p.vec_k, kf);
-  load_frag<NI>(p.v + kr * p.ld_v + hk, g, p.hd, p.vec_v, vf);
+  float kf[KVL ? 1 : NI][4], vf[KVL ? 1 : NI][4];
+  float4 *const kl = reinterpret_cast<float4 *>(sk) + lane, *const vl = reinterpret_cast<float4 *>(sv) + lane;
+  if constexpr (KVL) {
+    if (w < 2) {
+      float x[NI][4];
+      load_frag<NI>((w ? p.v + kr * p.ld_v : p.k + kr * p.ld_k) + hk, g, p.hd, w ? p.vec_v : p.vec_k, x);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) (w ? vl : kl)[64 * j] = make_float4(x[j][0], x[j][1], x[j][2], x[j][3]);
+    }
+    __syncthreads();
+  } else {
+    load_frag<NI>(p.k + kr * p.ld_k + hk, g, p.hd, p.vec_k, kf);
+    load_frag<NI>(p.v + kr * p.ld_v + hk, g, p.hd, p.vec_v, vf);
+  }
   f32x4_v dk[NI], dv[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) dk[i] = dv[i] = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
   // units: (query head of the group, block of 32 queries that reach the keys)
   const int qb0 = k0 / KB, nqb = max(0, (qend + KB - 1) / KB - qb0);
-  for (int u = w; u < p.G * nqb; u += NW) {
+  for (int u = w; u < p.G * nqb; u += dkdv_waves<NI>()) {
     const int h = kvh * p.G + u / nqb, q0 = (qb0 + u % nqb) * KB;
     const int64_t hq = (int64_t)h * p.hd;
     const float *Q = p.q + hq, *dO = p.dout + hq;
     const float *lse = p.lse + (int64_t)h * p.T, *D = p.D + (int64_t)h * p.T;
     f32x4_v pr[2], ds[2];
     auto vis = [&](int qi) { return (uint32_t)(qi - kj) < (uint32_t)cnt; };
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      float qf[NI][4], df[NI][4];
+    float qf[2][NI][4], df[2][NI][4], L[2][4], Dq[2][4], xq[2][4][NI], xo[2][4][NI];
+    auto load = [&](int t) {
       const int64_t qr = min(q0 + 16 * t + c, last);
-      load_frag<NI>(Q + qr * p.ld_q, g, p.hd, p.vec_q, qf);
-      load_frag<NI>(dO + qr * p.ld_do, g, p.hd, p.vec_do, df);
-      const f32x4_v s4 = score<NI>(qf, kf), dp = score<NI>(df, vf);
+      load_frag<NI>(Q + qr * p.ld_q, g, p.hd, p.vec_q, qf[t]);
+      load_frag<NI>(dO + qr * p.ld_do, g, p.hd, p.vec_do, df[t]);
+    };
+    auto load_stats = [&](int t) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int qi = q0 + 16 * t + 4 * g + r, at = min(qi, last);
-        const float P = expf(s4[r] * p.scale - lse[at]);
-        const bool on = vis(qi);
+        const int at = min(q0 + 16 * t + 4 * g + r, last);
+        L[t][r] = lse[at];
+        Dq[t][r] = D[at];
+      }
+    };
+    if (EARLY) {
+      load(0);
+      load(1);
+      load_stats(0);
+      load_stats(1);
+      load_rows<NI>(xo, dO, p.ld_do, q0, last, p.hd, p.vec_do, lane);
+      load_rows<NI>(xq, Q, p.ld_q, q0, last, p.hd, p.vec_q, lane);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (!EARLY) load(t);
+      f32x4_v s4 = {0.0f, 0.0f, 0.0f, 0.0f}, dp = s4;
+      if constexpr (KVL) {
+        asm volatile("" ::: "memory");  // (not kept from the half block before)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const float4 k4 = kl[64 * j], v4 = vl[64 * j];
+          const float ke[4] = {k4.x, k4.y, k4.z, k4.w}, ve[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s4 = mfma4(qf[t][j][e], ke[e], s4);
+            dp = mfma4(df[t][j][e], ve[e], dp);
+          }
+        }
+      } else {
+        s4 = score<NI>(qf[t], kf);
+        dp = score<NI>(df[t], vf);
+      }
+      if (!EARLY) load_stats(t);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float P = expf(s4[r] * p.scale - L[t][r]);
+        const bool on = vis(q0 + 16 * t + 4 * g + r);
         pr[t][r] = on ? P : 0.0f;
-        ds[t][r] = on ? P * (dp[r] - D[at]) : 0.0f;
+        ds[t][r] = on ? P * (dp[r] - Dq[t][r]) : 0.0f;
       }
     }
     const bool masked = q0 < k0 + QR - 1 || q0 + KB > hi_min;
-    accumulate<NI>(dv, pr, dO, p.ld_do, q0, last, p.hd, p.vec_do, lane, masked, vis);
-    accumulate<NI>(dk, ds, Q, p.ld_q, q0, last, p.hd, p.vec_q, lane, masked, vis);
+    if (!EARLY) load_rows<NI>(xo, dO, p.ld_do, q0, last, p.hd, p.vec_do, lane);
+    accumulate_rows<NI>(dv, pr, xo, dO, p.ld_do, q0, last, p.hd, lane, masked, vis);
+    if (!EARLY) load_rows<NI>(xq, Q, p.ld_q, q0, last, p.hd, p.vec_q, lane);
+    accumulate_rows<NI>(dk, ds, xq, Q, p.ld_q, q0, last, p.hd, lane, masked, vis);
   }
-  Merge<NI>::put(sk, dk, w, lane);
-  Merge<NI>::put(sv, dv, w, lane);
+  if (KVL) __syncthreads();  // (the last reads of K and V)
+  Merge<NI, dkdv_waves<NI>()>::put(sk, dk, w, lane);
+  Merge<NI, dkdv_waves<NI>()>::put(sv, dv, w, lane);
   __syncthreads();
-  for (int x = tid; x < QR * p.hd; x += NTF) {
+  for (int x = tid; x < QR * p.hd; x += 64 * dkdv_waves<NI>()) {
     const int r = x / p.hd, el = x % p.hd;
     if (!live[r]) continue;
-    p.dk[(k0 + r) * p.ld_dk + hk + el] = Merge<NI>::sum(sk, r, el) * p.scale;
-    p.dv[(k0 + r) * p.ld_dv + hk + el] = Merge<NI>::sum(sv, r, el);
+    p.dk[(k0 + r) * p.ld_dk + hk + el] = Merge<NI, dkdv_waves<NI>()>::sum(sk, r, el) * p.scale;
+    p.dv[(k0 + r) * p.ld_dv + hk + el] = Merge<NI, dkdv_waves<NI>()>::sum(sv, r, el);
   }
 }
 
@@ -368,7 +487,7 @@ lc_status window_f32_bwd_launch(const lc_window_attn_args &a, hipStream_t s) {
   }));
   return run(p, p.Hkv, "window_f32_dkdv_kernel", [&](const WinF &q, dim3 grid) {
     with_blocks(p.hd, [&](auto ni) {
-      hipLaunchKernelGGL((window_f32_dkdv_kernel<decltype(ni)::value>), grid, dim3(NTF), 0, s, q);
+      hipLaunchKernelGGL((window_f32_dkdv_kernel<decltype(ni)::value>), grid, dim3(64 * dkdv_waves<decltype(ni)::value>()), 0, s, q);
     });
   });
 }
