@@ -102,3 +102,92 @@ def test_attention_half_of_a_layer(fused):
     assert rel(y, Y.detach()) < 2.0 ** -7
     assert rel(dx, X.grad) < 2.0 ** -6 and rel(dw, Wq.grad) < 2.0 ** -6
     assert rel(dg, Gn.grad) < 2.0 ** -6 and rel(db, Bn.grad) < 2.0 ** -6
+
+
+class Pass:
+    """A LayerNorm and a window attention, forward and backward, with tensors of their own."""
+
+    def __init__(self, seed, lens, dt, H, Hkv, hd, W, S):
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed)
+        self.T, self.lens, self.a = sum(lens), lens, (H, Hkv, hd, W, S)
+        self.dt, self.out = dt, F32 if dt == F32 else BF16
+        ty, to = (torch.float32, torch.float32) if dt == F32 else (torch.bfloat16, torch.bfloat16)
+        r = lambda w, t: torch.randn((self.T, w), generator=g, device=DEV).to(t)
+        self.q, self.k, self.v, self.do = r(H * hd, ty), r(Hkv * hd, ty), r(Hkv * hd, ty), r(H * hd, to)
+        self.off = torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device=DEV)
+        self.x, self.dy, self.gain = r(1000, to), r(1000, to), torch.randn(1000, generator=g, device=DEV)
+        e = torch.empty_like
+        self.outs = [e(self.do), torch.empty((H, self.T), device=DEV), e(self.do), e(self.k, dtype=to), e(self.v, dtype=to),
+                     e(self.x), torch.empty(self.T, device=DEV), torch.empty(self.T, device=DEV), e(self.x),
+                     torch.empty(1000, device=DEV), torch.empty(1000, device=DEV)]
+        self.need = (lc.lc_window_attention_scratch_bytes(dt, self.T, H, Hkv, hd, W, S),
+                     lc.lc_layernorm_scratch_bytes(self.T, 1000))
+
+    def __call__(self, scratch, st=None):
+        H, Hkv, hd, W, S = self.a
+        o, lse, dq, dk, dv, y, mean, rstd, dx, dg, db = self.outs
+        a, b, T, B = H * hd, Hkv * hd, self.T, len(self.lens)
+        lc.lc_window_attention_forward(self.dt, self.out, T, B, self.off, H, Hkv, hd, W, S, self.q, a, self.k, b,
+                                       self.v, b, o, a, lse, stream=st)
+        lc.lc_layernorm_forward(T, 1000, self.x, self.gain, None, 1e-5, y, mean, rstd, self.out, F32, self.out, stream=st)
+        lc.lc_window_attention_backward(self.dt, self.out, T, B, self.off, H, Hkv, hd, W, S, self.q, a, self.k, b,
+                                        self.v, b, o, a, lse, self.do, a, dq, a, dk, b, dv, b, scratch, self.need[0],
+                                        stream=st)
+        lc.lc_layernorm_backward(T, 1000, self.dy, self.x, mean, rstd, self.gain, None, dx, dg, db, scratch,
+                                 self.need[1], self.out, self.out, F32, F32, self.out, store_dg=1, stream=st)
+
+    def scratch(self):
+        return torch.full((max(self.need),), 0xFF, dtype=torch.uint8, device=DEV)
+
+    def clear(self):
+        for t in self.outs:
+            t.fill_(7.0)
+        torch.cuda.synchronize()
+
+    def results(self):
+        torch.cuda.synchronize()
+        return [t.clone() for t in self.outs]
+
+
+def passes():
+    return [Pass(1, [700, 3, 900], BF16, 16, 4, 128, 100, 3), Pass(2, [40] * 70, F32, 4, 2, 64, 30, 2),
+            Pass(3, [2000], lc.LC_FP16, 8, 8, 128, 300, 5)]
+
+
+def test_calls_at_once_on_three_streams():
+    banner("layer forms on three streams")
+    ps, streams = passes(), [torch.cuda.Stream() for _ in range(3)]
+    ws = [p.scratch() for p in ps]
+    want = []
+    for p, w in zip(ps, ws):
+        p(w)
+        want.append(p.results())
+        p.clear()
+    for _ in range(5):
+        for p, w, s in zip(ps, ws, streams):
+            p(w, s)
+    for p, ref in zip(ps, want):
+        assert all(torch.equal(a, b) for a, b in zip(p.results(), ref))
+
+
+def test_captured_graphs_that_share_a_workspace():
+    banner("layer forms, graphs that share a workspace")
+    ps = passes()
+    w = max((p.scratch() for p in ps), key=len)
+    want, graphs, side = [], [], torch.cuda.Stream()
+    for p in ps:
+        p(w)
+        want.append(p.results())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            p(w, side)
+    for order in ((0, 1, 2), (2, 0, 1), (1, 1, 0, 2)):
+        for p in ps:
+            p.clear()
+        w.fill_(0xFF)
+        for i in order:  # (one after the other, on one stream)
+            graphs[i].replay()
+        for p, ref in zip(ps, want):
+            assert all(torch.equal(a, b) for a, b in zip(p.results(), ref))
+        ps[order[0]](w)  # eager work of the program's own between the replays
