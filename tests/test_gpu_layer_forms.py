@@ -191,3 +191,45 @@ def test_captured_graphs_that_share_a_workspace():
         for p, ref in zip(ps, want):
             assert all(torch.equal(a, b) for a, b in zip(p.results(), ref))
         ps[order[0]](w)  # eager work of the program's own between the replays
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_rows_past_32_bit_offsets(dt):
+    """Tensors whose rows lie 2^24 values apart (the last ones past 2^31 values, 2^32 bytes) give the
+    same bits as packed ones."""
+    banner(f"layer forms, rows 2^24 values apart {dt}")
+    p = Pass(5, [150, 60], dt, 4, 2, 64, 40, 3)
+    H, Hkv, hd, W, S = p.a
+    T, ld, d, w = p.T, 1 << 24, 1000, p.scratch()
+    p(w)
+    want = p.results()
+    t = torch.float32 if dt == F32 else torch.bfloat16
+    big = torch.empty((T, ld), dtype=t, device=DEV)
+    assert big.numel() > 1 << 31
+    cols = 0
+
+    def wide(src=None, width=0):
+        nonlocal cols
+        v = big[:, cols:cols + (width or src.shape[1])]
+        cols += (v.shape[1] + 63) // 64 * 64
+        if src is not None:
+            v.copy_(src)
+        return v
+
+    q, k, v, do, x, dy = (wide(s) for s in (p.q, p.k, p.v, p.do, p.x, p.dy))
+    o, dq, dk, dv, y, dx = (wide(width=n) for n in (H * hd, H * hd, Hkv * hd, Hkv * hd, d, d))
+    lse, mean, rstd, dg, db = (torch.empty_like(want[i]) for i in (1, 6, 7, 9, 10))
+    lc.lc_window_attention_forward(dt, dt, T, 2, p.off, H, Hkv, hd, W, S, q, ld, k, ld, v, ld, o, ld, lse)
+    lc.lc_window_attention_backward(dt, dt, T, 2, p.off, H, Hkv, hd, W, S, q, ld, k, ld, v, ld, o, ld, lse, do, ld,
+                                    dq, ld, dk, ld, dv, ld, w, p.need[0])
+    lc.lc_layernorm_forward(T, d, x, p.gain, None, 1e-5, y, mean, rstd, dt, F32, dt, ld_x=ld, ld_y=ld)
+    lc.lc_layernorm_backward(T, d, dy, x, mean, rstd, p.gain, None, dx, dg, db, w, p.need[1], dt, dt, F32, F32, dt,
+                             store_dg=1, ld_x=ld, ld_dy=ld, ld_dx=ld)
+    torch.cuda.synchronize()
+    for a, b in zip((o, lse, dq, dk, dv, y, mean, rstd, dx, dg, db), want):
+        assert torch.equal(a, b)
+    pos = torch.arange(2 * T, dtype=torch.int32, device=DEV)
+    packed, apart = torch.empty_like(p.q), wide(width=H * hd)
+    lc.lc_rope_axes_forward(T, H, hd, [20, 12], pos, T, p.q, H * hd, packed, H * hd, dt, dt)
+    lc.lc_rope_axes_forward(T, H, hd, [20, 12], pos, T, q, ld, apart, ld, dt, dt)
+    assert torch.equal(packed, apart)
