@@ -125,7 +125,7 @@ struct WinP {
   int gh, nq;                  // forward, dQ: heads per workgroup, blocks of query rows
   int krows, GP, parts, period;       // dK/dV: keys, query heads per workgroup, blocks of a window (see the walk; 0: none)
   int chunk, chunks;
-  int nmain, nsplit, nkb;      // dK/dV workgroups; 128-key blocks that hold a sequence's sinks
+  int nmain, nsplit, nkb;      // dK/dV workgroups; blocks of krows keys that hold a sequence's sinks
   float scale;
 };
 

@@ -4,8 +4,8 @@
 //
 // A workgroup owns 16 packed rows of one head, whatever sequences they belong to, and its
 // four waves take the visible blocks of 32 keys in turn: the first row's sinks, then from its window on.
-// dK/dV: 16 key rows of a key/value head; the waves take (query head, block of 32 queries)
-// in turn, up to the end of the window of the last key or, where a sink is among the keys,
+// dK/dV: 16 key rows of a key/value head; the waves (eight of head_dim above 64) take (query
+// head, block of 32 queries) in turn, up to the end of the window of the last key or, where a sink is among the keys,
 // of its sequence.
 //
 // Measured: 600 tokens in 4 sequences, 12 heads of 64, window 128: forward 13 us, dQ 17, dK/dV 23, where
