@@ -387,14 +387,17 @@ __global__ __launch_bounds__(NTB) void layernorm_bwd_kernel(LnP p) {
           for (int e = 0; e < 8; ++e) o[u][e] += rc * (t[u][e] - st - xh[u][e] * sx);
           if (skip[u] && p.dres && lpr > 64) {
             // (dx may lie over dres, and the shared values belong to another wave, which may not have
-            // read them: they are left to it)
+            // read them, or have stored dx over what was read here: dx and its copy are left to it)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (e >= skip[u]) st1(p.dx, row * p.ld_dx + at[u] + e, p.out_dt, o[u][e]);
+              if (e >= skip[u]) {
+                st1(p.dx, row * p.ld_dx + at[u] + e, p.out_dt, o[u][e]);
+                if (p.dx_copy) st1(p.dx_copy, row * p.ld_dx + at[u] + e, LC_BF16, o[u][e]);
+              }
           } else {
             store8<OS>(p.dx, row * p.ld_dx + at[u], p.out_dt, o[u]);
+            if (p.dx_copy) store8<2>(p.dx_copy, row * p.ld_dx + at[u], LC_BF16, o[u]);
           }
-          if (p.dx_copy) store8<2>(p.dx_copy, row * p.ld_dx + at[u], LC_BF16, o[u]);
         }
     }
     r0 += step;

@@ -256,3 +256,24 @@ def test_dx_over_dres_in_rows_of_no_whole_runs(T, d, out):
         over = dres.clone()
         run(T, d, x, gain, None, dy, over, types, dx=over)
         assert torch.equal(over, want)
+
+
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("T,d", [(40, 1537), (40, 4097), (30, 8191), (30, 8193), (30, 8195), (20, 8711), (20, 12289), (9, 16383)])
+def test_copy_of_dx_over_dres_in_rows_of_no_whole_runs(T, d, out):
+    """dx_copy where dx lies over dres, at lengths whose last run shares values with another wave's
+    (8193 to 8199, 8705 to 8711, ...: with the wave of another of its runs)."""
+    banner(f"layernorm copy of dx over dres T={T} d={d} {out}")
+    g = torch.Generator(device=DEV)
+    g.manual_seed(d)
+    x, dy, dres = rows(g, T, d, BF16, d), rows(g, T, d, BF16, d), rows(g, T, d, out, d)
+    gain = rows(g, 1, d, F32, d)[0]
+    types = (BF16, F32, BF16, BF16, out, out)
+    copy = torch.full((T + 1, d), 5.0, dtype=torch.bfloat16, device=DEV)
+    want = run(T, d, x, gain, None, dy, dres, types, copy=copy)[3]
+    assert torch.equal(copy[:T], want.to(torch.bfloat16)) and bool((copy[T] == 5.0).all())
+    for _ in range(3):
+        over, copy = dres.clone(), torch.full((T + 1, d), 5.0, dtype=torch.bfloat16, device=DEV)
+        run(T, d, x, gain, None, dy, over, types, dx=over, copy=copy)
+        assert torch.equal(over, want)
+        assert torch.equal(copy[:T], want.to(torch.bfloat16)) and bool((copy[T] == 5.0).all())
