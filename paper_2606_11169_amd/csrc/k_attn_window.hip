@@ -9,12 +9,16 @@
 // the product that takes them.
 //
 // fp16 q, k, v: a gradient's range does not fit fp16, its rows' do. A query's dO is multiplied by
-// the power of two that brings its largest value into [1, 2) (row_scale), which makes dP = dO V^T
-// and dQ = dS K fp16 products of the caller's own k and v, exact but for dS's rounding, undone
-// in fp32. dV and dK sum over queries, so P and dS are bf16 there, and q's rows are rounded to
-// bf16 on their way from LDS. (With bf16 copies of q, k and v for every gradient product the
-// gradients were 1.85 times as far from 64 bits as their last rounding alone, now 1.45, like
-// those of bf16 inputs.)
+// the power of two that brings its largest value into [1, 2) (row_scale), and its dS by one that
+// keeps the largest seen so far between 2^3 and 2^15, lowered (with the sums formed so far, as a
+// softmax's with its maximum) when a block's exceeds that. So dP = dO V^T and dQ = dS K are fp16
+// products of the caller's own k and v, undone in fp32, and besides its rounding dS loses 2^-28 of
+// the row's largest, whatever v's size and the number of keys (with dO's scale alone, rows of 4100 keys
+// with v near 1e-3 were off by up to 4.9 times what the roundings allow; 32768 tokens, 16/4 heads,
+// window 4096 backward 4.55 -> 4.60 ms by it, 8192 x 32 of 64 428 -> 434 us). dV and dK sum over
+// queries, so P and dS are bf16 there, and q's rows are rounded to bf16 on their way from LDS.
+// (With bf16 copies of q, k and v for every gradient product the gradients were 1.85 times as far
+// from 64 bits as their last rounding alone, now 1.45, like those of bf16 inputs.)
 //
 // Work is laid over the packed rows, not over the sequences: a workgroup owns consecutive
 // rows whatever sequences they belong to, each row knows its sequence's start (a search
@@ -526,8 +530,9 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
     __syncthreads();
   };
   const int64_t si = (int64_t)h * p.T + min(R.row, p.T - 1);
-  const float lse2 = ok ? p.lse[si] * LOG2E : 0.0f;
-  float Dq = 0.0f, scale = 1.0f;  // (D, and with it dP and dS, in units of 1 / scale)
+  const float lse2 = ok ? p.lse[si] * LOG2E : INFINITY;  // (a row of no sequence: weights of 0)
+  float Dq = 0.0f, scale = 1.0f;  // (D and dP in units of 1 / scale)
+  int up = F16 ? 60 : 0;          // (dS in units of 2^-up / scale)
   float off[2] = {0.0f, 0.0f};    // the sums of the row's dS
   f32x16_v acc[NI];
   auto pass = [&](auto pairs_) {
@@ -551,10 +556,6 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
         }
       Dq = sum_with_partner(Dq);
       if constexpr (F16) scale = row_scale(max_with_partner(mx));
-    } else if constexpr (F16) {
-      // (dS over the range of fp16, with a |v| of some thousands, is one reason to be here)
-      scale *= 0x1p-12f;
-      Dq *= 0x1p-12f;
     }
     if constexpr (F16) {
 #pragma unroll
@@ -604,12 +605,13 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
           __builtin_amdgcn_sched_barrier(0);
         }
         const bool masked = !R.all(k0);
+        const float nl = F16 ? (float)up - lse2 : -lse2;
         if (masked) {
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              const float pv = ex2(__builtin_fmaf(s[j][r], sc, -lse2));
+              const float pv = ex2(__builtin_fmaf(s[j][r], sc, nl));
               dp[j][r] = R.sees(k0 + j * 32 + out_row(r, hf)) ? pv * (dp[j][r] - Dq) : 0.0f;
               if (!pairs) off[j] += dp[j][r];
             }
@@ -618,10 +620,33 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              const float pv = ex2(__builtin_fmaf(s[j][r], sc, -lse2));
+              const float pv = ex2(__builtin_fmaf(s[j][r], sc, nl));
               dp[j][r] = pv * (dp[j][r] - Dq);
               if (!pairs) off[j] += dp[j][r];
             }
+        }
+        if constexpr (F16 && !pairs) {
+          float mx = 0.0f;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fabsf(dp[j][r]));
+          mx = max_with_partner(mx);
+          if (__any(mx > 0x1p15f)) {
+            const int down = mx > 0x1p15f ? min((int)(__float_as_uint(mx) >> 23) - 130, up + 100) : 0;
+            const float by = __uint_as_float((uint32_t)(127 - down) << 23);
+            up -= down;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              off[j] *= by;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) dp[j][r] *= by;
+            }
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[i][r] *= by;
+          }
         }
         // K^T fragments: transposing reads of the K rows in dS's key order
         if (masked && pairs) {
@@ -640,8 +665,17 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_dq_kernel(WinP p) {
     }
   };
   pass(std::false_type{});
-  float Dk = sum_with_partner(off[0] + off[1]) + (kg == 0 ? Dq : 0.0f);
+  float Dk = sum_with_partner(off[0] + off[1]);
   if (__syncthreads_or(not_finite(acc))) pass(std::true_type{});
+  if constexpr (F16) {
+    const float by = __uint_as_float((uint32_t)(127 - up) << 23);
+    Dk *= by;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] *= by;
+  }
+  if (kg == 0) Dk += Dq;
   if constexpr (KG > 1) {
     typedef __attribute__((address_space(3))) float lds_f;
     constexpr int N = HD / 2 + 1;

@@ -404,3 +404,64 @@ def test_dk_and_dv_are_two_roundings_off(lens, W, S, H, Hkv, hd):
     for i in (3, 4):
         one = float((ref[i].to(torch.bfloat16).double() - ref[i]).norm())
         assert float((got[i].double() - ref[i]).norm()) < 1.05 * math.sqrt(2) * one, i
+
+
+def dq_given_o(m, W, S, o):
+    """dq by its formula in float64, D from the given o; per value the size (root of the sum of
+    squares) of the products that it sums; per row and head the size of what its fp32 sums dP and D
+    come from, |dout| times the weighted mean of |v| |k| / sqrt(hd)."""
+    T, H, Hkv, hd, lens = (m[x] for x in ("T", "H", "Hkv", "hd", "lens"))
+    see = seen(lens, m["first"], T, W, S)
+    q, k, v, dout = (m[x].double() for x in ("q", "k", "v", "dout"))
+    dq, size, sums = torch.zeros_like(q), torch.zeros_like(q), torch.zeros((T, H), dtype=torch.float64, device=DEV)
+    for h in range(H):
+        a, b = slice(h * hd, (h + 1) * hd), slice(h // (H // Hkv) * hd, (h // (H // Hkv) + 1) * hd)
+        s = (q[:, a] @ k[:, b].T / math.sqrt(hd)).masked_fill_(~see, -math.inf)
+        P = torch.exp(s.sub_(torch.logsumexp(s, 1, keepdim=True)))
+        dS = P * (dout[:, a] @ v[:, b].T - (dout[:, a] * o[:, a].double()).sum(1, keepdim=True)) / math.sqrt(hd)
+        dS = torch.where(see, dS, 0.0)
+        dq[:, a], size[:, a] = dS @ k[:, b], (dS.square() @ k[:, b].square()).sqrt()
+        sums[:, h] = dout[:, a].norm(dim=1) * (P @ (v[:, b].norm(dim=1) * k[:, b].norm(dim=1))) / math.sqrt(hd)
+    return dq, size, sums
+
+
+# (lens, W, S, H, Hkv): what a call's rows and heads choose; see WIDE
+DQ = [([8192], 8192, 0, 2, 1), ([4096], 512, 4, 1, 1), ([4100], 5000, 0, 4, 2), ([300, 1, 2700], 700, 3, 16, 16)]
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("size", [1.0, 0.02, 1e-3, 3000.0])
+@pytest.mark.parametrize("lens,W,S,H,Hkv", DQ, ids=[f"{'_'.join(map(str, a[0]))}w{a[1]}h{a[3]}" for a in DQ])
+@pytest.mark.parametrize("bad", ["none", "tail", "token"])
+def test_fp16_dq_is_as_exact_for_any_size_of_v_and_number_of_keys(bad, lens, W, S, H, Hkv, size, hd):
+    """fp16, v of any size and weights of thousands of keys, also in workgroups that hold rows of NaN
+    (behind the last sequence; one key that the rows compared do not see).
+
+    dq is rounded to bf16, each value by at most half a step: 2^-8 of a row's norm, and over all
+    rows as far off as the exact one rounded. Besides that dS is rounded to fp16, each of its products
+    with k by at most 2^-11: independent, so 2^-11 of their root of the sum of squares. And dP and D are
+    fp32 sums of hd products: the n-th step rounds by 2^-24 of a partial sum of size sqrt(n / hd)
+    |dout||v| / sqrt(hd) (independent terms), which add up to less than 2^-24 |dout||v| for each of
+    the two, however much of them cancels in dP - D: 2^-23 of `sums`. (Found to be needed where a
+    row sees one key and D is off by nearly nothing: |dq| 5e-6 where |dout||v| is 2.7, off by 4e-8.)"""
+    banner(f"window attention fp16 dq {bad} {lens} W={W} S={S} {H}/{Hkv} x {hd} v {size}")
+    m = make(lens, H, Hkv, hd, F16, seed=W, tail=40 if bad == "tail" else 0)
+    m["v"].mul_(size)
+    clean = {x: m[x].clone() for x in ("q", "k", "v", "dout")}
+    T, n, at = m["T"], sum(lens), sum(lens) // 2 + 5
+    for x in ("q", "k", "v", "dout"):
+        m[x][n:] = math.nan
+    if bad == "token":
+        m["k"][at], m["v"][at] = math.nan, math.inf
+    o, _, dq, _, _ = run(m, W, S)
+    m.update({x: clean[x] for x in clean})
+    rows = torch.arange(T, device=DEV) < n
+    if bad == "token":
+        rows &= ~seen(lens, 0, T, W, S)[:, at]
+    o[~rows] = 0.0
+    want, parts, sums = dq_given_o(m, W, S, o)
+    off, want, parts = (x[rows].view(-1, H, hd) for x in (dq.double() - want, want, parts))
+    most = 2.0 ** -8 * want.norm(dim=2) + 2.0 ** -11 * parts.norm(dim=2) + 2.0 ** -23 * sums[rows]
+    assert bool((off.norm(dim=2) <= most).all()), float((off.norm(dim=2) / most).max())
+    one = float((want.to(torch.bfloat16).double() - want).norm())
+    assert float(off.norm()) < 1.05 * one + 2.0 ** -11 * float(parts.norm())
