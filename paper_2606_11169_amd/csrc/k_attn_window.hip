@@ -9,11 +9,11 @@
 // the product that takes them.
 //
 // fp16 q, k, v: a gradient's range does not fit fp16, its rows' do. A query's dO is multiplied by
-// the power of two that brings its largest value into [1, 2) (row_scale), and its dS by one that
+// the power of two that brings its largest value into [2^14, 2^15) (row_scale), and its dS by one that
 // keeps the largest seen so far between 2^3 and 2^15, lowered (with the sums formed so far, as a
 // softmax's with its maximum) when a block's exceeds that. So dP = dO V^T and dQ = dS K are fp16
-// products of the caller's own k and v, undone in fp32, and besides its rounding dS loses 2^-28 of
-// the row's largest, whatever v's size and the number of keys (with dO's scale alone, rows of 4100 keys
+// products of the caller's own k and v, undone in fp32, and besides dS's rounding either loses 2^-28
+// of the row's largest value, whatever v's size and the number of keys (with dO's scale alone, rows of 4100 keys
 // with v near 1e-3 were off by up to 4.9 times what the roundings allow; 32768 tokens, 16/4 heads,
 // window 4096 backward 4.55 -> 4.60 ms by it, 8192 x 32 of 64 428 -> 434 us). dV and dK sum over
 // queries, so P and dS are bf16 there, and q's rows are rounded to bf16 on their way from LDS.
@@ -488,11 +488,11 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void window_fwd_kernel(WinP p) {
 }
 
 // ---------------------------------------------------------------- backward
-// the power of two that brings a row's largest absolute value x into [1, 2) (1 for a row of zeros,
-// at most 2^100)
+// the power of two that brings a row's largest absolute value x into [2^14, 2^15), the top of fp16's
+// range but one step (1 for a row of zeros, at most 2^112)
 __device__ __forceinline__ float row_scale(float x) {
   const int e = (int)(__float_as_uint(x) >> 23);
-  return x > 0.0f ? __uint_as_float((uint32_t)(254 - min(max(e, 27), 253)) << 23) : 1.0f;
+  return x > 0.0f ? __uint_as_float((uint32_t)(268 - min(max(e, 29), 253)) << 23) : 1.0f;
 }
 
 // dQ, and what dK/dV needs of every query: D, -lse log2(e) and, for fp16 inputs, the inverse of its dO
@@ -732,10 +732,10 @@ __device__ __forceinline__ float *slot(const WinP &p, int set, int c, int kvh, i
          ((((((int64_t)set * p.chunks + c) * p.Hkv + kvh) * p.parts + part) * p.n_sink) + sink) * (2 * HD);
 }
 
-// fp16 inputs: 8 values of a dO row times its scale, as fp16. c: the scale as (e - 15) << 7 in both
+// fp16 inputs: 8 values of a dO row times its scale, as fp16. c: the scale as (e - 29) << 7 in both
 // halves, e the exponent of the row's largest value in bf16's terms, so that exponents fall by
-// e - 15 and fp16's bias is 15. What falls below fp16's range (2^-14 of the row's largest value) is
-// left as a mantissa of the exponent 0, off by less than that.
+// e - 29 and the largest value's is 29, 2^14 in fp16. What falls below fp16's normal range (2^-28 of the
+// row's largest value) is left as a mantissa of the exponent 0, off by less than that.
 __device__ __forceinline__ f16x8_v scaled_row(bf16x8_v x, uint32_t c) {
   typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_v;
   typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_v;
@@ -915,6 +915,7 @@ __global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
         // each fragment is read one product ahead of the product that uses it
         uint32_t rs = 0;  // this fragment row's scale
         if constexpr (F16) {
+          // (the inverse of the scale has the exponent e - 14)
           rs = (frag_at<uint32_t>(cur + 2 * TL::BYTES + 512 + 128 * hq + 4 * (ln & 31)) >> 23) - 15;
           rs = rs << 7 | rs << 23;
         }
@@ -954,7 +955,7 @@ __global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
             const int r = 4 * gq + x;  // out_row(r, hf) = 8 gq + 4 hf + x
             const float pv = ex2(__builtin_fmaf(sv[r], sc, lc[x]));
             sv[r] = pv;
-            dp[r] = (F16 ? pv * ic[x] : pv) * (dp[r] - dc[x]);
+            dp[r] = pv * (F16 ? ic[x] * (dp[r] - dc[x]) : dp[r] - dc[x]);
           }
         }
         if (masked) {

@@ -465,3 +465,25 @@ def test_fp16_dq_is_as_exact_for_any_size_of_v_and_number_of_keys(bad, lens, W, 
     assert bool((off.norm(dim=2) <= most).all()), float((off.norm(dim=2) / most).max())
     one = float((want.to(torch.bfloat16).double() - want).norm())
     assert float(off.norm()) < 1.05 * one + 2.0 ** -11 * float(parts.norm())
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("lens,W,S,H,Hkv", [([300, 100], 64, 2, 2, 1), ([2000], 300, 0, 24, 24)])
+def test_fp16_a_dominant_value_of_dout(lens, W, S, H, Hkv, hd):
+    """One value of every dout row 2^15 times the others, in a column where v is 1: its part of dP - D
+    cancels, and the gradients are those of the others.
+
+    dP and D are fp32 sums whose terms include the dominant one, 2^12: each of their hd steps rounds by
+    at most 2^-24 of 2^13, sqrt(hd) of them 2^-8 at most, where dP - D has the size sqrt(hd) / 8: less than
+    2^-8 of it at hd = 64. The rest as everywhere: 4 * 2^-8 for a gradient."""
+    banner(f"window attention fp16 dominant dout {lens} {H}/{Hkv} x {hd}")
+    m = make(lens, H, Hkv, hd, F16, seed=5)
+    T = m["T"]
+    m["dout"].mul_(0.125)
+    m["dout"].view(T, H, hd)[:, :, 7] = 4096.0
+    m["v"].view(T, Hkv, hd)[:, :, 7] = 1.0
+    o, lse, dq, dk, dv = run(m, W, S)
+    assert bool((o.view(T, H, hd)[:, :, 7] == 1.0).all())  # (a mean of ones: within 2^-11 of 1, so rounded to it)
+    ref = reference(m["q"], m["k"], m["v"], m["dout"], seen(lens, 0, T, W, S), H, Hkv, hd)
+    for name, got, want in (("dq", dq, ref[2]), ("dk", dk, ref[3])):
+        assert rel(got, want) < 5 * 2.0 ** -8, name
