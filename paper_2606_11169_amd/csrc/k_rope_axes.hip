@@ -39,6 +39,7 @@ template <int N> struct RopeP {
   int64_t ld_x, ld_y, T;
   float *cos, *sin;
   int heads, half, axes, x_dt, y_dt;
+  int turned;      // pairs in the sections
   int lpg, share;  // lanes per group; waves that share a token's heads
   int64_t first;   // the launch's first workgroup
   float sign;  // 1 forward, -1 backward
@@ -171,6 +172,7 @@ __global__ __launch_bounds__(NTH) void rope_axes_kernel(RopeP<N> p) {
       s[i] *= p.sign;
     }
     if (i0 >= p.half) continue;
+    const bool stays = i0 + RUN > p.turned;  // some pair of the run lies past the sections
     int h = h0;
     while (h < p.heads) {
       const int hn = h + stride;
@@ -185,6 +187,14 @@ __global__ __launch_bounds__(NTH) void rope_axes_kernel(RopeP<N> p) {
         const float ai = a.get(i, p.x_dt), bi = b.get(i, p.x_dt);
         u[i] = ai * c[i] - bi * s[i];
         v[i] = bi * c[i] + ai * s[i];
+      }
+      if (stays) {  // (whatever its partner holds: inf 0 is NaN)
+#pragma unroll
+        for (int i = 0; i < RUN; ++i)
+          if (i0 + i >= p.turned) {
+            u[i] = a.get(i, p.x_dt);
+            v[i] = b.get(i, p.x_dt);
+          }
       }
       Vals<YS, RUN> o;
       o.put(u, p.y_dt);
@@ -264,6 +274,7 @@ RopeP<N> params(const lc_rope_axes_args &a, Kind kind) {
     for (int j = 0; j < a.sections[ax]; ++j, ++i, f *= step) p.turn[i] = (uint64_t)llroundl(f * turns);  // (under 2^62)
     if (ax < 3) p.end[ax] = i;
   }
+  p.turned = i;
   for (int ax = a.n_axes; ax < 3; ++ax) p.end[ax] = N;
   p.axes = a.n_axes;
   p.pos = a.pos;

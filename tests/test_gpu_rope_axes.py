@@ -169,3 +169,28 @@ def test_no_tokens():
     lc.lc_rope_axes_forward(0, 2, 64, [32], None, 0, None, 128, None, 128, BF16, BF16)
     lc.lc_rope_axes_table(0, 64, [32], None, 0, None, None)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,heads,hd,sections", [(5, 3, 128, [16, 24, 10]), (40, 9, 64, [8, 9, 10]), (7, 2, 6, [1, 1]),
+                                                 (9, 4, 256, [30, 0, 40, 20]), (3, 5, 130, [64]), (33, 2, 72, [7])])
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+def test_pairs_past_the_sections_stay_as_they_are(T, heads, hd, sections, dt):
+    """Bit for bit (NaN: NaN), also beside an infinite, NaN or negative value of their pair, and with
+    the sign of zero."""
+    banner(f"rope axes pairs past the sections T={T} heads={heads} hd={hd} {sections} {dt}")
+    g = torch.Generator(device=DEV)
+    g.manual_seed(hd)
+    n, half, width = sum(sections), hd // 2, heads * hd
+    pos = torch.randint(-40, 5000, (len(sections), T), generator=g, device=DEV, dtype=torch.int32)
+    x = torch.randn((T, heads, 2, half), generator=g, device=DEV).to(DT[dt])
+    for i, v in enumerate((math.inf, -math.inf, math.nan, -0.0, 0.0)):
+        x[i % T, :, 0, n + i % (half - n)] = v
+        x[(i + 1) % T, :, 1, n + (i + 2) % (half - n)] = v
+    for fn in (lc.lc_rope_axes_forward, lc.lc_rope_axes_backward):
+        y = torch.full_like(x, 3.0)
+        fn(T, heads, hd, sections, pos, T, x, width, y, width, dt, dt)
+        a, b = x[..., n:], y[..., n:]
+        ints = torch.int32 if dt == F32 else torch.int16
+        same = a.contiguous().view(ints) == b.contiguous().view(ints)
+        assert bool((same | (a.isnan() & b.isnan())).all())
+        assert bool(y[..., :n].isfinite().all())
