@@ -279,7 +279,8 @@ size_t lc_attention_scratch_bytes_kv(int32_t B, int32_t S, int32_t H, int32_t Hk
  * A value in a place that a result does not depend on never reaches it, infinite
  * and NaN ones included: later tokens, tokens behind the window, other sequences.
  * Rows of no sequence (before seq_offsets[0], from seq_offsets[B] on) are left as
- * they were in every output. Any T >= 0 (0: nothing happens); T < 2^30.
+ * they were in every output. Any T >= 0 (0: nothing happens), T < 2^30, and T * H up to 2^35
+ * (some larger ones are refused, LC_ERR_UNSUPPORTED).
  * Deterministic (no atomics). The backward's scratch
  * (lc_window_attention_scratch_bytes, for the same arguments) needs no clearing.
  * No output may overlap a tensor that the call reads.

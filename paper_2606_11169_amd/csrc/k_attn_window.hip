@@ -130,6 +130,7 @@ struct WinP {
   int krows, GP, parts, period;       // dK/dV: keys, query heads per workgroup, blocks of a window (see the walk; 0: none)
   int chunk, chunks;
   int nmain, nsplit, nkb;      // dK/dV workgroups; blocks of krows keys that hold a sequence's sinks
+  int first;                   // forward, dQ, dK/dV: the launch's first workgroup
   float scale;
 };
 
@@ -253,7 +254,7 @@ __device__ __forceinline__ bool rows_of(const WinP &p, int qb, int w, int lane, 
 // The workgroup's block of rows and first head, neighbouring blocks of a head next to each other, the last
 // ones (under a window longer than the sequences the heaviest) first
 __device__ __forceinline__ bool place(const WinP &p, int w, int &qb, int &h) {
-  const int t = xcd_task((int)blockIdx.x, p.nq * (p.H / p.gh));
+  const int t = xcd_task(p.first + (int)blockIdx.x, p.nq * (p.H / p.gh));
   if (t < 0) return false;
   qb = p.nq - 1 - t % p.nq;
   h = t / p.nq * p.gh + w % p.gh;
@@ -781,7 +782,7 @@ __global__ __launch_bounds__(128 * NP * QG, 2) void window_dkdv_kernel(WinP p) {
   const Sequences sq(p.off, p.S, p.T, p.B, lane);
   int kblk, kvh, part, c = -1, b, s, e, qa, qb;
   {
-    int i = (int)blockIdx.x;
+    int i = p.first + (int)blockIdx.x;
     const int pad = (p.nsplit + 7) & ~7;  // the long tasks first
     if (i < pad) {
       if (i >= p.nsplit) return;
@@ -1227,9 +1228,18 @@ lc_status row_grid(WinP &p, int QW, unsigned &grid) {
   const int qrows = 32 * QW / p.gh;
   p.nq = (p.T + qrows - 1) / qrows;
   const int64_t n = (int64_t)p.nq * (p.H / p.gh);
-  if (n > 1 << 22) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^22 blocks of rows and heads");
+  if (n > 1 << 30) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^30 blocks of rows and heads");
   grid = (unsigned)((n + 7) / 8 * 8);
   return LC_OK;
+}
+
+// A launch of `kernel` with n workgroups, in parts
+lc_status launch(void (*kernel)(WinP), WinP p, unsigned n, unsigned threads, hipStream_t s, const char *what) {
+  launch_parts(n, [&](uint32_t first, uint32_t count) {
+    p.first = (int)first;
+    hipLaunchKernelGGL(kernel, dim3(count), dim3(threads), 0, s, p);
+  });
+  return check_launch(what);
 }
 
 template <typename QE, int HD>
@@ -1238,10 +1248,9 @@ lc_status fwd(const lc_window_attn_args &a, hipStream_t s) {
   const Shape sh = row_shape(p);
   unsigned grid = 0;
   LC_TRY(row_grid(p, sh.QW, grid));
-  if (sh.QW == 1) hipLaunchKernelGGL((window_fwd_kernel<QE, HD, 1, 4>), dim3(grid), dim3(256), 0, s, p);
-  else if (sh.KG == 2) hipLaunchKernelGGL((window_fwd_kernel<QE, HD, 4, 2>), dim3(grid), dim3(512), 0, s, p);
-  else hipLaunchKernelGGL((window_fwd_kernel<QE, HD, 4, 1>), dim3(grid), dim3(256), 0, s, p);
-  return check_launch("window_fwd_kernel");
+  if (sh.QW == 1) return launch(window_fwd_kernel<QE, HD, 1, 4>, p, grid, 256, s, "window_fwd_kernel");
+  if (sh.KG == 2) return launch(window_fwd_kernel<QE, HD, 4, 2>, p, grid, 512, s, "window_fwd_kernel");
+  return launch(window_fwd_kernel<QE, HD, 4, 1>, p, grid, 256, s, "window_fwd_kernel");
 }
 
 template <typename QE, int HD>
@@ -1255,15 +1264,13 @@ lc_status bwd(const lc_window_attn_args &a, hipStream_t s) {
   const int64_t n = ((nsplit + 7) / 8 + (nmain + 7) / 8) * 8;
   p.nmain = (int)nmain;
   p.nsplit = (int)nsplit;
-  if (n > 1 << 22) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^22 blocks of keys and heads");
+  if (n > 1 << 30) return fail(LC_ERR_UNSUPPORTED, "window attention: more than 2^30 blocks of keys and heads");
   const int width = p.Hkv * HD;
-  if (sh.QW == 1) hipLaunchKernelGGL((window_dq_kernel<QE, HD, 1, 4>), dim3(grid), dim3(256), 0, s, p);
-  else if (sh.KG == 2) hipLaunchKernelGGL((window_dq_kernel<QE, HD, 4, 2>), dim3(grid), dim3(512), 0, s, p);
-  else hipLaunchKernelGGL((window_dq_kernel<QE, HD, 4, 1>), dim3(grid), dim3(256), 0, s, p);
-  LC_TRY(check_launch("window_dq_kernel"));
-  if (p.krows == 32) hipLaunchKernelGGL((window_dkdv_kernel<QE, HD, 1, 2>), dim3((unsigned)n), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((window_dkdv_kernel<QE, HD, 2, 1>), dim3((unsigned)n), dim3(256), 0, s, p);
-  LC_TRY(check_launch("window_dkdv_kernel"));
+  if (sh.QW == 1) LC_TRY(launch(window_dq_kernel<QE, HD, 1, 4>, p, grid, 256, s, "window_dq_kernel"));
+  else if (sh.KG == 2) LC_TRY(launch(window_dq_kernel<QE, HD, 4, 2>, p, grid, 512, s, "window_dq_kernel"));
+  else LC_TRY(launch(window_dq_kernel<QE, HD, 4, 1>, p, grid, 256, s, "window_dq_kernel"));
+  if (p.krows == 32) LC_TRY(launch(window_dkdv_kernel<QE, HD, 1, 2>, p, (unsigned)n, 256, s, "window_dkdv_kernel"));
+  else LC_TRY(launch(window_dkdv_kernel<QE, HD, 2, 1>, p, (unsigned)n, 256, s, "window_dkdv_kernel"));
   if (p.parts > 1) {
     // (fewer than 384 blocks of keys and heads: window_plan)
     hipLaunchKernelGGL(window_sum_kernel, dim3(ceil_div(2 * (size_t)p.T * width / 8, 256)), dim3(256), 0, s, p, width);

@@ -487,3 +487,28 @@ def test_fp16_a_dominant_value_of_dout(lens, W, S, H, Hkv, hd):
     ref = reference(m["q"], m["k"], m["v"], m["dout"], seen(lens, 0, T, W, S), H, Hkv, hd)
     for name, got, want in (("dq", dq, ref[2]), ("dk", dk, ref[3])):
         assert rel(got, want) < 5 * 2.0 ** -8, name
+
+
+def test_more_workgroups_than_a_launch_holds():
+    """2080 tokens of 2^18 heads are 65 x 2^16 workgroups, over the 2^22 of one launch: 130 GB of q and o."""
+    banner("window attention forward of 2^18 heads")
+    T, H, hd, W = 2080, 1 << 18, 64, 40
+    if torch.cuda.mem_get_info()[0] + torch.cuda.memory_reserved() - torch.cuda.memory_allocated() < 160e9:
+        pytest.skip("less than 160 GB of memory are free")
+    torch.cuda.empty_cache()
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    q = torch.empty((T, H * hd), dtype=torch.bfloat16, device=DEV)
+    for rows in q.split(130):
+        rows.normal_(generator=g)
+    k, v = (torch.randn((T, hd), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    o, lse = torch.empty_like(q), torch.empty((H, T), device=DEV)
+    lc.lc_window_attention_forward(BF16, BF16, T, 1, None, H, 1, hd, W, 2, q, H * hd, k, hd, v, hd, o, H * hd, lse)
+    torch.cuda.synchronize()
+    heads = [0, 1, 5, 4095, 100001, H // 2, H - 2, H - 1]
+    qs = torch.stack([q[:, h * hd:(h + 1) * hd] for h in heads], 1).view(T, -1)
+    os = torch.stack([o[:, h * hd:(h + 1) * hd] for h in heads], 1).view(T, -1)
+    ref = reference(qs, k, v, torch.zeros_like(qs), seen([T], 0, T, W, 2), len(heads), 1, hd)
+    assert rel(os, ref[0]) < TOL_O[BF16] and float((lse[heads].double() - ref[1]).abs().max()) < 2e-4
+    del q, o, lse
+    torch.cuda.empty_cache()
