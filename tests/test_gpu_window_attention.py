@@ -512,3 +512,28 @@ def test_more_workgroups_than_a_launch_holds():
     assert rel(os, ref[0]) < TOL_O[BF16] and float((lse[heads].double() - ref[1]).abs().max()) < 2e-4
     del q, o, lse
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("tail", [0, 37])
+@pytest.mark.parametrize("lens,W,S,H,Hkv", [([700, 300], 40, 0, 4, 4), ([2000, 1, 500], 300, 3, 24, 24),
+                                            ([3000], 3000, 0, 10, 5), ([1000], 100, 2, 4, 2)])
+def test_gradients_are_their_roundings_off(lens, W, S, H, Hkv, tail, dt, hd):
+    """Independent roundings of one relative size add up in squares to that of the exact result alone:
+    two for dq of bf16 (dS and the result; D given o), dv (the weights and the result) and dk of bf16 (dS
+    and the result), three for dk of fp16, whose q is rounded to bf16; one for dq of fp16, whose dS has
+    an eighth of its step. Rows of NaN behind the last sequence change nothing."""
+    banner(f"window attention gradient roundings {lens} +{tail} W={W} S={S} {dt} {H}/{Hkv} x {hd}")
+    m = make(lens, H, Hkv, hd, dt, seed=3, tail=tail)
+    n = sum(lens)
+    clean = {x: m[x].clone() for x in ("q", "k", "v", "dout")}
+    for x in clean:
+        m[x][n:] = math.nan
+    o, _, dq, dk, dv = run(m, W, S)
+    m.update(clean)
+    ref = reference(m["q"], m["k"], m["v"], m["dout"], seen(lens, 0, m["T"], W, S), H, Hkv, hd)
+    want = (dq_given_o(m, W, S, o)[0], ref[3], ref[4])
+    for name, a, b, k in zip(("dq", "dk", "dv"), (dq, dk, dv), want, (2, 2, 2) if dt == BF16 else (1 + 1 / 64, 3, 2)):
+        one = float((b[:n].to(torch.bfloat16).double() - b[:n]).norm())
+        assert float((a[:n].double() - b[:n]).norm()) < 1.05 * math.sqrt(k) * one, name
