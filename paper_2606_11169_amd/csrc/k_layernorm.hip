@@ -260,18 +260,31 @@ __device__ __forceinline__ float block_sum(float v, float *red) {
   return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+// A thread's sum of up to 65536 values of a row, with what each addition rounds off carried along
+// (added up plainly, 2^24 equal values are off by the same direction's rounding 65536 times: their mean by
+// 6.5e-4 of them, now 1e-7; 512 x 100000 fp32 forward 536 -> 549 us, backward 713 -> 721)
+struct Sum {
+  float s = 0.0f, lost = 0.0f;
+  __device__ __forceinline__ void add(float x) {
+#pragma clang fp contract(off)
+    const float y = x - lost, t = s + y;
+    lost = (t - s) - y;
+    s = t;
+  }
+};
+
 // rows shorter than a run or longer than registers hold: a workgroup per row, value by value
 __global__ __launch_bounds__(NTH) void layernorm_fwd_any_kernel(LnP p) {
   __shared__ float red[4];
   const int64_t t = p.first + blockIdx.x;
-  float s = 0.0f, v = 0.0f;
-  for (int k = threadIdx.x; k < p.d; k += NTH) s += ld1(p.x, t * p.ld_x + k, p.x_dt);
-  const float mu = block_sum(s, red) / (float)p.d;
+  Sum s, v;
+  for (int k = threadIdx.x; k < p.d; k += NTH) s.add(ld1(p.x, t * p.ld_x + k, p.x_dt));
+  const float mu = block_sum(s.s, red) / (float)p.d;
   for (int k = threadIdx.x; k < p.d; k += NTH) {
     const float c = ld1(p.x, t * p.ld_x + k, p.x_dt) - mu;
-    v += c * c;
+    v.add(c * c);
   }
-  const float r = 1.0f / sqrtf(block_sum(v, red) / (float)p.d + p.eps);
+  const float r = 1.0f / sqrtf(block_sum(v.s, red) / (float)p.d + p.eps);
   if (threadIdx.x == 0) {
     p.mean[t] = mu;
     p.rstd[t] = r;
@@ -492,14 +505,13 @@ __global__ __launch_bounds__(NTH) void layernorm_bwd_any_kernel(LnP p) {
   __shared__ float red[4];
   const int64_t t = p.first + blockIdx.x;
   const float mu = p.mean[t], r = p.rstd[t];
-  float s = 0.0f, q = 0.0f;
+  Sum su, sq;
   for (int k = threadIdx.x; k < p.d; k += NTH) {
     const float u = scaled(ld1(p.dy, t * p.ld_dy + k, p.dy_dt), ld1(p.g, k, p.w_dt));
-    s += u;
-    q += u * ((ld1(p.x, t * p.ld_x + k, p.x_dt) - mu) * r);
+    su.add(u);
+    sq.add(u * ((ld1(p.x, t * p.ld_x + k, p.x_dt) - mu) * r));
   }
-  s = block_sum(s, red) / (float)p.d;
-  q = block_sum(q, red) / (float)p.d;
+  const float s = block_sum(su.s, red) / (float)p.d, q = block_sum(sq.s, red) / (float)p.d;
   for (int k = threadIdx.x; k < p.d; k += NTH) {
     const float u = scaled(ld1(p.dy, t * p.ld_dy + k, p.dy_dt), ld1(p.g, k, p.w_dt));
     const float xh = (ld1(p.x, t * p.ld_x + k, p.x_dt) - mu) * r;

@@ -277,3 +277,21 @@ def test_copy_of_dx_over_dres_in_rows_of_no_whole_runs(T, d, out):
         run(T, d, x, gain, None, dy, over, types, dx=over, copy=copy)
         assert torch.equal(over, want)
         assert torch.equal(copy[:T], want.to(torch.bfloat16)) and bool((copy[T] == 5.0).all())
+
+
+@pytest.mark.parametrize("d", [70001, 1 << 20, (1 << 24) - 3])
+def test_long_rows_of_equal_values(d):
+    """Rows of one value: y is the bias, and with equal dy g the row's dx is 0. A thread's compensated sum
+    is off by some 2^-23 of itself and eight more additions join the threads' (2^-24 each), so the mean is
+    off by less than 2^-20 of the value, y by that over sqrt(eps), which also bounds xh; dx = r (t - mean t
+    - xh mean(t xh)): 2^-20 |t| r for the first two terms, less for the third."""
+    banner(f"layernorm long rows of equal values d={d}")
+    T, r = 3, EPS ** -0.5
+    x = torch.tensor([0.1, -0.7, 0.3], device=DEV)[:, None].expand(T, d).contiguous()
+    dy = torch.tensor([0.3, 0.1, -1.1], device=DEV)[:, None].expand(T, d).contiguous()
+    gain, bias = torch.ones(d, device=DEV), torch.zeros(d, device=DEV)
+    y, mean, _, dx, _, _ = run(T, d, x, gain, bias, dy, None, (F32,) * 6)
+    at = 2.0 ** -20
+    assert bool(((mean - x[:, 0]).abs() <= at * x[:, 0].abs()).all())
+    assert float(y.abs().max()) <= at * 0.7 * r
+    assert float(dx.abs().max()) <= 2 * at * 1.1 * r
