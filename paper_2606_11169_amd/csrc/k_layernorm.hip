@@ -13,8 +13,9 @@
 // Rows are read in runs of 8 values at any alignment (the instruction takes any address); the
 // last run of a row whose length is no multiple of 8 begins 8 values before the row's end, and the
 // values that it shares with the run before count once in the sums and are written twice, alike
-// (but where dx may lie over dres: there once). Whether a tensor has 2 or 4 bytes per value is a template argument (straight-line
-// loads); which 16-bit type is a run-time choice of the conversion.
+// (but once by the backward of two runs per lane, which reads dres late, where dx may lie over it).
+// Whether a tensor has 2 or 4 bytes per value is a template argument (straight-line loads); which
+// 16-bit type is a run-time choice of the conversion.
 //
 // The weight gradients are sums over rows. A backward workgroup keeps its rows' share of
 // its columns in registers over all of its rows (one or two workgroups per compute unit, so the
@@ -380,6 +381,9 @@ __global__ __launch_bounds__(NTB) void layernorm_bwd_kernel(LnP p) {
         dots[odd][0][wv] = st;
         dots[odd][1][wv] = sx;
       }
+      // (dx may lie over dres, whose shared values another wave stores from here on: the run's last value
+      // is waited for, loads return in order)
+      if (HOLD) asm volatile("" ::"v"(o[0][7]));
       __syncthreads();
       const int w0 = slot * (lpr / 64);
       st = dots[odd][0][w0];
@@ -398,7 +402,7 @@ __global__ __launch_bounds__(NTB) void layernorm_bwd_kernel(LnP p) {
           if (!HOLD && p.dres) load8<RS>(p.dres, row * p.ld_dres + at[u], p.dres_dt, o[u]);
 #pragma unroll
           for (int e = 0; e < 8; ++e) o[u][e] += rc * (t[u][e] - st - xh[u][e] * sx);
-          if (skip[u] && p.dres && lpr > 64) {
+          if (!HOLD && skip[u] && p.dres) {
             // (dx may lie over dres, and the shared values belong to another wave, which may not have
             // read them, or have stored dx over what was read here: dx and its copy are left to it)
 #pragma unroll
