@@ -616,7 +616,7 @@ void fwd_shape(LnP p, hipStream_t s) {
           p.first = first;
           hipLaunchKernelGGL((layernorm_fwd_kernel<WPR, U, decltype(xs)::value, decltype(ws)::value, decltype(ys)::value>),
                              dim3(count), dim3(64 * NW), 0, s, p);
-        });
+        }, 64 * NW > 512 ? 64 * NW : 512);
       });
     });
   });

@@ -295,3 +295,29 @@ def test_long_rows_of_equal_values(d):
     assert bool(((mean - x[:, 0]).abs() <= at * x[:, 0].abs()).all())
     assert float(y.abs().max()) <= at * 0.7 * r
     assert float(dx.abs().max()) <= 2 * at * 1.1 * r
+
+
+def test_more_long_rows_than_a_launch_holds():
+    """Rows of over 8192 values are a workgroup of 1024 threads each: 2^22 of them (69 GB, in place) are
+    2^32 work-items, one more than a launch takes."""
+    T, d = (1 << 22) + 3, 8200
+    banner(f"layernorm forward T={T} d={d}")
+    if torch.cuda.mem_get_info()[0] + torch.cuda.memory_reserved() - torch.cuda.memory_allocated() < 100e9:
+        pytest.skip("less than 100 GB of memory are free")
+    torch.cuda.empty_cache()
+    g = torch.Generator(device=DEV)
+    g.manual_seed(9)
+    x = torch.empty((T, d), dtype=torch.bfloat16, device=DEV)
+    for part in x.split(1 << 17):
+        part.normal_(generator=g)
+    gain = 1 + 0.1 * torch.randn(d, generator=g, device=DEV)
+    at = torch.tensor([0, 1, (1 << 21) - 1, 1 << 21, (1 << 22) - 1, 1 << 22, T - 1], device=DEV)
+    was = x[at].double()
+    mean, rstd = (torch.full((T,), -7.0, device=DEV) for _ in range(2))
+    lc.lc_layernorm_forward(T, d, x, gain, None, EPS, x, mean, rstd, BF16, F32, BF16)
+    torch.cuda.synchronize()
+    y, m, r = reference(was, gain.double(), None, was, None)[:3]
+    assert rel(x[at], y) < STEP[BF16] and rel(mean[at], m) < 1e-5 and rel(rstd[at], r) < 1e-6
+    assert bool((rstd > 0).all())
+    del x
+    torch.cuda.empty_cache()
