@@ -275,19 +275,23 @@ size_t lc_attention_scratch_bytes_kv(int32_t B, int32_t S, int32_t H, int32_t Hk
  * their own leading dimensions. Grouped-query attention: k, v, dk and dv have
  * Hkv heads (0: H) and query head h uses key/value head h / (H / Hkv).
  * Backward: the formulas of lc_attention_backward over the pairs above, given o
- * and lse of the forward; dk and dv sum over the query heads of their group.
+ * and lse as lc_window_attention_forward gives them for the same q, k, v, sequences,
+ * window and sinks: a row's weights are taken to sum to 1, so an o and lse joined over
+ * the keys of several calls are not meant. dk and dv sum over the query heads of their group.
  * A value in a place that a result does not depend on never reaches it, infinite
  * and NaN ones included: later tokens, tokens behind the window, other sequences.
  * Rows of no sequence (before seq_offsets[0], from seq_offsets[B] on) are left as
- * they were in every output. Any T >= 0 (0: nothing happens), T < 2^30, and T * H up to 2^35
- * (some larger ones are refused, LC_ERR_UNSUPPORTED).
+ * they were in every output. Any T >= 0 (0: nothing happens), T < 2^30, and T * H up to 2^34
+ * (some larger ones are refused, LC_ERR_UNSUPPORTED). Sinks are seen by their whole sequence: in
+ * 16 bits dk and dv of up to 256 of them are shared out over the sequence's queries; of more, and
+ * in fp32, one workgroup per block of keys and head visits them all, a call's time with it.
  * Deterministic (no atomics). The backward's scratch
  * (lc_window_attention_scratch_bytes, for the same arguments) needs no clearing.
  * No output may overlap a tensor that the call reads.
  * Types: matrix-core path: q, k, v LC_FP16 or LC_BF16 (`dtype`; forward
  * products in that type), o, dout, dq, dk, dv LC_BF16 (gradient products in
- * bf16; with LC_FP16 inputs those of dO with v and of dS with k in fp16, dO's
- * rows scaled by powers of two), head_dim 64 or 128, leading dimensions
+ * bf16; with LC_FP16 inputs those of dO with v and of dS with k in fp16, rows of dO
+ * and of dS scaled by powers of two of their own), head_dim 64 or 128, leading dimensions
  * multiples of 8. fp32 path: everything LC_FP32, even head_dim <= 128.
  * Leading dimensions up to 2^24.
  */
@@ -333,7 +337,7 @@ size_t lc_window_attention_scratch_bytes(int32_t dtype, int64_t T, int32_t H, in
  * the sections). Given with rope_seq = T to lc_gemm's LC_EPI_ROPE, or with
  * seq_len = T to lc_qk_norm_rope_forward, it makes those rotate by several axes.
  * Overlap: y may lie over x, element for element (the same type and leading
- * dimension). Any T >= 0 (0: nothing happens), 1 <= n_axes <= 4, even hd <= 256,
+ * dimension). 0 <= T < 2^31 (0: nothing happens), 1 <= n_axes <= 4, even hd <= 256,
  * 1 <= sum of sections <= hd/2, base >= 1.
  */
 typedef enum lc_rope_freq { LC_ROPE_FREQ_HEAD = 0, LC_ROPE_FREQ_AXIS = 1 } lc_rope_freq;
