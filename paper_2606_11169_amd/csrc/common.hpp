@@ -130,13 +130,13 @@ __device__ __forceinline__ float wave_sum(float v) {
 
 inline unsigned ceil_div(size_t a, size_t b) { return unsigned((a + b - 1) / b); }
 
-// launch(first, count) for n workgroups of `threads` in parts that keep under the launch limit of
-// 2^32 work-items; the kernel adds `first` to its index
+// launch(first, count) for n workgroups in parts that keep under the launch limit of 2^32
+// work-items (for workgroups of at most 512 threads); the kernel adds `first` to its index
 template <typename F>
-inline void launch_parts(uint32_t n, F launch, uint32_t threads = 512) {
-  const uint32_t part = (1u << 31) / threads;
+inline void launch_parts(uint32_t n, F launch) {
+  constexpr uint32_t PART = 1u << 22;
   for (uint32_t first = 0; n > 0;) {
-    const uint32_t count = n < part ? n : part;
+    const uint32_t count = n < PART ? n : PART;
     launch(first, count);
     first += count;
     n -= count;

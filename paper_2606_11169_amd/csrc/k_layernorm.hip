@@ -608,15 +608,18 @@ template <typename F> void with_size(int dt, F f) {
 template <int WPR, int U>
 void fwd_shape(LnP p, hipStream_t s) {
   constexpr int NW = WPR > 4 ? WPR : NTH / 64;
+  constexpr uint32_t PART = 1u << 21;
   const int64_t rows = U == 1 ? NW * (64 / p.lpr) : NW / WPR;
   with_size(p.x_dt, [&](auto xs) {
     with_size(p.w_dt, [&](auto ws) {
       with_size(p.out_dt, [&](auto ys) {
-        launch_parts((uint32_t)((p.T + rows - 1) / rows), [&](uint32_t first, uint32_t count) {
+        const uint32_t n = (uint32_t)((p.T + rows - 1) / rows);
+        // in parts under a launch's limit of 2^32 work-items (launch_parts is for up to 512 threads)
+        for (uint32_t first = 0; first < n; first += PART) {
           p.first = first;
           hipLaunchKernelGGL((layernorm_fwd_kernel<WPR, U, decltype(xs)::value, decltype(ws)::value, decltype(ys)::value>),
-                             dim3(count), dim3(64 * NW), 0, s, p);
-        }, 64 * NW > 512 ? 64 * NW : 512);
+                             dim3(std::min(PART, n - first)), dim3(64 * NW), 0, s, p);
+        }
       });
     });
   });
