@@ -36,12 +36,12 @@
 // masked blocks pair by pair, leaving out the masked ones: a value that a result does not
 // depend on never reaches it, and finite data pay one look at the result.
 //
-// Measured, bf16: one sequence of 32768, 16/4 heads of 128, window 4096, 64 sinks: forward 1050 us, dQ
-// 1420, dK/dV 2070, 1.00, 1.10 and 1.01 PFLOP/s of the products over visible pairs (2, 3 and 4 of
+// Measured, bf16: one sequence of 32768, 16/4 heads of 128, window 4096, 64 sinks: forward 1030 us, dQ
+// 1410, dK/dV 2050, 1.02, 1.11 and 1.02 PFLOP/s of the products over visible pairs (2, 3 and 4 of
 // them); the matrix cores are 48, 56 and 51% busy, vector units 43, 44 and 35%, LDS 24 to 32%: two
 // waves per SIMD alternate between products and exponentials and overlap in part. One of 4096, 32 heads,
-// window 1024, 4 sinks: all of it 378 us, 70% of that rate: chains of 18 blocks each with its start,
-// three of them a window's edges and the sinks'. 77 tokens in 5 sequences, 8 heads of 64, forward: 7.3,
+// window 1024, 4 sinks: all of it 377 us, 70% of that rate: chains of 18 blocks each with its start,
+// three of them a window's edges and the sinks'. 77 tokens in 5 sequences, 8 heads of 64, forward: 7.2,
 // offsets, rows and keys loaded one after the other.
 #include "attn_tiles.hpp"
 #include "attn_window.hpp"

@@ -6,9 +6,10 @@
 //             dg += sum_t dy xh, db += sum_t dy
 //
 // Every tensor is read once and written once: a row stays in registers between its
-// sums and its write (up to 65536 values forward, 16384 backward; longer rows are read
-// again, from L2), the variance is a second sum over the registers, of differences to the
-// mean (sums of squares would lose it in rows far from 0).
+// sums and its write (8 to 65536 values forward, 16384 backward), the variance is a second sum
+// over the registers, of differences to the mean (sums of squares would lose it in rows far from
+// 0). Shorter and longer rows are read three times forward; backward once by the weight
+// gradients' launch and twice by the rows', so x and dy come from HBM at least twice there.
 //
 // Rows are read in runs of 8 values at any alignment (the instruction takes any address); the
 // last run of a row whose length is no multiple of 8 begins 8 values before the row's end, and the
@@ -22,9 +23,10 @@
 // shares stay a small part of the traffic), adds its row slots through LDS in order, and a second
 // kernel adds the workgroups' shares of each column in order: the same bits every run.
 //
-// Measured: 16411 rows of 8192, bf16, forward 107 us, backward with a residual 201 + 5, 5.0 and
-// 5.3 TB/s (a large copy reaches 5.1 to 5.5 here); 4096 of 4096, fp32 in, 16.4 and 44 + 4; 3001 of
-// 1155 bf16 6.6 and 13 + 2.5, 9 of 768 2.7, bound by the latency of loads, sums and launches.
+// Measured (shortest launches of a trace): 16411 rows of 8192, bf16, forward 107 us (98 back to
+// back), backward with a residual 201 + 5, 5.0 and 5.3 TB/s (a large copy reaches 5.1 to 5.5 here);
+// 4096 of 4096, fp32 in, 17.3 and 44 + 4; 3001 of 1155 bf16 6.3 and 13 + 2.7, 9 of 768 2.7, bound by
+// the latency of loads, sums and launches.
 #include "common.hpp"
 
 #include <algorithm>

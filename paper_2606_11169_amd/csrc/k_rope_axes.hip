@@ -16,7 +16,7 @@
 // the wave's groups walk the token's heads with the same cos and sin in registers. Few
 // tokens share out their heads over more waves instead, so that the chip is filled. Measured: 32760
 // tokens of 24 heads of 128, bf16, 76 us, 5.3 TB/s (a large copy reaches 5.1 to 5.5 here); 1601 of 40
-// heads 9.8 us, a launch and two dependent loads; a table of 8192 x 64 4.0 us.
+// heads 8.6 us, a launch and two dependent loads; a table of 8192 x 64 4.0 us.
 #include "common.hpp"
 
 #include <math.h>
