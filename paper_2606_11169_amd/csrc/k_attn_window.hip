@@ -13,11 +13,11 @@
 // keeps the largest seen so far between 2^3 and 2^15, lowered (with the sums formed so far, as a
 // softmax's with its maximum) when a block's exceeds that. So dP = dO V^T and dQ = dS K are fp16
 // products of the caller's own k and v, undone in fp32, and besides dS's rounding either loses 2^-28
-// of the row's largest value, whatever v's size and the number of keys (with dO's scale alone, rows of 4100 keys
-// with v near 1e-3 were off by up to 4.9 times what the roundings allow; 32768 tokens, 16/4 heads,
-// window 4096 backward 4.55 -> 4.60 ms by it, 8192 x 32 of 64 428 -> 434 us). dV and dK sum over
-// queries, so P and dS are bf16 there, and q's rows are rounded to bf16 on their way from LDS.
-// (With bf16 copies of q, k and v for every gradient product the gradients were 1.85 times as far
+// of the row's largest value, whatever v's size and the number of keys (with dO's scale alone, rows
+// of 4100 keys with v near 1e-3 were off by up to 4.9 times what the roundings allow; 32768 tokens,
+// 16/4 heads, window 4096 backward 4.55 -> 4.60 ms by it, 8192 x 32 of 64 428 -> 434 us). dV and dK
+// sum over queries, so P and dS are bf16 there, and q's rows are rounded to bf16 on their way from
+// LDS. (With bf16 copies of q, k and v for every gradient product the gradients were 1.85 times as far
 // from 64 bits as their last rounding alone, now 1.45, like those of bf16 inputs.)
 //
 // Work is laid over the packed rows, not over the sequences: a workgroup owns consecutive

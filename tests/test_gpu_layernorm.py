@@ -9,6 +9,8 @@ step more (bf16 2^-8, fp16 2^-11). dx is a difference: r (t - mean t - xh mean(t
 term rounded by 2^-24 of its size, however much of them cancels (of two values all but
 eps / variance does: xh = +-1 and t lies in the span of the two terms taken off), so its fp32
 error is measured against the size of r t where that is larger than dx itself."""
+import math
+
 import pytest
 import torch
 
@@ -321,3 +323,24 @@ def test_more_long_rows_than_a_launch_holds():
     assert bool((rstd > 0).all())
     del x
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("d", [3, 300, 70001, 1 << 20])
+def test_infinite_values_stay_in_their_row(d):
+    """Rows with an infinite value have an infinite mean, whatever holds them, and a NaN output; both
+    signs, or a NaN, a NaN mean. Their neighbours are what they were."""
+    banner(f"layernorm infinite values d={d}")
+    g = torch.Generator(device=DEV)
+    g.manual_seed(d)
+    T, gain, bias = 6, torch.ones(d, device=DEV), torch.zeros(d, device=DEV)
+    x, dy = rows(g, T, d, F32, d), rows(g, T, d, F32, d)
+    y, mean, rstd, dx, _, _ = run(T, d, x, gain, bias, dy, None, (F32,) * 6)
+    bad = x.clone()
+    bad[1, d // 2], bad[2, d - 1], bad[4, 0] = math.inf, -math.inf, math.nan
+    bad[5, 0], bad[5, d - 1] = math.inf, -math.inf
+    yb, mb, rb, dxb, _, _ = run(T, d, bad, gain, bias, dy, None, (F32,) * 6)
+    assert float(mb[1]) == math.inf and float(mb[2]) == -math.inf and bool(mb[4:].isnan().all())
+    assert bool(yb[[1, 2, 4, 5]].isnan().all())
+    keep = [0, 3]
+    assert torch.equal(yb[keep], y[keep]) and torch.equal(mb[keep], mean[keep])
+    assert torch.equal(rb[keep], rstd[keep]) and torch.equal(dxb[keep], dx[keep])
