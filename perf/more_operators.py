@@ -1,0 +1,558 @@
+"""8-bit matrix products with a power-of-two scale per block of 128, the
+quantisation that makes their operands, and a router's balance loss: the calls
+whose speed counts, their plain forms and their definitions in 64 bits.
+
+Each case is one pass through one operator of the library, as a training
+program calls it:
+
+  quantize  rows of x to 8 bits, a scale per block of 1 or 128 rows x 128
+            columns: as rows (`rows`), as columns with blocks along the tokens
+            (`cols`, a weight gradient's operand), or both; `groups` > 0: the
+            rows of a mixture's experts, gathered by token, weighted, each
+            expert's tokens in blocks of its own
+  product   C = A B^T of quantised operands; `rows`: groups of rows with a B of
+            their own (the experts' forward and input gradients); `k`: groups
+            along k with a C of their own (the experts' weight gradients)
+  balance   a top-2 router's balance and z losses and per-expert counts;
+            `train`: then the gradients of the router's input and weights
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False  # True: run() makes the library's calls; False: the plain forms
+
+DEV = "cuda"
+DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16,
+          "e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+SIZE = {"fp32": 4, "bf16": 2, "fp16": 2}
+BLOCK = 128
+# a block's largest value is at most LARGEST 2^k: fraction and exponent of 448 and 57344
+LARGEST = {"e4m3": (0.875, 9), "e5m2": (0.875, 16)}
+COEF, Z_COEF = 0.01, 0.001
+
+
+def _quantize(name, tokens, d, x, q, layout, block, groups=0, source=0, split=0):
+    c = {"op": "quantize", "tokens": tokens, "d": d, "x": x, "q": q, "layout": layout, "block": block,
+         "groups": groups, "source": source, "split": split}
+    return {"name": name, **c} if name else c
+
+
+def _product(name, mode, m, n, k, a, b, c_type, a_block, b_block, groups=0, tail=0, split=0):
+    c = {"op": "product", "mode": mode, "m": m, "n": n, "k": k, "a": a, "b": b, "c": c_type,
+         "a_block": a_block, "b_block": b_block, "groups": groups, "tail": tail, "split": split}
+    return {"name": name, **c} if name else c
+
+
+def _balance(name, direction, tokens, d, experts, n, w, dn, masked):
+    c = {"op": "balance", "pass": direction, "tokens": tokens, "d": d, "experts": experts, "n": n,
+         "w": w, "dn": dn, "masked": masked}
+    return {"name": name, **c} if name else c
+
+
+def listed():
+    return [
+        # a few tokens before a small product: the call's latency
+        _quantize("quantize_t5_d2048", 5, 2048, "bf16", "e4m3", "rows", 1),
+        # a 7B-shaped layer's activations: the forward's operand and the weight gradient's
+        _quantize("quantize_both_t4096_d4096", 4096, 4096, "bf16", "e4m3", "both", 1),
+        # a weight matrix after the optimizer's step, for the forward and the input gradient
+        _quantize("quantize_weight_11008x4096", 11008, 4096, "bf16", "e4m3", "both", BLOCK),
+        # the gradient at eight experts' outputs: tokens' rows gathered and weighted by the gate
+        _quantize("quantize_experts_t8187_d2048", 8187, 2048, "bf16", "e5m2", "both", 1, 8, 4096, 3),
+        # one token through a projection
+        _product("product_t1_n4096_k4096", "none", 1, 4096, 4096, "e4m3", "e4m3", "bf16", 1, BLOCK),
+        # a 7B-shaped layer's microbatch through a gate or up projection
+        _product("product_t4096_n11008_k4096", "none", 4096, 11008, 4096, "e4m3", "e4m3", "bf16", 1, BLOCK),
+        # an input gradient of odd sizes, added up and kept in fp32
+        _product("product_t3001_n1155_k1872", "none", 3001, 1155, 1872, "e5m2", "e4m3", "fp32", 1, BLOCK),
+        # eight experts' gate and up projections over their tokens, and rows of no expert behind
+        _product("product_experts_t8187", "rows", 8187, 2816, 2048, "e4m3", "e4m3", "bf16", 1, BLOCK, 8, 5, 5),
+        # the same experts' weight gradients
+        _product("product_experts_grad_t8187", "k", 2816, 2048, 8187, "e5m2", "e4m3", "bf16", 1, 1, 8, 0, 7),
+        # a few tokens through a small router: the call's latency
+        _balance("balance_t9_e8", "forward", 9, 512, 8, "bf16", "bf16", "fp32", False),
+        # a mixture's microbatch, forward and backward
+        _balance("balance_train_t4096_e8", "train", 4096, 2048, 8, "bf16", "bf16", "fp32", False),
+        # a long padded microbatch, many experts
+        _balance("balance_train_t16411_e64", "train", 16411, 4096, 64, "bf16", "bf16", "bf16", True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return round(math.exp(rng.uniform(math.log(lo), math.log(hi))))
+
+
+def draw(rng):
+    op = rng.choice(["quantize", "product", "product", "balance"])
+    key = "flops" if op == "product" else "bytes"
+    top = max(work(c)[key] for c in listed() if c["op"] == op)
+    while True:
+        if op == "quantize":
+            d = _log(rng, 64, 12288)
+            d = 8 * max(8, round(d / 8)) if rng.random() < 0.7 else d
+            tokens, groups = _log(rng, 1, 32768), rng.choice([0, 0, rng.randint(1, 64)])
+            c = _quantize("", tokens, d, rng.choice(["fp32", "bf16", "fp16"]), rng.choice(["e4m3", "e5m2"]),
+                          "both" if groups else rng.choice(["rows", "cols", "both"]),
+                          1 if groups else rng.choice([1, 1, BLOCK]), groups,
+                          (tokens + 1) // 2 if groups else 0, rng.randint(1, 1 << 20))
+        elif op == "product":
+            mode = rng.choice(["none", "none", "rows", "k"])
+            m, n, k = _log(rng, 1, 16384), _log(rng, 16, 16384), 16 * _log(rng, 4, 1024)
+            groups = 0 if mode == "none" else rng.randint(1, 32)
+            if mode == "k":
+                m, k = _log(rng, 16, 4096), _log(rng, 16, 16384)
+            c = _product("", mode, m, n, k, rng.choice(["e4m3", "e4m3", "e5m2"]),
+                         rng.choice(["e4m3", "e4m3", "e5m2"]), rng.choice(["bf16", "bf16", "fp16", "fp32"]),
+                         1, 1 if mode == "k" else rng.choice([1, BLOCK, BLOCK]), groups,
+                         rng.choice([0, rng.randint(1, 40)]) if mode == "rows" else 0, rng.randint(1, 1 << 20))
+            # (what the plain form holds in 32 and 64 bits is bounded too)
+            if max(1, groups) * n * (m if mode == "k" else k) > 2e8:
+                continue
+        else:
+            c = _balance("", rng.choice(["forward", "train", "train"]), _log(rng, 1, 32768),
+                         8 * _log(rng, 8, 1024), rng.randint(2, 64), rng.choice(["bf16", "bf16", "fp16", "fp32"]),
+                         rng.choice(["bf16", "fp32"]), rng.choice(["fp32", "bf16"]), rng.random() < 0.5)
+        if work(c)[key] <= top:
+            return c
+
+
+# ------------------------------------------------------------------ sizes
+
+def _up(n, to):
+    return -(-n // to) * to
+
+
+def _lengths(c, total):
+    """Rows of each group: `total` cut at random places, some groups empty."""
+    cuts = sorted(random.Random(c["split"]).randint(0, total) for _ in range(c["groups"] - 1))
+    return [b - a for a, b in zip([0] + cuts, cuts + [total])]
+
+
+def _ld_scale(k):
+    """Scale bytes of a row of k values, in whole words."""
+    return _up(-(-k // BLOCK), 4)
+
+
+def _columns(c):
+    """Columns of the column layout: each group's tokens up to a multiple of the block."""
+    rows, groups = (c["k"] if c["op"] == "product" else c["tokens"]), max(1, c["groups"])
+    return BLOCK * ((rows + (BLOCK - 1) * groups) // BLOCK)
+
+
+def work(case):
+    c = case
+    if c["op"] == "quantize":
+        n = c["tokens"] * c["d"]
+        layouts = 2 if c["layout"] == "both" else 1
+        source = n if not c["groups"] else min(c["source"], c["tokens"]) * c["d"]
+        scales = n // (BLOCK * c["block"])
+        return {"bytes": source * SIZE[c["x"]] + layouts * (n + scales) + (8 * c["tokens"] if c["groups"] else 0),
+                "flops": 4 * n}
+    if c["op"] == "product":
+        m, n, k = c["m"], c["n"], c["k"]
+        g = max(1, c["groups"])
+        gb, gc = (g if c["mode"] == "rows" else 1), (g if c["mode"] == "k" else 1)
+        blocks = m * k // (BLOCK * c["a_block"]) + gb * n * k // (BLOCK * c["b_block"])
+        return {"bytes": m * k + gb * n * k + blocks + gc * m * n * SIZE[c["c"]], "flops": 2 * m * n * k}
+    T, d, E = c["tokens"], c["d"], c["experts"]
+    b = T * d * SIZE[c["n"]] + E * d * SIZE[c["w"]] + 8 * T + 4 * T * E + 4 * T
+    f = 2 * T * E * d
+    if c["pass"] == "train":  # n, the weights, p, lse, sel, w, dw, dres in, dn and dWr out
+        b += T * d * (SIZE[c["n"]] + 2 * SIZE[c["dn"]]) + E * d * (SIZE[c["w"]] + 4) + 4 * T * E + 28 * T
+        f += 4 * T * E * d
+    return {"bytes": b, "flops": f}
+
+
+# ------------------------------------------------------------------ inputs
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, shape, std=1.0):
+    return torch.randn(shape, generator=g, device=DEV).mul_(std)
+
+
+def _zeros(shape, dtype):
+    return torch.zeros(shape, dtype=dtype, device=DEV)
+
+
+def _offsets(lengths):
+    return torch.tensor([0] + lengths, device=DEV).cumsum(0).to(torch.int32)
+
+
+def _pow2(byte):
+    """2^(byte - 127) in 64 bits, from its bits: a power function may be an ulp off."""
+    return ((byte.to(torch.int64) + 896) << 52).view(torch.float64)
+
+
+def _blocks(x, q, rows):
+    """x [r, k] in blocks of `rows` x 128: bytes of the scales [ceil(r / rows), ceil(k / 128)] and
+    the 8-bit values [r, k]."""
+    r, k = x.shape
+    y = torch.nn.functional.pad(x.float(), (0, -k % BLOCK, 0, -r % rows))
+    y = y.view(-1, rows, y.shape[1] // BLOCK, BLOCK)
+    fraction, exponent = torch.frexp(y.abs().amax((1, 3)))
+    top, shift = LARGEST[q]
+    scale = (exponent - shift + 127 + (fraction > top)).clamp(min=0)
+    up = ((254 - scale) << 23).to(torch.int32).view(torch.float32)  # 2^(127 - scale)
+    y = (y * up[:, None, :, None]).to(DTYPES[q])
+    return scale.to(torch.uint8), y.view(-1, y.shape[2] * BLOCK)[:r, :k]
+
+
+def _operand(x, q, block):
+    """An operand of the product as a program holds it: values, scales in rows of whole words."""
+    scale, y = _blocks(x, q, block)
+    s = _zeros((scale.shape[0], _ld_scale(x.shape[1])), torch.uint8)
+    s[:, :scale.shape[1]] = scale
+    return y.contiguous(), s
+
+
+def _padded(lengths):
+    """For each row of the groups one after the other: its column in the column layout."""
+    at, start, n = [], 0, 0
+    for k in lengths:
+        at.append(torch.arange(k, device=DEV) + start)
+        start, n = start + _up(k, BLOCK), n + k
+    return torch.cat(at)
+
+
+def prepare(case, seed):
+    """The operator's inputs, and the output buffers that the program keeps."""
+    c, g, s = case, _gen(seed), {"case": case}
+    if c["op"] == "quantize":
+        T, d = c["tokens"], c["d"]
+        rows = c["source"] or T
+        x = _randn(g, (rows, d)) * torch.exp(_randn(g, d, 0.5))  # channels of unequal size
+        if c["q"] == "e5m2":
+            x *= torch.exp(_randn(g, (rows, 1))) * 1e-4  # gradients: tokens of unequal weight
+        s["x"] = x.to(DTYPES[c["x"]])
+        if c["groups"]:
+            s["offsets"] = _offsets(_lengths(c, T))
+            s["index"] = torch.randint(0, rows, (T,), generator=g, device=DEV, dtype=torch.int32)
+            s["weight"] = torch.rand(T, generator=g, device=DEV)
+        if c["layout"] != "cols":
+            s["q"] = _zeros((T, _up(d, 16)), torch.uint8)
+            s["scale"] = _zeros((-(-T // c["block"]), _ld_scale(d)), torch.uint8)
+        if c["layout"] != "rows":
+            s["qt"] = _zeros((d, _columns(c)), torch.uint8)
+            s["scale_t"] = _zeros((-(-d // c["block"]), _ld_scale(_columns(c))), torch.uint8)
+    elif c["op"] == "product":
+        m, n, k, G = c["m"], c["n"], c["k"], max(1, c["groups"])
+        if c["mode"] == "k":  # k: tokens, each group's from a multiple of the block on
+            lengths = _lengths(c, k)
+            s["offsets"], at, k = _offsets(lengths), _padded(lengths), _columns(c)
+            full = [_zeros((r, k), torch.float32) for r in (m, n)]
+            full[0][:, at] = _randn(g, (m, len(at)), 1e-4)
+            full[1][:, at] = _randn(g, (n, len(at)))
+            a, b = full
+        else:
+            a = _randn(g, (m + c["tail"], k)) * torch.exp(_randn(g, k, 0.5))
+            b = _randn(g, (n * (G if c["mode"] == "rows" else 1), k), 0.02)
+            if c["mode"] == "rows":
+                s["offsets"] = _offsets(_lengths(c, m))
+        s["A"], s["a_scale"] = _operand(a, c["a"], c["a_block"])
+        if c["mode"] == "rows":  # each group's matrix by itself: its last block of rows may be short
+            parts = [_operand(t, c["b"], c["b_block"]) for t in b.view(G, n, k)]
+            s["B"], s["b_scale"] = torch.cat([p[0].view(torch.uint8) for p in parts]).view(DTYPES[c["b"]]), \
+                torch.cat([p[1] for p in parts])
+        else:
+            s["B"], s["b_scale"] = _operand(b, c["b"], c["b_block"])
+        s["C"] = _zeros((G, m, n) if c["mode"] == "k" else (m + c["tail"], n), DTYPES[c["c"]])
+        s["K"] = k
+    else:
+        T, d, E = c["tokens"], c["d"], c["experts"]
+        s["n"] = _randn(g, (T, d)).to(DTYPES[c["n"]])
+        s["wr"] = _randn(g, (E, d), 0.02).to(DTYPES[c["w"]])
+        logits = s["n"].float() @ s["wr"].float().T
+        top = torch.topk(logits, 2, dim=1)
+        s["sel"] = top.indices.to(torch.int32).contiguous()
+        s["mask"] = (torch.arange(T, device=DEV) < T - T // 9).to(torch.uint8) if c["masked"] else None
+        s["p"], s["lse"] = _zeros((T, E), torch.float32), _zeros(T, torch.float32)
+        s["counts"], s["loss"] = _zeros(E + 1, torch.int32), _zeros(2, torch.float32)
+        if c["pass"] == "train":
+            s["w"] = torch.softmax(top.values, 1).contiguous()
+            s["dw"] = _randn(g, (T, 2), 1e-3)
+            s["dres"] = _randn(g, (T, d), 1e-3).to(DTYPES[c["dn"]])
+            s["dn"], s["dwr"] = torch.empty_like(s["dres"]), _zeros((E, d), torch.float32)
+    return s
+
+
+# ------------------------------------------------------------------ the pass
+
+def run(state):
+    op = state["case"]["op"]
+    if own:
+        return {"quantize": _quantize_own, "product": _product_own, "balance": _balance_own}[op](state)
+    return {"quantize": _quantize_plain, "product": _product_plain, "balance": _balance_plain}[op](state)
+
+
+def _codes(lc):
+    return {"fp32": lc.LC_FP32, "bf16": lc.LC_BF16, "fp16": lc.LC_FP16, "e4m3": lc.LC_FP8_E4M3,
+            "e5m2": lc.LC_FP8_E5M2}
+
+
+def _quantize_own(s):
+    from paper_2606_11169_amd import libchunk as lc
+    c, code = s["case"], _codes(lc)
+    ld = {k: s[k].stride(0) if k in s else 0 for k in ("q", "scale", "qt", "scale_t")}
+    lc.lc_fp8_quantize(c["tokens"], c["d"], s["x"], code[c["x"]], code[c["q"]], q=s.get("q"), ld_q=ld["q"],
+                       scale=s.get("scale"), ld_scale=ld["scale"], qt=s.get("qt"), ld_qt=ld["qt"],
+                       scale_t=s.get("scale_t"), ld_scale_t=ld["scale_t"], block_rows=c["block"],
+                       row_index=s.get("index"), x_rows=c["source"], row_weight=s.get("weight"),
+                       group_offsets=s.get("offsets"), n_groups=c["groups"],
+                       stream=torch.cuda.current_stream())
+    return _quantized(s, s.get("q"), s.get("scale"), s.get("qt"), s.get("scale_t"))
+
+
+def _quantized(s, q, scale, qt, scale_t):
+    view = lambda t: t.view(DTYPES[s["case"]["q"]])  # noqa: E731
+    out = {} if q is None else {"q": view(q), "scale": scale}
+    return out if qt is None else {**out, "qt": view(qt), "scale_t": scale_t}
+
+
+def _product_own(s):
+    from paper_2606_11169_amd import libchunk as lc
+    c, code = s["case"], _codes(lc)
+    mode = {"none": lc.LC_GROUP_NONE, "rows": lc.LC_GROUP_ROWS, "k": lc.LC_GROUP_K}[c["mode"]]
+    n, K, lds = c["n"], s["K"], s["b_scale"].stride(0)
+    lc.lc_gemm_fp8(lc.LC_EPI_STORE, c["m"] + c["tail"], n, K, s["A"], K, s["a_scale"], s["a_scale"].stride(0),
+                   s["B"], K, s["b_scale"], lds, s["C"], n, a_dtype=code[c["a"]], b_dtype=code[c["b"]],
+                   c_dtype=code[c["c"]], a_block_rows=c["a_block"], b_block_rows=c["b_block"],
+                   group_mode=mode, n_groups=c["groups"], group_offsets=s.get("offsets"),
+                   group_stride_b=n * K if c["mode"] == "rows" else 0,
+                   group_stride_b_scale=-(-n // c["b_block"]) * lds if c["mode"] == "rows" else 0,
+                   group_stride_c=c["m"] * n if c["mode"] == "k" else 0, stream=torch.cuda.current_stream())
+    return {"C": s["C"]}
+
+
+def _balance_own(s):
+    from paper_2606_11169_amd import libchunk as lc
+    c, code, st = s["case"], _codes(lc), torch.cuda.current_stream()
+    T, d, E = c["tokens"], c["d"], c["experts"]
+    if "scratch" not in s:  # the workspace that the program keeps
+        s["scratch_bytes"] = lc.lc_moe_balance_scratch_bytes(T, d, E)
+        s["scratch"] = torch.empty(max(1, s["scratch_bytes"]), dtype=torch.uint8, device=DEV)
+    lc.lc_moe_balance_forward(T, d, E, s["n"], s["wr"], s["sel"], s["p"], s["lse"], s["counts"], s["loss"],
+                              s["scratch"], s["scratch_bytes"], code[c["n"]], code[c["w"]], mask=s["mask"],
+                              stream=st)
+    out = {k: s[k] for k in ("p", "lse", "counts", "loss")}
+    if c["pass"] == "train":
+        lc.lc_moe_balance_backward(T, d, E, s["n"], s["wr"], s["sel"], s["p"], s["lse"], s["counts"], COEF,
+                                   Z_COEF, s["dn"], s["dwr"], s["scratch"], s["scratch_bytes"], code[c["n"]],
+                                   code[c["w"]], code[c["dn"]], dres=s["dres"], dres_dtype=code[c["dn"]],
+                                   w=s["w"], dw=s["dw"], mask=s["mask"], store_dwr=1, stream=st)
+        out |= {"dn": s["dn"], "dwr": s["dwr"]}
+    return out
+
+
+# ------------------------------------------------------------------ plain forms
+
+def _group_of(offsets, n):
+    """Group of each of n rows (the number of groups for rows behind the last)."""
+    return torch.searchsorted(offsets[1:].contiguous(), torch.arange(n, device=DEV, dtype=torch.int32), right=True)
+
+
+def _starts(offsets):
+    """Each group's first column in the column layout."""
+    length = (offsets[1:] - offsets[:-1]).long()
+    padded = (length + BLOCK - 1) // BLOCK * BLOCK
+    return padded.cumsum(0) - padded
+
+
+def _quantize_plain(s):
+    c = s["case"]
+    T, d = c["tokens"], c["d"]
+    x = s["x"].float()
+    if c["groups"]:
+        x = x[s["index"].long()] * s["weight"][:, None]
+    q = scale = qt = scale_t = None
+    if c["layout"] != "cols":
+        q, scale = torch.zeros_like(s["q"]), torch.zeros_like(s["scale"])
+        byte, y = _blocks(x, c["q"], c["block"])
+        q[:, :d], scale[:, :byte.shape[1]] = y.view(torch.uint8), byte
+    if c["layout"] != "rows":
+        if c["groups"]:
+            off = s["offsets"]
+            group = _group_of(off, T)
+            full = _zeros((_columns(c), d), torch.float32)
+            full[_starts(off)[group] + torch.arange(T, device=DEV) - off[group].long()] = x
+            used = int(((off[1:] - off[:-1] + BLOCK - 1) // BLOCK).sum())
+        else:
+            full, used = torch.nn.functional.pad(x, (0, 0, 0, _columns(c) - T)), -(-T // BLOCK)
+        scale_t = torch.zeros_like(s["scale_t"])
+        byte, y = _blocks(full.T.contiguous(), c["q"], c["block"])
+        qt, scale_t[:, :used] = y.contiguous().view(torch.uint8), byte[:, :used]
+    return _quantized(s, q, scale, qt, scale_t)
+
+
+def _values(q, scale, block):
+    """The numbers that an operand stands for, in 32 bits."""
+    r, k = q.shape
+    f = _pow2(scale[:, :-(-k // BLOCK)]).float()
+    return q.float() * f.repeat_interleave(block, 0)[:r].repeat_interleave(BLOCK, 1)[:, :k]
+
+
+def _product_plain(s):
+    c = s["case"]
+    m, n, G, K = c["m"], c["n"], c["groups"], s["K"]
+    a = _values(s["A"], s["a_scale"], c["a_block"])
+    if c["mode"] == "none":
+        return {"C": (a @ _values(s["B"], s["b_scale"], c["b_block"]).T).to(s["C"].dtype)}
+    off = s["offsets"].long()
+    length = off[1:] - off[:-1]
+    most = max(1, int(length.max()))
+    at = torch.arange(most, device=DEV)
+    inside = at < length[:, None]
+    if c["mode"] == "rows":
+        f = _pow2(s["b_scale"].view(G, -(-n // c["b_block"]), -1)[:, :, :-(-K // BLOCK)]).float()
+        f = f.repeat_interleave(c["b_block"], 1)[:, :n].repeat_interleave(BLOCK, 2)[:, :, :K]
+        b = s["B"].float().view(G, n, K) * f
+        rows = torch.where(inside, off[:-1, None] + at, 0)
+        y = torch.bmm(a[rows], b.transpose(1, 2).contiguous())
+        out = torch.zeros_like(s["C"])
+        out[:m] = y[inside].to(out.dtype)
+        return {"C": out}
+    b = _values(s["B"], s["b_scale"], c["b_block"])
+    cols = torch.where(inside, _starts(s["offsets"])[:, None] + at, 0)
+    left = a.T[cols] * inside[:, :, None]  # [G, most, m]
+    return {"C": torch.bmm(left.transpose(1, 2).contiguous(), b.T[cols]).to(s["C"].dtype)}
+
+
+def _balance_plain(s):
+    c = s["case"]
+    T, E = c["tokens"], c["experts"]
+    n, wr = s["n"].float(), s["wr"].float()
+    keep = s["mask"] != 0 if s["mask"] is not None else torch.ones(T, dtype=torch.bool, device=DEV)
+    k = keep.float()[:, None]
+    N = max(1, int(keep.sum()))
+    l = n @ wr.T
+    top = l.amax(1, keepdim=True)
+    e = torch.exp(l - top)
+    z = e.sum(1, keepdim=True)
+    p, lse = e / z * k, (top + torch.log(z)) * k
+    pair = (s["sel"].long()[:, :, None] == torch.arange(E, device=DEV)) & keep[:, None, None]
+    count = pair.sum((0, 1))
+    f = count.float() / (2 * N)
+    loss = torch.stack([E * (f * (p.double().sum(0) / N)).sum(), (lse.double() ** 2).sum() / N]).float()
+    out = {"p": p, "lse": lse[:, 0], "counts": torch.cat([count, keep.sum()[None]]).to(torch.int32), "loss": loss}
+    if c["pass"] == "train":
+        dl = COEF * E / N * p * (f - (p * f).sum(1, keepdim=True)) + Z_COEF * 2 / N * lse * p
+        gate = s["w"] * (s["dw"] - (s["w"] * s["dw"]).sum(1, keepdim=True))
+        dl = dl + (pair * gate[:, :, None]).sum(1)
+        out["dn"] = (s["dres"].float() + dl @ wr).to(s["dn"].dtype)
+        out["dwr"] = dl.T @ n
+    return out
+
+
+# ------------------------------------------------------------------ definitions, in 64 bits
+
+def exact(case, seed):
+    s, c = prepare(case, seed), case
+    return {"quantize": _quantize_exact, "product": _product_exact, "balance": _balance_exact}[c["op"]](s, c)
+
+
+def _nearest(x, q):
+    """Blocks x [..., 128 values or more]: scale bytes and values rounded to the 8-bit type, ties to even."""
+    largest, low, bits = (448.0, -6, 3) if q == "e4m3" else (57344.0, -14, 2)
+    a = x.abs().flatten(1).amax(1)
+    k = torch.ceil(torch.log2(a.clamp(min=1e-300) / largest))
+    k = torch.where(a > largest * _pow2(k + 127), k + 1, k)
+    k = torch.where(a <= largest * _pow2(k + 126), k - 1, k).clamp(min=-127)
+    y = x / _pow2(k + 127).view(-1, *[1] * (x.dim() - 1))
+    e = torch.floor(torch.log2(y.abs().clamp(min=1e-300)))
+    e = torch.where(y.abs() < _pow2(e + 127), e - 1, e)
+    e = torch.where(y.abs() >= _pow2(e + 128), e + 1, e).clamp(min=low)
+    step = _pow2(e - bits + 127)
+    return (k + 127).long(), torch.round(y / step) * step
+
+
+def _quantize_exact(s, c):
+    T, d, block = c["tokens"], c["d"], c["block"]
+    x = s["x"].double()
+    if c["groups"]:  # the weighted row is a 32-bit number
+        x = (s["x"].float()[s["index"].long()] * s["weight"][:, None]).double()
+    out = {}
+
+    def layout(y, name):  # y [r, k]: its values, a strip of blocks at a time
+        r, k = y.shape
+        v = _zeros(s[name].shape, torch.float64)
+        for r0 in range(0, r, 2048):
+            part = y[r0:r0 + 2048]
+            h = part.shape[0]
+            part = torch.nn.functional.pad(part, (0, -k % BLOCK, 0, -h % block))
+            b = part.view(-1, block, part.shape[1] // BLOCK, BLOCK).transpose(1, 2)
+            _, w = _nearest(b.reshape(-1, block, BLOCK), c["q"])
+            w = w.view(b.shape).transpose(1, 2).reshape(part.shape)
+            v[r0:r0 + h, :k] = w[:h, :k]
+        out[name] = v
+
+    if c["layout"] != "cols":
+        layout(x, "q")
+        out["scale"] = None
+    if c["layout"] != "rows":
+        wide = _zeros((d, _columns(c)), torch.float64)
+        at = _padded(_lengths(c, T)) if c["groups"] else torch.arange(T, device=DEV)
+        wide[:, at] = x.T
+        layout(wide, "qt")
+        out["scale_t"] = None
+    return out
+
+
+def _product_exact(s, c):
+    m, n, K = c["m"], c["n"], s["K"]
+
+    def number(q, scale, block):
+        r = torch.arange(q.shape[0], device=DEV) // block
+        k = torch.arange(q.shape[1], device=DEV) // BLOCK
+        return q.double() * _pow2(scale[r][:, k])
+
+    a = number(s["A"], s["a_scale"], c["a_block"])
+    out = _zeros(s["C"].shape, torch.float64)
+    if c["mode"] == "none":
+        out[:] = a @ number(s["B"], s["b_scale"], c["b_block"]).T
+    elif c["mode"] == "rows":
+        begin, per = 0, -(-n // c["b_block"])
+        for g, length in enumerate(_lengths(c, m)):
+            b = number(s["B"][g * n:(g + 1) * n], s["b_scale"][g * per:(g + 1) * per], c["b_block"])
+            out[begin:begin + length] = a[begin:begin + length] @ b.T
+            begin += length
+    else:
+        b, begin = number(s["B"], s["b_scale"], c["b_block"]), 0
+        for g, length in enumerate(_lengths(c, c["k"])):
+            out[g] = a[:, begin:begin + length] @ b[:, begin:begin + length].T
+            begin += _up(length, BLOCK)
+    return {"C": out}
+
+
+def _balance_exact(s, c):
+    T, E = c["tokens"], c["experts"]
+    live = torch.nonzero(s["mask"])[:, 0] if s["mask"] is not None else torch.arange(T, device=DEV)
+    N = max(1, len(live))
+    n, wr = s["n"].double(), s["wr"].double()
+    l = torch.einsum("td,ed->te", n[live], wr)
+    L = torch.logsumexp(l, 1)
+    p = torch.exp(l - L[:, None])
+    sel = s["sel"][live].long()
+    f = torch.bincount(sel.flatten(), minlength=E).double() / (2 * N)
+    mean = p.sum(0) / N
+    p_all, lse = _zeros((T, E), torch.float64), _zeros(T, torch.float64)
+    p_all[live], lse[live] = p, L
+    out = {"p": p_all, "lse": lse, "counts": None,
+           "loss": torch.stack([E * torch.dot(f, mean), torch.dot(L, L) / N])}
+    if c["pass"] == "train":
+        # through the softmax's own derivative: dp, then dl = p (dp - p . dp)
+        dp = (COEF * E / N * f).expand(len(live), E)
+        dl = p * (dp - (p * dp).sum(1, keepdim=True)) + p * (2 * Z_COEF / N * L)[:, None]
+        w, dw = s["w"][live].double(), s["dw"][live].double()
+        dl.scatter_add_(1, sel, w * (dw - (w * dw).sum(1, keepdim=True)))
+        dn = s["dres"].double()
+        dn[live] += dl @ wr
+        out |= {"dn": dn, "dwr": dl.T @ n[live]}
+    return out
