@@ -132,9 +132,10 @@ def _lengths(c, total):
     return [b - a for a, b in zip([0] + cuts, cuts + [total])]
 
 
-def _ld_scale(k):
-    """Scale bytes of a row of k values, in whole words."""
-    return _up(-(-k // BLOCK), 4)
+def _scales(r, k, block):
+    """Shape of the scales of [r, k] values: a line per 128 of k, a byte per block of rows, whole
+    words."""
+    return -(-k // BLOCK), _up(-(-r // block), 4)
 
 
 def _columns(c):
@@ -193,7 +194,7 @@ def _pow2(byte):
 
 
 def _blocks(x, q, rows):
-    """x [r, k] in blocks of `rows` x 128: bytes of the scales [ceil(r / rows), ceil(k / 128)] and
+    """x [r, k] in blocks of `rows` x 128: bytes of the scales [ceil(k / 128), ceil(r / rows)] and
     the 8-bit values [r, k]."""
     r, k = x.shape
     y = torch.nn.functional.pad(x.float(), (0, -k % BLOCK, 0, -r % rows))
@@ -203,13 +204,13 @@ def _blocks(x, q, rows):
     scale = (exponent - shift + 127 + (fraction > top)).clamp(min=0)
     up = ((254 - scale) << 23).to(torch.int32).view(torch.float32)  # 2^(127 - scale)
     y = (y * up[:, None, :, None]).to(DTYPES[q])
-    return scale.to(torch.uint8), y.view(-1, y.shape[2] * BLOCK)[:r, :k]
+    return scale.to(torch.uint8).T, y.view(-1, y.shape[2] * BLOCK)[:r, :k]
 
 
 def _operand(x, q, block):
-    """An operand of the product as a program holds it: values, scales in rows of whole words."""
+    """An operand of the product as a program holds it: values, scales in lines of whole words."""
     scale, y = _blocks(x, q, block)
-    s = _zeros((scale.shape[0], _ld_scale(x.shape[1])), torch.uint8)
+    s = _zeros(_scales(*x.shape, block), torch.uint8)
     s[:, :scale.shape[1]] = scale
     return y.contiguous(), s
 
@@ -239,10 +240,10 @@ def prepare(case, seed):
             s["weight"] = torch.rand(T, generator=g, device=DEV)
         if c["layout"] != "cols":
             s["q"] = _zeros((T, _up(d, 16)), torch.uint8)
-            s["scale"] = _zeros((-(-T // c["block"]), _ld_scale(d)), torch.uint8)
+            s["scale"] = _zeros(_scales(T, d, c["block"]), torch.uint8)
         if c["layout"] != "rows":
             s["qt"] = _zeros((d, _columns(c)), torch.uint8)
-            s["scale_t"] = _zeros((-(-d // c["block"]), _ld_scale(_columns(c))), torch.uint8)
+            s["scale_t"] = _zeros(_scales(d, _columns(c), c["block"]), torch.uint8)
     elif c["op"] == "product":
         m, n, k, G = c["m"], c["n"], c["k"], max(1, c["groups"])
         if c["mode"] == "k":  # k: tokens, each group's from a multiple of the block on
@@ -327,7 +328,7 @@ def _product_own(s):
                    c_dtype=code[c["c"]], a_block_rows=c["a_block"], b_block_rows=c["b_block"],
                    group_mode=mode, n_groups=c["groups"], group_offsets=s.get("offsets"),
                    group_stride_b=n * K if c["mode"] == "rows" else 0,
-                   group_stride_b_scale=-(-n // c["b_block"]) * lds if c["mode"] == "rows" else 0,
+                   group_stride_b_scale=-(-K // BLOCK) * lds if c["mode"] == "rows" else 0,
                    group_stride_c=c["m"] * n if c["mode"] == "k" else 0, stream=torch.cuda.current_stream())
     return {"C": s["C"]}
 
@@ -388,14 +389,14 @@ def _quantize_plain(s):
             full, used = torch.nn.functional.pad(x, (0, 0, 0, _columns(c) - T)), -(-T // BLOCK)
         scale_t = torch.zeros_like(s["scale_t"])
         byte, y = _blocks(full.T.contiguous(), c["q"], c["block"])
-        qt, scale_t[:, :used] = y.contiguous().view(torch.uint8), byte[:, :used]
+        qt, scale_t[:used, :byte.shape[1]] = y.contiguous().view(torch.uint8), byte[:used]
     return _quantized(s, q, scale, qt, scale_t)
 
 
 def _values(q, scale, block):
     """The numbers that an operand stands for, in 32 bits."""
     r, k = q.shape
-    f = _pow2(scale[:, :-(-k // BLOCK)]).float()
+    f = _pow2(scale.T).float()
     return q.float() * f.repeat_interleave(block, 0)[:r].repeat_interleave(BLOCK, 1)[:, :k]
 
 
@@ -411,7 +412,7 @@ def _product_plain(s):
     at = torch.arange(most, device=DEV)
     inside = at < length[:, None]
     if c["mode"] == "rows":
-        f = _pow2(s["b_scale"].view(G, -(-n // c["b_block"]), -1)[:, :, :-(-K // BLOCK)]).float()
+        f = _pow2(s["b_scale"].view(G, -(-K // BLOCK), -1).transpose(1, 2)).float()
         f = f.repeat_interleave(c["b_block"], 1)[:, :n].repeat_interleave(BLOCK, 2)[:, :, :K]
         b = s["B"].float().view(G, n, K) * f
         rows = torch.where(inside, off[:-1, None] + at, 0)
@@ -511,14 +512,14 @@ def _product_exact(s, c):
     def number(q, scale, block):
         r = torch.arange(q.shape[0], device=DEV) // block
         k = torch.arange(q.shape[1], device=DEV) // BLOCK
-        return q.double() * _pow2(scale[r][:, k])
+        return q.double() * _pow2(scale[k][:, r].T)
 
     a = number(s["A"], s["a_scale"], c["a_block"])
     out = _zeros(s["C"].shape, torch.float64)
     if c["mode"] == "none":
         out[:] = a @ number(s["B"], s["b_scale"], c["b_block"]).T
     elif c["mode"] == "rows":
-        begin, per = 0, -(-n // c["b_block"])
+        begin, per = 0, -(-K // BLOCK)
         for g, length in enumerate(_lengths(c, m)):
             b = number(s["B"][g * n:(g + 1) * n], s["b_scale"][g * per:(g + 1) * per], c["b_block"])
             out[begin:begin + length] = a[begin:begin + length] @ b.T
