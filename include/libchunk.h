@@ -55,8 +55,12 @@ typedef enum lc_status {
 
 /* Element types. A stage's compute_dtype is LC_FP32 or LC_BF16; LC_FP16
  * appears only in the per-tensor types of libchunk_ops.h (a bf16 stage keeps
- * its attention q, k, v in fp16, see lc_stage_desc). */
-typedef enum lc_dtype { LC_FP32 = 0, LC_BF16 = 1, LC_FP16 = 2 } lc_dtype;
+ * its attention q, k, v in fp16, see lc_stage_desc), the 8-bit types (OCP
+ * e4m3, largest value 448, no infinities, and e5m2, largest 57344) only in
+ * its operations with block scales. */
+typedef enum lc_dtype {
+  LC_FP32 = 0, LC_BF16 = 1, LC_FP16 = 2, LC_FP8_E4M3 = 3, LC_FP8_E5M2 = 4
+} lc_dtype;
 
 /* Piper's PASS dimension (Section 4.1): F = forward, B = full backward,
  * BI = backward for the inputs (dX only), BW = backward for the weights (the

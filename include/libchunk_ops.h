@@ -116,6 +116,108 @@ typedef struct lc_gemm_args {
 
 lc_status lc_gemm(const lc_gemm_args *args, void *stream);
 
+/* ------------------------------------------------------------------ 8-bit values with block scales
+ * Quantises T rows of d values in blocks of block_rows (1 or 128) rows x 128
+ * columns, each with a scale that is a power of two, kept as one byte s:
+ *   a = the block's largest finite |x|,
+ *   s = the smallest integer in [0, 254] with a <= max * 2^(s - 127)
+ *       (max: 448 for e4m3, 57344 for e5m2; 0 where a is 0),
+ *   q = x * 2^(127 - s), rounded to nearest even,
+ * so x is about q * 2^(s - 127); the scaling is exact. A NaN stays NaN and an
+ * infinity an infinity (e5m2) or NaN (e4m3), in their own place: they take no
+ * part in their block's scale.
+ * Row layout (q, scale; NULL: not written): value (t, k) at q[t*ld_q + k], zeros
+ * from column d to the next multiple of 16; its scale at
+ * scale[(k/128)*ld_scale + t/block_rows].
+ * Column layout (qt, scale_t; NULL: not written), the operand of a product that
+ * sums over the rows: value (t, k) at qt[k*ld_qt + t], zeros from row T to the
+ * next multiple of 128. Blocks are then 128 rows x block_rows columns, scale at
+ * scale_t[(t/128)*ld_scale_t + k/block_rows].
+ * Groups (n_groups > 0: the rows of a mixture's experts; block_rows 1): group g is
+ * rows [off[g], off[g + 1]) of the device array group_offsets (n_groups + 1
+ * nondecreasing int32, clamped to [0, T]). In the column layout every group starts
+ * at a multiple of 128: row t of group g is column P(g) + t - off[g], P(g) the sum
+ * over the groups before g of their lengths, each up to a multiple of 128; zeros
+ * follow a group up to that multiple. Columns behind the last group, and their
+ * scales, are left as they were. The row layout holds all T rows, of groups or not.
+ * lc_fp8_padded_rows(T, n_groups) is the largest number of columns that any
+ * offsets need (n_groups 0: T up to a multiple of 128).
+ * row_index (device int32 [T], or NULL): row t of the result is made of row
+ * row_index[t] of x, which has x_rows rows; of zeros where that is outside
+ * [0, x_rows). Without it x has T rows. row_weight (device fp32 [T], or NULL):
+ * multiplies row t first (rounded to fp32).
+ * x_dtype LC_FP32, LC_BF16 or LC_FP16; q_dtype LC_FP8_E4M3 or LC_FP8_E5M2.
+ * ld_x 0 means d. ld_q and ld_qt are multiples of 16, ld_scale and ld_scale_t of 4,
+ * each at least what its rows take (columns of the column layout:
+ * lc_fp8_padded_rows). 0 <= T < 2^31 (0: nothing happens), 1 <= d <= 2^24,
+ * n_groups <= 64. No output may overlap a tensor that the call reads. */
+typedef struct lc_fp8_quantize_args {
+  int64_t T, d;
+  int32_t x_dtype, q_dtype;
+  int32_t block_rows;  /* 1 or 128 */
+  int32_t n_groups;    /* 0: no groups */
+  const void *x; int64_t ld_x;
+  const int32_t *row_index; int64_t x_rows; const float *row_weight;
+  const int32_t *group_offsets;
+  void *q; int64_t ld_q; uint8_t *scale; int64_t ld_scale;
+  void *qt; int64_t ld_qt; uint8_t *scale_t; int64_t ld_scale_t;
+} lc_fp8_quantize_args;
+
+lc_status lc_fp8_quantize(const lc_fp8_quantize_args *args, void *stream);
+int64_t lc_fp8_padded_rows(int64_t T, int32_t n_groups);
+
+/* The product of two such operands, both k-major:
+ *   C(m, n) = sum_b 2^(sa(m, b) + sb(n, b) - 254) sum_{k in block b} A(m, k) B(n, k)
+ * with A(m, k) = A[m*lda + k], blocks b of 128 k, sa(m, b) =
+ * a_scale[b*ld_a_scale + m/a_block_rows], likewise B and b_scale (a_block_rows and
+ * b_block_rows 1 or 128; a scale byte of 255 is NaN). a_dtype and b_dtype:
+ * LC_FP8_E4M3 or LC_FP8_E5M2. Then an epilogue as in lc_gemm: LC_EPI_STORE (c_dtype),
+ * LC_EPI_STORE_F32, LC_EPI_ACCUM_F32, LC_EPI_RESIDUAL (r_dtype, c_dtype).
+ * Sums: a C of 16 bits takes the 8-bit matrix instructions, which add each 8
+ * neighbouring products to about 14 bits below the largest of them and the sums of
+ * those in fp32: an error of about 1.5e-5 of the result on values of either sign, a
+ * hundredth of the result's own rounding. A C of fp32 takes the bf16 instructions on
+ * the same values (exact in bf16), whose sums are fp32, at half the rate. There a
+ * value times its scale below 2^-126 counts as 0 and from 2^128 on as infinite.
+ * Groups as in lc_gemm, 1 to 64:
+ *   LC_GROUP_ROWS  rows [off[g], off[g+1]) of A and C with B + g*group_stride_b and
+ *                  b_scale + g*group_stride_b_scale (a_block_rows 1); STORE,
+ *                  STORE_F32 or ACCUM_F32. Rows of no group are not written.
+ *   LC_GROUP_K     C + g*group_stride_c receives the sum over the columns of group g
+ *                  in the column layout of lc_fp8_quantize: columns P(g) to P(g) +
+ *                  its length of both operands, with group_offsets as given there;
+ *                  zeros follow up to the next multiple of 128. K: the columns of
+ *                  both operands (lc_fp8_padded_rows; what offsets reach past it
+ *                  is left out). An empty group's C is 0 (accumulated: as it was);
+ *                  STORE, STORE_F32 or ACCUM_F32.
+ * K, lda, ldb and group_stride_b are multiples of 16 (a row's values between its own
+ * length and K are zeros, as lc_fp8_quantize leaves them), ld_a_scale and ld_b_scale of
+ * 4. Any M >= 0 (0: nothing happens) and N >= 1, each below 2^30; K below 2^30, lda
+ * and ldb up to 2^22, ldc and ldr up to 2^30. Deterministic: a result depends on its
+ * operands, sizes and types only. C may lie over R, element for element (the same
+ * type and stride); no other output may overlap a tensor that the call reads. */
+typedef struct lc_gemm_fp8_args {
+  int32_t a_dtype, b_dtype;
+  int32_t epilogue;      /* lc_gemm_epilogue */
+  int32_t c_dtype;       /* C for STORE and RESIDUAL */
+  int32_t r_dtype;       /* R */
+  int32_t a_block_rows, b_block_rows;
+  int32_t reserved;
+  int64_t M, N, K;
+  const void *A; int64_t lda; const uint8_t *a_scale; int64_t ld_a_scale;
+  const void *B; int64_t ldb; const uint8_t *b_scale; int64_t ld_b_scale;
+  void *C; int64_t ldc;
+  const void *R; int64_t ldr;
+  int32_t group_mode;    /* lc_gemm_group */
+  int32_t n_groups;
+  const int32_t *group_offsets;
+  int64_t group_stride_b;        /* LC_GROUP_ROWS: values from B_g to B_(g+1) */
+  int64_t group_stride_b_scale;  /* LC_GROUP_ROWS: bytes from one group's scales to the next's */
+  int64_t group_stride_c;        /* LC_GROUP_K: elements from C_g to C_(g+1) */
+} lc_gemm_fp8_args;
+
+lc_status lc_gemm_fp8(const lc_gemm_fp8_args *args, void *stream);
+
 /* ------------------------------------------------------------------ RMSNorm
  * Forward over T rows of d:
  *   rstd[t] = 1/sqrt(mean_k x[t,k]^2 + eps)   (fp32)
@@ -442,6 +544,59 @@ typedef struct lc_moe_args {
 
 lc_status lc_moe_route(const lc_moe_args *args, void *stream);
 lc_status lc_moe_dispatch(const lc_moe_args *args, void *stream);
+
+/* ------------------------------------------------------------------ MoE balance
+ * What keeps a top-2 router's load even: counts of the pairs that each expert gets,
+ * the balance loss on them and the z loss on the logits' size, and the gradients of
+ * both through the router's product. n, wr, sel, T, d and E as in lc_moe_route (sel:
+ * its result, or any selection); token t counts where mask is NULL or mask[t] is not 0
+ * (device uint8 [T]), N tokens in all. Forward, with l[t, e] = sum_i n[t, i] wr[e, i]:
+ *   probs[t, e] = softmax(l[t])[e], lse[t] = log sum_e exp(l[t, e])   (fp32 [T, E], [T];
+ *                 0 for a token that does not count)
+ *   counts[e]   = pairs (t, k) with sel[t, k] = e, counts[E] = N      (int32 [E + 1]; a
+ *                 pair that lc_moe_dispatch does not place is not counted)
+ *   loss[0]     = E * sum_e f_e P_e, f_e = counts[e] / (2N), P_e = sum_t probs[t, e] / N
+ *   loss[1]     = sum_t lse[t]^2 / N                                  (fp32; 0 where N is 0)
+ * Backward, given probs, lse and counts: the gradient of coef * loss[0] + z_coef *
+ * loss[1] (f_e a constant), and, where w and dw are given (fp32 [T, 2]: lc_moe_route's
+ * weights and the gradient at them), that of the pair's weights:
+ *   dl[t, e] = coef E / N probs[t, e] (f_e - sum_e' f_e' probs[t, e'])
+ *            + 2 z_coef / N lse[t] probs[t, e]
+ *            + (e = sel[t, k]: w[t, k] (dw[t, k] - sum_j w[t, j] dw[t, j]))
+ *   dn[t]    = dres[t] + sum_e dl[t, e] wr[e]        (dres may be NULL: 0)
+ *   dwr_accum[e] += sum_t dl[t, e] n[t]              (fp32 [E, d]; stored if store_dwr is
+ *                                                     1, and where N is 0 it is 0 or stays)
+ * A token that does not count has dl = 0, whatever its values: what it holds reaches
+ * no result, infinities and NaN included. A pair that is not placed carries no gradient
+ * (a pair whose partner is not placed: with the partner's w and dw taken as 0).
+ * Sums are fp32 and of fixed order (partial sums in `scratch`,
+ * lc_moe_balance_scratch_bytes, no clearing needed). dn and dwr_accum may each be NULL.
+ * n_dtype, w_dtype (wr), dn_dtype and dres_dtype: LC_FP32, LC_BF16 or LC_FP16. d a
+ * multiple of 8; 0 <= T < 2^30 (0: counts, loss and a stored dwr_accum are 0). Overlap:
+ * dn may lie over dres, element for element (the same type); no other output may
+ * overlap a tensor that the call reads. */
+typedef struct lc_moe_balance_args {
+  int64_t T;
+  int32_t d, E;
+  int32_t n_dtype, w_dtype;
+  int32_t dn_dtype, dres_dtype;
+  float coef, z_coef;
+  int32_t store_dwr;
+  int32_t reserved;
+  const void *n;          /* [T, d] */
+  const void *wr;         /* [E, d] */
+  const int32_t *sel;     /* [T, 2] */
+  const uint8_t *mask;    /* [T] or NULL */
+  float *probs; float *lse; int32_t *counts; float *loss;
+  const float *w; const float *dw;  /* [T, 2], or both NULL */
+  const void *dres; void *dn;       /* [T, d] */
+  float *dwr_accum;
+  void *scratch; size_t scratch_bytes;
+} lc_moe_balance_args;
+
+lc_status lc_moe_balance_forward(const lc_moe_balance_args *args, void *stream);
+lc_status lc_moe_balance_backward(const lc_moe_balance_args *args, void *stream);
+size_t lc_moe_balance_scratch_bytes(int64_t T, int32_t d, int32_t E);
 
 /* ------------------------------------------------------------------ casts */
 

@@ -1,0 +1,244 @@
+// Products of 8-bit operands with a power-of-two scale per block of 128 (gfx950):
+//
+//   C(m, n) = sum_b 2^(sa(m, b) + sb(n, b) - 254) sum_{k in block b} A(m, k) B(n, k)
+//
+// Results of 16 bits are summed by v_mfma_scale_f32_16x16x128_f8f6f4, which takes the
+// scales as they are, one byte per row and 32 k. It adds each 8 neighbouring products
+// to about 14 bits below the largest of them (2^16 + 2^3 is exact, 2^16 + 1 is not),
+// 1.5e-5 of the result on random signs, where a 16-bit result rounds by 2e-3. Results
+// of fp32 are summed by v_mfma_f32_16x16x32_bf16 on the same values.
+#include "gemm_fp8.hpp"
+
+namespace lc {
+namespace {
+
+// Fragments straight from global memory: WM x WN x WK waves of MF x NF blocks of 16 x
+// 16; the WK waves of one place take the k blocks in turn and their sums are added in
+// LDS in order.
+template <int FA, int FB, bool F32, int MF, int NF, int WM, int WN, int WK>
+__global__ __launch_bounds__(64 * WM * WN * WK) void fp8_direct_kernel(Fp8P p, uint32_t first) {
+  constexpr int BM = 16 * MF * WM, BN = 16 * NF * WN;
+  Fp8Tile t;
+  if (!fp8_tile<BM, BN>(p, first + blockIdx.x, t)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i16 = lane & 15, g = lane >> 4;
+  const int wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN;
+
+  const uint8_t *pa[MF], *pb[NF];
+  int64_t oa[MF], ob[NF];  // scale bytes of the lane's rows in a line
+#pragma unroll
+  for (int i = 0; i < MF; ++i) {
+    const int64_t m = min(t.m0 + (wm * MF + i) * 16 + i16, t.m_lim - 1);  // (rows past the end: unused)
+    pa[i] = p.A + m * p.lda + 16 * g;
+    oa[i] = m >> p.ash;
+  }
+#pragma unroll
+  for (int j = 0; j < NF; ++j) {
+    const int64_t n = min(t.n0 + (wn * NF + j) * 16 + i16, p.N - 1);
+    pb[j] = t.B + n * p.ldb + 16 * g;
+    ob[j] = n >> p.bsh;
+  }
+  f32x4_v acc[MF][NF];
+#pragma unroll
+  for (int i = 0; i < MF; ++i)
+#pragma unroll
+    for (int j = 0; j < NF; ++j) acc[i][j] = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
+
+  auto frag = [&](const uint8_t *q, int k) -> i32x8_v {  // k: the lane's first of the block
+    typedef __attribute__((ext_vector_type(4))) int i4;
+    i4 lo = i4{0, 0, 0, 0}, hi = i4{0, 0, 0, 0};
+    if (k < t.kend) lo = *reinterpret_cast<const i4 *>(q);
+    if (k + 64 < t.kend) hi = *reinterpret_cast<const i4 *>(q + 64);
+    return i32x8_v{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  };
+  for (int kb = t.kb0 + wk; kb < t.kb1; kb += WK) {
+    const int k = kb * KB + 16 * g;
+    i32x8_v fa[MF], fb[NF];
+    int ea[MF], eb[NF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+      fa[i] = frag(pa[i] + (int64_t)kb * KB, k);
+      ea[i] = p.sa[kb * p.ldsa + oa[i]];
+    }
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+      fb[j] = frag(pb[j] + (int64_t)kb * KB, k);
+      eb[j] = t.sb[kb * p.ldsb + ob[j]];
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        bf16x8_v ca[MF], cb[NF];
+#pragma unroll
+        for (int i = 0; i < MF; ++i) ca[i] = fp8_to_bf16<FA>(fa[i][2 * h], fa[i][2 * h + 1], fp8_scale(ea[i]));
+#pragma unroll
+        for (int j = 0; j < NF; ++j) cb[j] = fp8_to_bf16<FB>(fb[j][2 * h], fb[j][2 * h + 1], fp8_scale(eb[j]));
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+          for (int j = 0; j < NF; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb[j], ca[i], acc[i][j], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = fp8_mul<FA, FB>(fa[i], fb[j], ea[i], eb[j], acc[i][j]);
+    }
+  }
+  if constexpr (WK > 1) {
+    __shared__ __align__(16) float part[WK - 1][WM * WN][MF * NF * 256];
+    if (wk > 0) {
+#pragma unroll
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+          *reinterpret_cast<f32x4_v *>(&part[wk - 1][wm * WN + wn][(i * NF + j) * 256 + 4 * lane]) = acc[i][j];
+    }
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll
+    for (int s = 0; s < WK - 1; ++s)
+#pragma unroll
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+          acc[i][j] += *reinterpret_cast<const f32x4_v *>(&part[s][wm * WN + wn][(i * NF + j) * 256 + 4 * lane]);
+  }
+#pragma unroll
+  for (int i = 0; i < MF; ++i)
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+      const int m = t.m0 + (wm * MF + i) * 16 + i16, n = t.n0 + (wn * NF + j) * 16 + 4 * g;
+      if (m < t.m_lim && n < p.N) fp8_store4(p, t.c_off, m, n, acc[i][j]);
+    }
+}
+
+// Calls f with the operands' formats and whether the sums are fp32 ones, as constants
+template <typename F>
+void with_formats(const lc_gemm_fp8_args &a, bool f32, F f) {
+  auto fb = [&](auto x) {
+    auto fs = [&](auto y) {
+      if (f32) f(x, y, std::true_type{});
+      else f(x, y, std::false_type{});
+    };
+    if (a.b_dtype == LC_FP8_E4M3) fs(std::integral_constant<int, 0>{});
+    else fs(std::integral_constant<int, 1>{});
+  };
+  if (a.a_dtype == LC_FP8_E4M3) fb(std::integral_constant<int, 0>{});
+  else fb(std::integral_constant<int, 1>{});
+}
+
+template <int MF, int NF, int WM, int WN, int WK>
+lc_status direct_launch(Fp8P p, const lc_gemm_fp8_args &a, bool f32, hipStream_t s) {
+  constexpr int BM = 16 * MF * WM, BN = 16 * NF * WN;
+  p.tiles_m = (p.M + BM - 1) / BM;
+  p.tiles_n = (p.N + BN - 1) / BN;
+  const int64_t rows = (int64_t)p.tiles_m + (p.gmode == LC_GROUP_ROWS ? p.ngroups : 0);
+  const int64_t grid = rows * p.tiles_n * (p.gmode == LC_GROUP_K ? p.ngroups : 1);
+  if (grid > (int64_t)UINT32_MAX) return fail(LC_ERR_UNSUPPORTED, "gemm fp8: too many outputs");
+  launch_parts((uint32_t)grid, [&](uint32_t first, uint32_t count) {
+    with_formats(a, f32, [&](auto fa, auto fb, auto f) {
+      hipLaunchKernelGGL((fp8_direct_kernel<decltype(fa)::value, decltype(fb)::value, decltype(f)::value, MF, NF, WM, WN, WK>),
+                         dim3(count), dim3(64 * WM * WN * WK), 0, s, p, first);
+    });
+  });
+  return check_launch("fp8_direct_kernel");
+}
+
+}  // namespace
+
+static lc_status check_gemm_fp8(const lc_gemm_fp8_args &a) {
+  if (a.M < 0 || a.N <= 0 || a.K <= 0) return fail(LC_ERR_INVALID_ARG, "gemm fp8: need M >= 0, N > 0, K > 0");
+  if (a.M >= (1 << 30) || a.N >= (1 << 30) || a.K >= (1 << 30))
+    return fail(LC_ERR_UNSUPPORTED, "gemm fp8: dimension too large");
+  if ((a.a_dtype != LC_FP8_E4M3 && a.a_dtype != LC_FP8_E5M2) || (a.b_dtype != LC_FP8_E4M3 && a.b_dtype != LC_FP8_E5M2))
+    return fail(LC_ERR_INVALID_ARG, "gemm fp8: operands must be e4m3 or e5m2");
+  if ((a.a_block_rows != 1 && a.a_block_rows != 128) || (a.b_block_rows != 1 && a.b_block_rows != 128))
+    return fail(LC_ERR_INVALID_ARG, "gemm fp8: block rows must be 1 or 128");
+  if (a.epilogue < LC_EPI_STORE || a.epilogue > LC_EPI_SWIGLU_BWD)
+    return fail(LC_ERR_INVALID_ARG, "gemm fp8: unknown epilogue %d", a.epilogue);
+  if (a.epilogue > LC_EPI_RESIDUAL)
+    return fail(LC_ERR_UNSUPPORTED, "gemm fp8: epilogues are STORE, STORE_F32, ACCUM_F32 and RESIDUAL");
+  const bool typed = a.epilogue == LC_EPI_STORE || a.epilogue == LC_EPI_RESIDUAL;
+  if (typed && !valid_dtype(a.c_dtype)) return fail(LC_ERR_INVALID_ARG, "gemm fp8: unknown c_dtype");
+  const int64_t MOST = (int64_t)1 << 30;
+  if (a.M > 0 && (!a.A || !a.B || !a.a_scale || !a.b_scale || !a.C || !aligned16(a.A) || !aligned16(a.B) ||
+                  !aligned16(a.a_scale) || !aligned16(a.b_scale) || !aligned16(a.C)))
+    return fail(LC_ERR_INVALID_ARG, "gemm fp8: null or unaligned pointer");
+  if (a.K % 16 || a.lda % 16 || a.ldb % 16 || a.ld_a_scale % 4 || a.ld_b_scale % 4)
+    return fail(LC_ERR_INVALID_ARG, "gemm fp8: K, lda, ldb must be multiples of 16, ld_a_scale, ld_b_scale of 4");
+  if (a.lda < a.K || a.ldb < a.K || a.ld_a_scale < (a.M + a.a_block_rows - 1) / a.a_block_rows ||
+      a.ld_b_scale < (a.N + a.b_block_rows - 1) / a.b_block_rows || a.ldc < a.N)
+    return fail(LC_ERR_INVALID_ARG, "gemm fp8: leading dimension too small");
+  if (a.lda > (1 << 22) || a.ldb > (1 << 22) || a.ld_a_scale > MOST || a.ld_b_scale > MOST || a.ldc > MOST)
+    return fail(LC_ERR_UNSUPPORTED, "gemm fp8: leading dimension too large");
+  if (a.epilogue == LC_EPI_RESIDUAL) {
+    if (a.M > 0 && (!a.R || !aligned16(a.R))) return fail(LC_ERR_INVALID_ARG, "gemm fp8: null or unaligned residual");
+    if (!valid_dtype(a.r_dtype) || a.ldr < a.N || a.ldr > MOST)
+      return fail(LC_ERR_INVALID_ARG, "gemm fp8: bad residual operand");
+  }
+  if (a.group_mode != LC_GROUP_NONE) {
+    if (a.group_mode != LC_GROUP_ROWS && a.group_mode != LC_GROUP_K)
+      return fail(LC_ERR_INVALID_ARG, "gemm fp8: unknown group mode %d", a.group_mode);
+    if (a.n_groups < 1 || a.n_groups > 64) return fail(LC_ERR_INVALID_ARG, "gemm fp8: n_groups must be 1..64");
+    if (!a.group_offsets || (reinterpret_cast<uintptr_t>(a.group_offsets) & 3))
+      return fail(LC_ERR_INVALID_ARG, "gemm fp8: group offsets must be a 4-byte aligned device array");
+    if (a.epilogue == LC_EPI_RESIDUAL)
+      return fail(LC_ERR_UNSUPPORTED, "gemm fp8: grouped products take STORE, STORE_F32 or ACCUM_F32");
+    const int64_t FAR = (int64_t)1 << 50;
+    if (a.group_mode == LC_GROUP_ROWS) {
+      if (a.a_block_rows != 1) return fail(LC_ERR_UNSUPPORTED, "gemm fp8: LC_GROUP_ROWS needs a_block_rows 1");
+      if (a.group_stride_b < 0 || a.group_stride_b % 16 || a.group_stride_b_scale < 0 ||
+          a.group_stride_b > FAR || a.group_stride_b_scale > FAR)
+        return fail(LC_ERR_INVALID_ARG, "gemm fp8: bad group stride of B or its scales");
+    } else if (a.group_stride_c < 0 || a.group_stride_c > FAR) {
+      return fail(LC_ERR_INVALID_ARG, "gemm fp8: bad group_stride_c");
+    }
+  }
+  return LC_OK;
+}
+
+static lc_status gemm_fp8_launch(const lc_gemm_fp8_args &a, hipStream_t s) {
+  LC_TRY(check_gemm_fp8(a));
+  if (a.M == 0) return LC_OK;
+  const bool typed = a.epilogue == LC_EPI_STORE || a.epilogue == LC_EPI_RESIDUAL;
+  Fp8P p{};
+  p.A = static_cast<const uint8_t *>(a.A);
+  p.B = static_cast<const uint8_t *>(a.B);
+  p.sa = a.a_scale;
+  p.sb = a.b_scale;
+  p.C = a.C;
+  p.R = a.R;
+  p.goff = a.group_offsets;
+  p.lda = a.lda;
+  p.ldb = a.ldb;
+  p.ldsa = a.ld_a_scale;
+  p.ldsb = a.ld_b_scale;
+  p.ldc = a.ldc;
+  p.ldr = a.ldr;
+  p.gstride_b = a.group_mode == LC_GROUP_ROWS ? a.group_stride_b : 0;
+  p.gstride_sb = a.group_mode == LC_GROUP_ROWS ? a.group_stride_b_scale : 0;
+  p.gstride_c = a.group_mode == LC_GROUP_K ? a.group_stride_c : 0;
+  p.M = (int)a.M;
+  p.N = (int)a.N;
+  p.K = (int)a.K;
+  p.ash = a.a_block_rows == 128 ? 7 : 0;
+  p.bsh = a.b_block_rows == 128 ? 7 : 0;
+  p.gmode = a.group_mode;
+  p.ngroups = a.group_mode == LC_GROUP_NONE ? 1 : a.n_groups;
+  p.epi = a.epilogue;
+  p.c_dt = typed ? a.c_dtype : LC_FP32;
+  p.r_dt = a.r_dtype;
+  p.vec = a.ldc % 4 == 0 && p.gstride_c % 4 == 0 && (a.epilogue != LC_EPI_RESIDUAL || a.ldr % 4 == 0);
+  const bool f32 = p.c_dt == LC_FP32;
+  if (a.M <= 16) return direct_launch<1, 1, 1, 1, 8>(p, a, f32, s);
+  return direct_launch<2, 2, 2, 2, 1>(p, a, f32, s);
+}
+
+}  // namespace lc
+
+extern "C" lc_status lc_gemm_fp8(const lc_gemm_fp8_args *args, void *stream) {
+  if (!args) return lc::fail(LC_ERR_INVALID_ARG, "gemm fp8: null args");
+  return lc::gemm_fp8_launch(*args, static_cast<hipStream_t>(stream));
+}

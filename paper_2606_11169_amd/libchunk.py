@@ -30,7 +30,7 @@ LC_ERR_HIP = -7
 STATUS_NAMES = {0: "OK", -1: "INVALID_ARG", -2: "UNSUPPORTED", -3: "BAD_ORDER",
                 -4: "STASH_FULL", -5: "STATE", -6: "WORKSPACE", -7: "HIP"}
 
-LC_FP32, LC_BF16, LC_FP16 = 0, 1, 2
+LC_FP32, LC_BF16, LC_FP16, LC_FP8_E4M3, LC_FP8_E5M2 = 0, 1, 2, 3, 4
 LC_PASS_F, LC_PASS_B, LC_PASS_BI, LC_PASS_BW = 0, 1, 2, 3
 LC_ORDER_WITH_NEXT = 0x100
 (LC_T_WQ, LC_T_WK, LC_T_WV, LC_T_WO, LC_T_G1, LC_T_W1, LC_T_W3, LC_T_W2, LC_T_G2,
@@ -180,6 +180,39 @@ class lc_rope_axes_args(C.Structure):
                 ("cos", C.c_void_p), ("sin", C.c_void_p)]
 
 
+class lc_fp8_quantize_args(C.Structure):
+    _fields_ = [("T", C.c_int64), ("d", C.c_int64), ("x_dtype", C.c_int32), ("q_dtype", C.c_int32),
+                ("block_rows", C.c_int32), ("n_groups", C.c_int32),
+                ("x", C.c_void_p), ("ld_x", C.c_int64), ("row_index", C.c_void_p), ("x_rows", C.c_int64),
+                ("row_weight", C.c_void_p), ("group_offsets", C.c_void_p),
+                ("q", C.c_void_p), ("ld_q", C.c_int64), ("scale", C.c_void_p), ("ld_scale", C.c_int64),
+                ("qt", C.c_void_p), ("ld_qt", C.c_int64), ("scale_t", C.c_void_p), ("ld_scale_t", C.c_int64)]
+
+
+class lc_gemm_fp8_args(C.Structure):
+    _fields_ = [("a_dtype", C.c_int32), ("b_dtype", C.c_int32), ("epilogue", C.c_int32),
+                ("c_dtype", C.c_int32), ("r_dtype", C.c_int32), ("a_block_rows", C.c_int32),
+                ("b_block_rows", C.c_int32), ("reserved", C.c_int32),
+                ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64),
+                ("A", C.c_void_p), ("lda", C.c_int64), ("a_scale", C.c_void_p), ("ld_a_scale", C.c_int64),
+                ("B", C.c_void_p), ("ldb", C.c_int64), ("b_scale", C.c_void_p), ("ld_b_scale", C.c_int64),
+                ("C", C.c_void_p), ("ldc", C.c_int64), ("R", C.c_void_p), ("ldr", C.c_int64),
+                ("group_mode", C.c_int32), ("n_groups", C.c_int32), ("group_offsets", C.c_void_p),
+                ("group_stride_b", C.c_int64), ("group_stride_b_scale", C.c_int64),
+                ("group_stride_c", C.c_int64)]
+
+
+class lc_moe_balance_args(C.Structure):
+    _fields_ = [("T", C.c_int64), ("d", C.c_int32), ("E", C.c_int32),
+                ("n_dtype", C.c_int32), ("w_dtype", C.c_int32), ("dn_dtype", C.c_int32),
+                ("dres_dtype", C.c_int32), ("coef", C.c_float), ("z_coef", C.c_float),
+                ("store_dwr", C.c_int32), ("reserved", C.c_int32),
+                ("n", C.c_void_p), ("wr", C.c_void_p), ("sel", C.c_void_p), ("mask", C.c_void_p),
+                ("probs", C.c_void_p), ("lse", C.c_void_p), ("counts", C.c_void_p), ("loss", C.c_void_p),
+                ("w", C.c_void_p), ("dw", C.c_void_p), ("dres", C.c_void_p), ("dn", C.c_void_p),
+                ("dwr_accum", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
+
+
 # name -> (restype, argtypes)
 _SIGS = {
     "lc_last_error": (C.c_char_p, []),
@@ -254,6 +287,12 @@ _SIGS = {
     "lc_rope_axes_backward": (C.c_int, [C.POINTER(lc_rope_axes_args), C.c_void_p]),
     "lc_rope_axes_table": (C.c_int, [C.POINTER(lc_rope_axes_args), C.c_void_p]),
     "lc_cast_bf16": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "lc_fp8_quantize": (C.c_int, [C.POINTER(lc_fp8_quantize_args), C.c_void_p]),
+    "lc_fp8_padded_rows": (C.c_int64, [C.c_int64, C.c_int32]),
+    "lc_gemm_fp8": (C.c_int, [C.POINTER(lc_gemm_fp8_args), C.c_void_p]),
+    "lc_moe_balance_forward": (C.c_int, [C.POINTER(lc_moe_balance_args), C.c_void_p]),
+    "lc_moe_balance_backward": (C.c_int, [C.POINTER(lc_moe_balance_args), C.c_void_p]),
+    "lc_moe_balance_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
     "lc_moe_route": (C.c_int, [C.POINTER(lc_moe_args), C.c_void_p]),
     "lc_moe_dispatch": (C.c_int, [C.POINTER(lc_moe_args), C.c_void_p]),
     "lc_stage_timer_enable": (C.c_int, [C.c_void_p, C.c_int32]),
@@ -736,6 +775,59 @@ def lc_moe_dispatch(T, E, sel, w, offsets, perm, wrow, rowpos, stream=None):
     a.offsets, a.perm = ptr(offsets) or None, ptr(perm) or None
     a.wrow, a.rowpos = ptr(wrow) or None, ptr(rowpos) or None
     return _check(lib().lc_moe_dispatch(C.byref(a), C.c_void_p(stream_ptr(stream) or None)))
+
+
+def lc_fp8_padded_rows(T, n_groups=0) -> int:
+    """Columns of the column layout of T rows in n_groups groups (0: none), at most."""
+    return int(lib().lc_fp8_padded_rows(T, n_groups))
+
+
+def lc_fp8_quantize(T, d, x, x_dtype, q_dtype, q=None, ld_q=0, scale=None, ld_scale=0, qt=None, ld_qt=0,
+                    scale_t=None, ld_scale_t=0, block_rows=1, ld_x=0, row_index=None, x_rows=0,
+                    row_weight=None, group_offsets=None, n_groups=0, stream=None):
+    """8-bit values and power-of-two scales per block of 128, as rows (q), columns (qt) or both."""
+    a = lc_fp8_quantize_args(T, d, x_dtype, q_dtype, block_rows, n_groups, ptr(x), ld_x, ptr(row_index),
+                             x_rows, ptr(row_weight), ptr(group_offsets), ptr(q), ld_q, ptr(scale),
+                             ld_scale, ptr(qt), ld_qt, ptr(scale_t), ld_scale_t)
+    return _check(lib().lc_fp8_quantize(C.byref(a), stream_ptr(stream)))
+
+
+def lc_gemm_fp8(epilogue, M, N, K, A, lda, a_scale, ld_a_scale, B, ldb, b_scale, ld_b_scale, Cm, ldc,
+                a_dtype=LC_FP8_E4M3, b_dtype=LC_FP8_E4M3, c_dtype=LC_BF16, a_block_rows=1,
+                b_block_rows=128, R=None, ldr=0, r_dtype=None, stream=None, group_mode=0, n_groups=0,
+                group_offsets=None, group_stride_b=0, group_stride_b_scale=0, group_stride_c=0):
+    """C = A.B^T of operands quantised by lc_fp8_quantize; r_dtype defaults to c_dtype."""
+    a = lc_gemm_fp8_args(a_dtype, b_dtype, epilogue, c_dtype, c_dtype if r_dtype is None else r_dtype,
+                         a_block_rows, b_block_rows, 0, M, N, K, ptr(A), lda, ptr(a_scale), ld_a_scale,
+                         ptr(B), ldb, ptr(b_scale), ld_b_scale, ptr(Cm), ldc, ptr(R), ldr, group_mode,
+                         n_groups, ptr(group_offsets), group_stride_b, group_stride_b_scale,
+                         group_stride_c)
+    return _check(lib().lc_gemm_fp8(C.byref(a), stream_ptr(stream)))
+
+
+def lc_moe_balance_scratch_bytes(T, d, E) -> int:
+    return int(lib().lc_moe_balance_scratch_bytes(T, d, E))
+
+
+def lc_moe_balance_forward(T, d, E, n, wr, sel, probs, lse, counts, loss, scratch, scratch_bytes, n_dtype,
+                           w_dtype, mask=None, stream=None):
+    """A router's balance and z losses, per-expert counts, and what their backward needs."""
+    a = lc_moe_balance_args(T, d, E, n_dtype, w_dtype, 0, 0, 0.0, 0.0, 0, 0, ptr(n), ptr(wr), ptr(sel),
+                            ptr(mask), ptr(probs), ptr(lse), ptr(counts), ptr(loss), 0, 0, 0, 0, 0,
+                            ptr(scratch), scratch_bytes)
+    return _check(lib().lc_moe_balance_forward(C.byref(a), stream_ptr(stream)))
+
+
+def lc_moe_balance_backward(T, d, E, n, wr, sel, probs, lse, counts, coef, z_coef, dn, dwr_accum, scratch,
+                            scratch_bytes, n_dtype, w_dtype, dn_dtype, dres=None, dres_dtype=LC_FP32,
+                            w=None, dw=None, mask=None, store_dwr=0, stream=None):
+    """Gradients of coef * balance + z_coef * z loss, and of the pair's weights (w, dw), at the
+    router's input and weights."""
+    a = lc_moe_balance_args(T, d, E, n_dtype, w_dtype, dn_dtype, dres_dtype, coef, z_coef, store_dwr, 0,
+                            ptr(n), ptr(wr), ptr(sel), ptr(mask), ptr(probs), ptr(lse), ptr(counts), 0,
+                            ptr(w), ptr(dw), ptr(dres), ptr(dn), ptr(dwr_accum), ptr(scratch),
+                            scratch_bytes)
+    return _check(lib().lc_moe_balance_backward(C.byref(a), stream_ptr(stream)))
 
 
 def lc_stage_timer_enable(stage, max_launches):

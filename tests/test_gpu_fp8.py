@@ -1,0 +1,403 @@
+"""Quantisation to 8 bits with block scales and the products of its operands, against their
+definitions in 64 bits.
+
+Quantised bytes and scales are compared exactly: the scale is a power of two, so the one rounding is
+the conversion's. Product tolerances:
+  * integers small enough that every sum is exact (products of 0, +-1, +-2, sums below 2^24): no error
+    beyond the result type's one rounding;
+  * real values, 16-bit results: half a step of the type (2^-8 bf16, 2^-11 fp16), and the 8-bit matrix
+    instruction's sums, which keep 8 neighbouring products to 2^-13 of the largest: at most
+    8 * 2^-13 of the sum of |a b|; over all values (2-norm) half a step and 2^-12;
+  * fp32 results: each instruction adds 32 products in fp32, K/32 additions of a few roundings:
+    (K/32 * 6 + 2) * 2^-24 of the sum of |a b|.
+"""
+import pytest
+import torch
+
+from paper_2606_11169_amd import libchunk as lc
+
+pytestmark = pytest.mark.gpu
+
+DT = {"fp32": (lc.LC_FP32, torch.float32), "bf16": (lc.LC_BF16, torch.bfloat16), "fp16": (lc.LC_FP16, torch.float16),
+      "e4m3": (lc.LC_FP8_E4M3, torch.float8_e4m3fn), "e5m2": (lc.LC_FP8_E5M2, torch.float8_e5m2)}
+HALF_STEP = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11, "fp32": 2.0 ** -24}
+LARGEST = {"e4m3": (448.0, -6, 3), "e5m2": (57344.0, -14, 2)}
+MARK = 0xA5
+
+
+def up(n, to):
+    return -(-n // to) * to
+
+
+def pow2(e):
+    """2^e in 64 bits, exactly."""
+    return ((torch.as_tensor(e).long() + 1023) << 52).view(torch.float64)
+
+
+def ref_blocks(x, q, rows):
+    """x [r, k] (64 bits, CPU): scale bytes [ceil(k/128), ceil(r/rows)] and rounded values, NaN and
+    infinities as q has them."""
+    largest, low, bits = LARGEST[q]
+    r, k = x.shape
+    y = torch.nn.functional.pad(x, (0, -k % 128, 0, -r % rows)).view(-1, rows, up(k, 128) // 128, 128)
+    a = torch.where(torch.isfinite(y), y.abs(), 0.0).amax((1, 3))
+    e = torch.frexp(a / largest)[1].clamp(min=-200)  # a / largest < 2^e
+    e = torch.where(a <= largest * pow2(e - 1), e - 1, e)
+    s = torch.where(a > 0, e + 127, 0).clamp(min=0)
+    z = y * pow2(127 - s)[:, None, :, None]
+    fe = torch.frexp(z)[1] - 1
+    step = pow2(fe.clamp(min=low) - bits)
+    v = torch.round(z / step) * step
+    v = torch.where(torch.isinf(z), float("nan") if q == "e4m3" else z, v).view(-1, up(k, 128))[:r, :k]
+    return s.to(torch.uint8).T.contiguous(), v
+
+
+def same(got, want):
+    got, want = got.double(), want.double()
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(got), nan)
+    assert torch.equal(torch.where(nan, 0.0, got), torch.where(nan, 0.0, want))
+
+
+def values(T, d, dtype, seed, kind="normal"):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, d, generator=g, dtype=torch.float64) * torch.exp(torch.randn(d, generator=g, dtype=torch.float64))
+    if kind == "ties":  # few significant bits: many values half way between two of the 8-bit type
+        x = torch.randint(-31, 32, (T, d), generator=g).double() * 2.0 ** torch.randint(-9, 3, (T, d), generator=g)
+    elif kind == "wide":  # zeros, blocks of zeros, subnormals, the largest and smallest of the type
+        x = x * 2.0 ** torch.randint(-60, 20, (T, 1), generator=g).double()
+        x[torch.rand(T, d, generator=g) < 0.3] = 0
+        x[: T // 3, : d // 2] = 0
+        if dtype != "fp16":
+            x[T // 3: T // 2] *= 2.0 ** -80
+            x[-1] *= 2.0 ** 100
+        x = x.clamp(-60000, 60000) if dtype == "fp16" else x
+    elif kind == "odd":  # NaN of both kinds and infinities beside numbers
+        x[torch.rand(T, d, generator=g) < 0.02] = float("nan")
+        x[torch.rand(T, d, generator=g) < 0.02] = float("inf")
+        x[torch.rand(T, d, generator=g) < 0.02] = -float("inf")
+    y = x.to(DT[dtype][1])
+    if kind == "odd" and T > 2:
+        bits = y.view(torch.int16 if dtype != "fp32" else torch.int32)
+        bits[1, 0] = {"bf16": 0x7F81, "fp16": 0x7C01, "fp32": 0x7F800001}[dtype]  # a signalling NaN
+        bits[2, : min(d, 128)] = {"bf16": -1, "fp16": -1, "fp32": -1}[dtype]  # nothing but NaN
+    return y
+
+
+class Quant:
+    """A call's buffers, filled with a mark, on the GPU."""
+
+    def __init__(self, T, d, block, layouts, n_groups=0, extra=0):
+        mk = lambda *s: torch.full(s, MARK, dtype=torch.uint8, device="cuda")  # noqa: E731
+        self.cols = lc.lc_fp8_padded_rows(T, n_groups)
+        self.q = mk(max(T, 1), up(d, 16) + 16 * extra) if "r" in layouts else None
+        self.s = mk(up(d, 128) // 128, max(4, up(-(-T // block), 4)) + 4 * extra) if "r" in layouts else None
+        self.qt = mk(d, max(16, self.cols) + 16 * extra) if "c" in layouts else None
+        self.st = mk(max(1, self.cols // 128), up(-(-d // block), 4) + 4 * extra) if "c" in layouts else None
+
+    def args(self):
+        ld = lambda t: 0 if t is None else t.stride(0)  # noqa: E731
+        return dict(q=self.q, ld_q=ld(self.q), scale=self.s, ld_scale=ld(self.s), qt=self.qt, ld_qt=ld(self.qt),
+                    scale_t=self.st, ld_scale_t=ld(self.st))
+
+
+def check_rows(b, x, q, block):
+    T, d = x.shape
+    s, v = ref_blocks(x, q, block)
+    got = b.q.cpu()
+    same(got[:, :d].contiguous().view(DT[q][1]).float(), v)
+    assert bool((got[:, d:up(d, 16)] == 0).all()) and bool((got[:, up(d, 16):] == MARK).all())
+    assert torch.equal(b.s.cpu()[:, :s.shape[1]], s) and bool((b.s.cpu()[:, s.shape[1]:] == MARK).all())
+
+
+def check_cols(b, full, q, block, used):
+    """full [columns, d]: what the column layout holds, zeros in its gaps; `used` columns written."""
+    d = full.shape[1]
+    got, st = b.qt.cpu(), b.st.cpu()
+    if used == 0:  # groups without a row: nothing is written
+        assert bool((got == MARK).all()) and bool((st == MARK).all())
+        return
+    s, v = ref_blocks(full[:used].T.contiguous(), q, block)
+    same(got[:, :used].contiguous().view(DT[q][1]).float(), v)
+    assert bool((got[:, used:] == MARK).all())
+    assert torch.equal(st[:used // 128, :s.shape[1]], s)
+    assert bool((st[used // 128:] == MARK).all()) and bool((st[:, -(-d // block):] == MARK).all())
+
+
+@pytest.mark.parametrize("kind", ["normal", "ties", "wide", "odd"])
+@pytest.mark.parametrize("q", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_quantize_values(dtype, q, kind):
+    T, d = 200, 264
+    x = values(T, d, dtype, 5, kind)
+    for block in (1, 128):
+        b = Quant(T, d, block, "rc")
+        lc.lc_fp8_quantize(T, d, x.cuda(), DT[dtype][0], DT[q][0], block_rows=block, **b.args())
+        torch.cuda.synchronize()
+        check_rows(b, x.double(), q, block)
+        check_cols(b, torch.nn.functional.pad(x.double(), (0, 0, 0, -T % 128)), q, block, up(T, 128))
+
+
+@pytest.mark.parametrize("T,d,dtype,block,layouts,extra,ld", [
+    (1, 1, "fp32", 1, "rc", 0, 0), (1, 2048, "bf16", 1, "r", 0, 0), (1, 40, "bf16", 128, "rc", 1, 0),
+    (127, 129, "bf16", 1, "rc", 0, 0), (128, 128, "fp16", 128, "c", 0, 0), (129, 127, "fp32", 128, "rc", 2, 0),
+    (257, 1000, "bf16", 1, "c", 1, 0), (300, 72, "bf16", 1, "rc", 0, 80), (300, 72, "bf16", 1, "rc", 0, 75),
+    (131, 200, "fp32", 1, "rc", 0, 202), (5, 4099, "fp16", 1, "r", 3, 0), (1000, 17, "bf16", 1, "rc", 0, 0)])
+def test_quantize_shapes(T, d, dtype, block, layouts, extra, ld):
+    """Odd sizes, rows with a stride (aligned or not), single layouts, wider outputs."""
+    wide = values(T, ld or d, dtype, T + d)
+    x, b = wide[:, :d], Quant(T, d, block, layouts, extra=extra)
+    lc.lc_fp8_quantize(T, d, wide.cuda(), DT[dtype][0], DT["e4m3"][0], block_rows=block, ld_x=ld, **b.args())
+    torch.cuda.synchronize()
+    if b.q is not None:
+        check_rows(b, x.double(), "e4m3", block)
+    if b.qt is not None:
+        check_cols(b, torch.nn.functional.pad(x.double(), (0, 0, 0, -T % 128)), "e4m3", block, up(T, 128))
+
+
+def in_columns(rows, offsets, columns):
+    """rows [T, d] as the column layout has them with groups; and how many columns are used."""
+    full, at = torch.zeros(columns, rows.shape[1], dtype=torch.float64), 0
+    for a, b in zip(offsets[:-1], offsets[1:]):
+        full[at:at + b - a] = rows[a:b]
+        at += up(b - a, 128)
+    return full, at
+
+
+@pytest.mark.parametrize("offsets", [[0, 300], [0, 0, 5, 5, 133, 300], [7, 7, 140, 290], [300, 300, 300],
+                                     [0] * 33 + [128, 256, 300] + [300] * 29], ids=str)
+@pytest.mark.parametrize("dtype,weighted", [("bf16", True), ("fp32", False), ("fp16", True), ("bf16", False)])
+def test_quantize_groups(offsets, dtype, weighted):
+    """Rows gathered (some indices out of range), weighted, in groups: empty ones, rows before and
+    behind all groups."""
+    T, d, src = 300, 136, 90
+    x = values(src, d, dtype, 3, "odd" if weighted else "normal")
+    g = torch.Generator().manual_seed(9)
+    index = torch.randint(0, src, (T,), generator=g, dtype=torch.int32)
+    index[[0, 50, 299]] = torch.tensor([-1, src, -2 ** 31], dtype=torch.int32)
+    w = torch.randn(T, generator=g)
+    n = len(offsets) - 1
+    rows = torch.where(((index >= 0) & (index < src))[:, None], x[index.clamp(0, src - 1).long()].float(), 0.0)
+    rows = (rows * w[:, None] if weighted else rows).double()
+    rows[(index < 0) | (index >= src)] = 0
+    b = Quant(T, d, 1, "rc", n)
+    lc.lc_fp8_quantize(T, d, x.cuda(), DT[dtype][0], DT["e5m2"][0], row_index=index.cuda(), x_rows=src,
+                       row_weight=w.cuda() if weighted else None, n_groups=n,
+                       group_offsets=torch.tensor(offsets, dtype=torch.int32, device="cuda"), **b.args())
+    torch.cuda.synchronize()
+    check_rows(b, rows, "e5m2", 1)
+    check_cols(b, *in_columns(rows, offsets, b.cols)[:1], "e5m2", 1, in_columns(rows, offsets, b.cols)[1])
+
+
+# ------------------------------------------------------------------ products
+
+def operand(r, k, q, block, seed, kind, scale=1.0):
+    """Bytes [r, ld], scales [blocks, ld], and the values they stand for in 64 bits."""
+    g = torch.Generator().manual_seed(seed)
+    if kind == "small":
+        v = torch.randint(-2, 3, (r, k), generator=g).double()
+        s = torch.full((up(k, 128) // 128, -(-r // block)), 127, dtype=torch.uint8)
+    else:
+        x = torch.randn(r, k, generator=g, dtype=torch.float64) * torch.exp(torch.randn(k, generator=g, dtype=torch.float64) * 0.5) * scale
+        s, v = ref_blocks(x.float().double(), q, block)
+    ld = up(s.shape[1], 4)
+    sp = torch.full((s.shape[0], ld), 255, dtype=torch.uint8)  # (bytes behind the rows are not used)
+    sp[:, :s.shape[1]] = s
+    f = pow2(s.int() - 127).T.repeat_interleave(block, 0)[:r].repeat_interleave(128, 1)[:, :k]
+    kp = up(k, 16)
+    b = torch.zeros(r, kp + 16, dtype=torch.uint8)
+    b[:, :k] = v.float().to(DT[q][1]).view(torch.uint8)
+    b[:, kp:] = 0x7F  # NaN behind a row's values
+    return b, sp, v * f
+
+
+def check_product(got, want, mag, c, K, kind, gone=None):
+    got = got.double().cpu()
+    if kind == "small":
+        assert torch.equal(got, want.to(DT[c][1]).double())
+        return
+    if c == "fp32":
+        tol = (K / 32 * 6 + 2) * 2.0 ** -24 * mag + 2.0 ** -24 * want.abs()
+    else:
+        tol = (8 * 2.0 ** -13 + (K / 128 + 8) * 2.0 ** -24) * mag + HALF_STEP[c] * want.abs()
+        assert (got - want).norm() <= (HALF_STEP[c] + 2.0 ** -12) * want.norm()
+    bad = (got - want).abs() > tol
+    assert not bool(bad.any()), ((got - want).abs() / tol).max()
+
+
+PRODUCTS = [
+    # M, N, K, a, b, c, a_block, b_block
+    (1, 1, 16, "e4m3", "e4m3", "bf16", 1, 1), (1, 129, 400, "e4m3", "e4m3", "fp32", 1, 128),
+    (3, 4096, 1040, "e5m2", "e4m3", "bf16", 1, 128), (16, 64, 128, "e4m3", "e5m2", "fp16", 1, 1),
+    (17, 65, 144, "e5m2", "e5m2", "bf16", 1, 1), (33, 200, 2064, "e4m3", "e4m3", "bf16", 1, 128),
+    (64, 127, 640, "e4m3", "e4m3", "fp32", 1, 1), (130, 258, 256, "e5m2", "e4m3", "fp32", 128, 128),
+    (200, 131, 4096, "e4m3", "e4m3", "fp16", 128, 1), (257, 513, 384, "e4m3", "e4m3", "bf16", 1, 128),
+    (300, 1155, 1872, "e5m2", "e4m3", "bf16", 1, 128), (512, 256, 96, "e4m3", "e4m3", "bf16", 1, 1),
+    (1000, 1000, 1008, "e4m3", "e4m3", "fp32", 1, 1), (2050, 1030, 272, "e4m3", "e4m3", "bf16", 1, 128),
+    (513, 4100, 528, "e4m3", "e5m2", "bf16", 1, 1), (4100, 700, 144, "e4m3", "e4m3", "bf16", 128, 128),
+    (2304, 2304, 144, "e4m3", "e4m3", "bf16", 1, 1), (2300, 2310, 144, "e5m2", "e4m3", "fp32", 1, 128),
+]
+
+
+@pytest.mark.parametrize("kind", ["small", "real"])
+@pytest.mark.parametrize("M,N,K,a,b,c,ab,bb", PRODUCTS, ids=str)
+def test_product(M, N, K, a, b, c, ab, bb, kind):
+    A, sa, va = operand(M, K, a, ab, 1, kind)
+    B, sb, vb = operand(N, K, b, bb, 2, kind, 0.02)
+    ldc = N + (3 if M % 2 else 8)
+    Cm = torch.full((M, ldc), 77.0, dtype=DT[c][1], device="cuda")
+    lc.lc_gemm_fp8(lc.LC_EPI_STORE, M, N, K, A.cuda(), A.stride(0), sa.cuda(), sa.stride(0), B.cuda(), B.stride(0),
+                   sb.cuda(), sb.stride(0), Cm, ldc, a_dtype=DT[a][0], b_dtype=DT[b][0], c_dtype=DT[c][0],
+                   a_block_rows=ab, b_block_rows=bb)
+    torch.cuda.synchronize()
+    check_product(Cm[:, :N], va @ vb.T, va.abs() @ vb.abs().T, c, K, kind)
+    assert bool((Cm[:, N:] == 77.0).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 60, 160), (70, 133, 272), (300, 520, 144), (2304, 2304, 144)])
+@pytest.mark.parametrize("epi,c,r", [("store_f32", "fp32", None), ("accum", "fp32", None), ("residual", "fp32", "fp32"),
+                                     ("residual", "bf16", "fp32"), ("residual", "fp32", "bf16"),
+                                     ("residual", "fp16", "fp16")])
+def test_epilogues(M, N, K, epi, c, r):
+    A, sa, va = operand(M, K, "e4m3", 1, 1, "small")
+    B, sb, vb = operand(N, K, "e4m3", 128, 2, "small")
+    g = torch.Generator().manual_seed(3)
+    R = torch.randint(-9, 10, (M, N), generator=g).double()
+    Cm = (R if epi == "accum" else R * 0 + 5).to(DT[c][1]).cuda()
+    code = {"store_f32": lc.LC_EPI_STORE_F32, "accum": lc.LC_EPI_ACCUM_F32, "residual": lc.LC_EPI_RESIDUAL}[epi]
+    lc.lc_gemm_fp8(code, M, N, K, A.cuda(), A.stride(0), sa.cuda(), sa.stride(0), B.cuda(), B.stride(0), sb.cuda(),
+                   sb.stride(0), Cm, N, c_dtype=DT[c][0], R=R.to(DT[r][1]).cuda() if r else None, ldr=N,
+                   r_dtype=DT[r][0] if r else None)
+    torch.cuda.synchronize()
+    want = va @ vb.T + (0 if epi == "store_f32" else R)
+    assert torch.equal(Cm.double().cpu(), want.to(DT[c][1]).double())
+
+
+def test_residual_in_place():
+    M, N, K = 140, 264, 144
+    A, sa, va = operand(M, K, "e4m3", 1, 1, "small")
+    B, sb, vb = operand(N, K, "e4m3", 128, 2, "small")
+    R = torch.randint(-9, 10, (M, N), generator=torch.Generator().manual_seed(3)).double()
+    Cm = R.float().cuda()
+    lc.lc_gemm_fp8(lc.LC_EPI_RESIDUAL, M, N, K, A.cuda(), A.stride(0), sa.cuda(), sa.stride(0), B.cuda(), B.stride(0),
+                   sb.cuda(), sb.stride(0), Cm, N, c_dtype=lc.LC_FP32, R=Cm, ldr=N, r_dtype=lc.LC_FP32)
+    torch.cuda.synchronize()
+    assert torch.equal(Cm.double().cpu(), R + va @ vb.T)
+
+
+@pytest.mark.parametrize("kind", ["small", "real"])
+@pytest.mark.parametrize("offsets,M,N,K,c,bb", [
+    ([0, 0, 1, 18, 18, 200, 300], 310, 200, 400, "bf16", 128), ([5, 40, 40, 45], 64, 130, 144, "fp32", 1),
+    ([0, 9, 9, 11, 12], 12, 513, 272, "bf16", 128), ([0] * 40 + [64] * 20 + [70], 75, 96, 160, "fp16", 128),
+    ([0, 700, 1500, 1500, 3001], 3003, 1034, 272, "bf16", 128), ([0, 900, 2500], 2500, 1040, 144, "fp32", 128),
+    ([0, 0, 0], 30, 64, 128, "bf16", 1)], ids=str)
+def test_grouped_rows(offsets, M, N, K, c, bb, kind):
+    G = len(offsets) - 1
+    A, sa, va = operand(M, K, "e4m3", 1, 1, kind)
+    parts = [operand(N, K, "e4m3", bb, 10 + i, kind, 0.02) for i in range(G)]
+    B, sb = torch.cat([p[0] for p in parts]), torch.cat([p[1] for p in parts])
+    Cm = torch.full((M, N), 77.0, dtype=DT[c][1], device="cuda")
+    lc.lc_gemm_fp8(lc.LC_EPI_STORE, M, N, K, A.cuda(), A.stride(0), sa.cuda(), sa.stride(0), B.cuda(), B.stride(0),
+                   sb.cuda(), sb.stride(0), Cm, N, c_dtype=DT[c][0], b_block_rows=bb, group_mode=lc.LC_GROUP_ROWS,
+                   n_groups=G, group_offsets=torch.tensor(offsets, dtype=torch.int32, device="cuda"),
+                   group_stride_b=N * B.stride(0), group_stride_b_scale=parts[0][1].numel())
+    torch.cuda.synchronize()
+    for i, (x, y) in enumerate(zip(offsets[:-1], offsets[1:])):
+        if y > x:
+            check_product(Cm[x:y], va[x:y] @ parts[i][2].T, va[x:y].abs() @ parts[i][2].abs().T, c, K, kind)
+    assert bool((Cm[:offsets[0]] == 77.0).all()) and bool((Cm[offsets[-1]:] == 77.0).all())
+
+
+@pytest.mark.parametrize("kind", ["small", "real"])
+@pytest.mark.parametrize("lengths,M,N,c,epi", [
+    ([300], 40, 72, "bf16", "store"), ([0, 5, 130, 0, 128], 65, 129, "fp32", "store"), ([1, 1, 1], 200, 300, "bf16", "store"),
+    ([700, 0, 33], 258, 513, "bf16", "store"), ([40, 200, 0], 130, 260, "fp32", "accum"),
+    ([3] * 64, 24, 40, "fp16", "store"), ([500, 600], 2304, 1030, "bf16", "store"),
+    ([400, 0, 200], 1040, 1032, "fp32", "accum")], ids=str)
+def test_grouped_k(lengths, M, N, c, epi, kind):
+    """Operands in the column layout: groups from multiples of 128 on, columns of no group behind."""
+    G, T = len(lengths), sum(lengths)
+    K = lc.lc_fp8_padded_rows(T, G)
+    start, full = [], []
+    at = 0
+    for n in lengths:
+        start.append(at)
+        at += up(n, 128)
+    A, sa, va = operand(M, K, "e5m2", 1, 1, kind)
+    B, sb, vb = operand(N, K, "e4m3", 1, 2, kind)
+    used = torch.zeros(K, dtype=torch.bool)
+    for s, n in zip(start, lengths):
+        used[s:s + n] = True
+    A[:, :K][:, ~used], va[:, ~used] = 0, 0  # zeros behind a group
+    A[:, at:K], B[:, at:K], sa[at // 128:], sb[at // 128:] = 0x7F, 0x7F, 255, 255  # NaN behind the last
+    Cm = torch.full((G, M, N + 5), 3.0, dtype=DT[c][1], device="cuda")
+    off = torch.tensor([0] + lengths).cumsum(0).to(torch.int32)
+    lc.lc_gemm_fp8(lc.LC_EPI_ACCUM_F32 if epi == "accum" else lc.LC_EPI_STORE, M, N, K, A.cuda(), A.stride(0), sa.cuda(),
+                   sa.stride(0), B.cuda(), B.stride(0), sb.cuda(), sb.stride(0), Cm, N + 5, a_dtype=DT["e5m2"][0],
+                   c_dtype=DT[c][0], b_block_rows=1, group_mode=lc.LC_GROUP_K, n_groups=G, group_offsets=off.cuda(),
+                   group_stride_c=M * (N + 5))
+    torch.cuda.synchronize()
+    for i, (s, n) in enumerate(zip(start, lengths)):
+        a, b = va[:, s:s + n], vb[:, s:s + n]
+        want, mag = a @ b.T, a.abs() @ b.abs().T
+        if epi == "accum":
+            want, mag = want + 3.0, mag + 3.0
+        check_product(Cm[i, :, :N], want, mag, c, n, kind)
+    assert bool((Cm[:, :, N:] == 3.0).all())
+
+
+@pytest.mark.parametrize("c", ["bf16", "fp32"])
+def test_nan_stays_in_its_row(c):
+    """A NaN value, a NaN scale and an infinity reach their own row or column and no other; a zero
+    times a large scale stays zero."""
+    M, N, K = 150, 140, 288
+    A, sa, va = operand(M, K, "e5m2", 1, 1, "small")
+    B, sb, vb = operand(N, K, "e4m3", 1, 2, "small")
+    want = (va @ vb.T).to(DT[c][1]).double()
+    A[7, 5], sa[1, 20], A[33, 9] = 0x7F, 255, 0x7C
+    B[11, 200], sb[2, 139] = 0x7F, 255
+    A[50], sa[0, 50] = 0, 254
+    want[50] = 0
+    Cm = torch.zeros(M, N, dtype=DT[c][1], device="cuda")
+    lc.lc_gemm_fp8(lc.LC_EPI_STORE, M, N, K, A.cuda(), A.stride(0), sa.cuda(), sa.stride(0), B.cuda(), B.stride(0),
+                   sb.cuda(), sb.stride(0), Cm, N, a_dtype=DT["e5m2"][0], c_dtype=DT[c][0], b_block_rows=1)
+    got = Cm.double().cpu()
+    rows, cols = torch.ones(M, dtype=torch.bool), torch.ones(N, dtype=torch.bool)
+    rows[[7, 20, 33]], cols[[11, 139]] = False, False
+    assert torch.equal(got[rows][:, cols], want[rows][:, cols])
+    assert bool(torch.isnan(got[[7, 20]]).all()) and bool(torch.isnan(got[:, [11, 139]]).all())
+    infinite = vb[:, 9] != 0
+    infinite[[11, 139]] = False
+    assert bool((~torch.isfinite(got[33, infinite])).all())
+
+
+def test_far_scales():
+    """Scales from the smallest to the largest, in pairs whose product is an ordinary number."""
+    M, N, K = 40, 24, 256
+    A, sa, va = operand(M, K, "e4m3", 1, 1, "small")
+    B, sb, vb = operand(N, K, "e4m3", 1, 2, "small")
+    for byte in (30, 60, 127, 200, 230):
+        sa[:], sb[:] = byte, 254 - byte
+        for c in ("bf16", "fp32"):
+            Cm = torch.zeros(M, N, dtype=DT[c][1], device="cuda")
+            lc.lc_gemm_fp8(lc.LC_EPI_STORE, M, N, K, A.cuda(), A.stride(0), sa.cuda(), sa.stride(0), B.cuda(),
+                           B.stride(0), sb.cuda(), sb.stride(0), Cm, N, c_dtype=DT[c][0], b_block_rows=1)
+            assert torch.equal(Cm.double().cpu(), (va @ vb.T).to(DT[c][1]).double())
+
+
+def test_deterministic():
+    """The same call gives the same bits, whatever ran between."""
+    M, N, K = 700, 900, 1040
+    A, sa, _ = operand(M, K, "e4m3", 1, 1, "real")
+    B, sb, _ = operand(N, K, "e4m3", 128, 2, "real")
+    A, sa, B, sb = (t.cuda() for t in (A, sa, B, sb))
+    out = []
+    for c in (lc.LC_BF16, lc.LC_FP32):
+        for _ in range(3):
+            Cm = torch.empty(M, N, dtype=torch.bfloat16 if c == lc.LC_BF16 else torch.float32, device="cuda")
+            lc.lc_gemm_fp8(lc.LC_EPI_STORE, M, N, K, A, A.stride(0), sa, sa.stride(0), B, B.stride(0), sb, sb.stride(0),
+                           Cm, N, c_dtype=c)
+            out.append(Cm)
+            (A.float() + 1).sum()
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+    assert torch.equal(out[3], out[4]) and torch.equal(out[3], out[5])
