@@ -42,6 +42,7 @@ EXTRA_FLAGS = {
     # than they save
     "k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "k_attn_window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "k_gemm_fp8_tile.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

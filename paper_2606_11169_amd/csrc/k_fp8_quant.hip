@@ -31,7 +31,6 @@ struct QuantP {
   int d, ngroups;
   int nct;         // column tiles
   int col_blocks;  // column layout: blocks of 128 that qt has room for
-  int vec;         // rows of x start at multiples of 16 bytes
 };
 
 typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_v;
@@ -156,12 +155,8 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t fi
 #pragma unroll
     for (int k = 0; k < (int)(sizeof(v) / 4); ++k) v[k] = 0;
     if (ok) {
-      if (p.vec && c0 + 8 <= p.d) {
-#pragma unroll
-        for (int k = 0; k < (int)(sizeof(v) / 16); ++k) {
-          const uint4 t = reinterpret_cast<const uint4 *>(row)[k];
-          v[4 * k] = t.x; v[4 * k + 1] = t.y; v[4 * k + 2] = t.z; v[4 * k + 3] = t.w;
-        }
+      if (c0 + 8 <= p.d) {  // (rows may start anywhere: wide loads take any address)
+        __builtin_memcpy(v, row, sizeof(v));
       } else {
 #pragma unroll
         for (int c = 0; c < 8; ++c)
@@ -385,7 +380,6 @@ static lc_status quantize_launch(const lc_fp8_quantize_args &a, hipStream_t s) {
   p.ngroups = a.n_groups;
   p.nct = (int)((a.d + 127) / 128);
   p.col_blocks = (int)(cols / 128);
-  p.vec = ld_x * (int64_t)dtype_size(a.x_dtype) % 16 == 0;
   // groups: one partial block each, and one each for the rows before and behind them
   const int64_t slots = a.n_groups > 0 ? (a.T + 127 * (int64_t)(a.n_groups + 2)) / 128 : (a.T + 127) / 128;
   if (slots * p.nct > (int64_t)UINT32_MAX) return fail(LC_ERR_UNSUPPORTED, "fp8 quantize: too many values");

@@ -51,39 +51,57 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void fp8_direct_kernel(Fp8P p, u
     if (k + 64 < t.kend) hi = *reinterpret_cast<const i4 *>(q + 64);
     return i32x8_v{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
   };
-  for (int kb = t.kb0 + wk; kb < t.kb1; kb += WK) {
-    const int k = kb * KB + 16 * g;
-    i32x8_v fa[MF], fb[NF];
+  // the blocks of this wave, the next one's values on their way while one is multiplied
+  struct Block {
+    i32x8_v a[MF], b[NF];
     int ea[MF], eb[NF];
+  };
+  auto fetch = [&](Block &x, int kb) {  // (a block past the last: zeros)
+    const int k = kb * KB + 16 * g;
+    const bool in = kb < t.kb1;
+    const int64_t at = in ? kb : t.kb0;
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-      fa[i] = frag(pa[i] + (int64_t)kb * KB, k);
-      ea[i] = p.sa[kb * p.ldsa + oa[i]];
+      x.a[i] = frag(pa[i] + at * KB, in ? k : t.kend);
+      x.ea[i] = p.sa[at * p.ldsa + oa[i]];
     }
 #pragma unroll
     for (int j = 0; j < NF; ++j) {
-      fb[j] = frag(pb[j] + (int64_t)kb * KB, k);
-      eb[j] = t.sb[kb * p.ldsb + ob[j]];
+      x.b[j] = frag(pb[j] + at * KB, in ? k : t.kend);
+      x.eb[j] = t.sb[at * p.ldsb + ob[j]];
     }
+  };
+  auto multiply = [&](const Block &x) {
     if constexpr (F32) {
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        bf16x8_v ca[MF], cb[NF];
+        bf16x8_v ca[MF];
 #pragma unroll
-        for (int i = 0; i < MF; ++i) ca[i] = fp8_to_bf16<FA>(fa[i][2 * h], fa[i][2 * h + 1], fp8_scale(ea[i]));
+        for (int i = 0; i < MF; ++i) ca[i] = fp8_to_bf16<FA>(x.a[i][2 * h], x.a[i][2 * h + 1], fp8_scale(x.ea[i]));
 #pragma unroll
-        for (int j = 0; j < NF; ++j) cb[j] = fp8_to_bf16<FB>(fb[j][2 * h], fb[j][2 * h + 1], fp8_scale(eb[j]));
+        for (int j = 0; j < NF; ++j) {
+          const bf16x8_v cb = fp8_to_bf16<FB>(x.b[j][2 * h], x.b[j][2 * h + 1], fp8_scale(x.eb[j]));
 #pragma unroll
-        for (int i = 0; i < MF; ++i)
-#pragma unroll
-          for (int j = 0; j < NF; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb[j], ca[i], acc[i][j], 0, 0, 0);
+          for (int i = 0; i < MF; ++i)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb, ca[i], acc[i][j], 0, 0, 0);
+        }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < MF; ++i)
 #pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = fp8_mul<FA, FB>(fa[i], fb[j], ea[i], eb[j], acc[i][j]);
+        for (int j = 0; j < NF; ++j) acc[i][j] = fp8_mul<FA, FB>(x.a[i], x.b[j], x.ea[i], x.eb[j], acc[i][j]);
+    }
+  };
+  if (t.kb0 + wk < t.kb1) {
+    Block x, y;
+    fetch(x, t.kb0 + wk);
+    for (int kb = t.kb0 + wk; kb < t.kb1; kb += 2 * WK) {
+      fetch(y, kb + WK);
+      multiply(x);
+      if (kb + WK >= t.kb1) break;
+      fetch(x, kb + 2 * WK);
+      multiply(y);
     }
   }
   if constexpr (WK > 1) {
@@ -110,37 +128,21 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void fp8_direct_kernel(Fp8P p, u
 #pragma unroll
     for (int j = 0; j < NF; ++j) {
       const int m = t.m0 + (wm * MF + i) * 16 + i16, n = t.n0 + (wn * NF + j) * 16 + 4 * g;
-      if (m < t.m_lim && n < p.N) fp8_store4(p, t.c_off, m, n, acc[i][j]);
+      if (m < t.m_lim && n < p.N) fp8_store4(p, t.c_off, m, n, acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
     }
-}
-
-// Calls f with the operands' formats and whether the sums are fp32 ones, as constants
-template <typename F>
-void with_formats(const lc_gemm_fp8_args &a, bool f32, F f) {
-  auto fb = [&](auto x) {
-    auto fs = [&](auto y) {
-      if (f32) f(x, y, std::true_type{});
-      else f(x, y, std::false_type{});
-    };
-    if (a.b_dtype == LC_FP8_E4M3) fs(std::integral_constant<int, 0>{});
-    else fs(std::integral_constant<int, 1>{});
-  };
-  if (a.a_dtype == LC_FP8_E4M3) fb(std::integral_constant<int, 0>{});
-  else fb(std::integral_constant<int, 1>{});
 }
 
 template <int MF, int NF, int WM, int WN, int WK>
 lc_status direct_launch(Fp8P p, const lc_gemm_fp8_args &a, bool f32, hipStream_t s) {
   constexpr int BM = 16 * MF * WM, BN = 16 * NF * WN;
-  p.tiles_m = (p.M + BM - 1) / BM;
-  p.tiles_n = (p.N + BN - 1) / BN;
-  const int64_t rows = (int64_t)p.tiles_m + (p.gmode == LC_GROUP_ROWS ? p.ngroups : 0);
-  const int64_t grid = rows * p.tiles_n * (p.gmode == LC_GROUP_K ? p.ngroups : 1);
-  if (grid > (int64_t)UINT32_MAX) return fail(LC_ERR_UNSUPPORTED, "gemm fp8: too many outputs");
-  launch_parts((uint32_t)grid, [&](uint32_t first, uint32_t count) {
-    with_formats(a, f32, [&](auto fa, auto fb, auto f) {
-      hipLaunchKernelGGL((fp8_direct_kernel<decltype(fa)::value, decltype(fb)::value, decltype(f)::value, MF, NF, WM, WN, WK>),
-                         dim3(count), dim3(64 * WM * WN * WK), 0, s, p, first);
+  uint32_t grid;
+  LC_TRY((fp8_grid<BM, BN>(p, &grid)));
+  launch_parts(grid, [&](uint32_t first, uint32_t count) {
+    fp8_with_formats(a, [&](auto fa, auto fb) {
+      constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value;
+      const dim3 threads(64 * WM * WN * WK);
+      if (f32) hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, true, MF, NF, WM, WN, WK>), dim3(count), threads, 0, s, p, first);
+      else hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, false, MF, NF, WM, WN, WK>), dim3(count), threads, 0, s, p, first);
     });
   });
   return check_launch("fp8_direct_kernel");
@@ -199,6 +201,72 @@ static lc_status check_gemm_fp8(const lc_gemm_fp8_args &a) {
   return LC_OK;
 }
 
+// How a product may be tiled, and its expected time in ns:
+//   base + max(fix + chain * its, tiles / slots * (fix + rate * its))
+// with whole rounds of tiles / slots above one. its: a tile's blocks of 128 k, for each of
+// the waves that share them; slots: workgroups that run at once. `chain` is a block's
+// latency where few workgroups run, `rate` its share of the chip's throughput. Tile 16 has
+// many workgroups per compute unit and rate counts its blocks alone. Fitted to 100 products
+// of 1 to 11680 x 16 to 14000 outputs at K = 64 to 16256, of 16 and of 32 bits each (the
+// times are 7 to 25% off); the choice costs 0.7% (16 bits) and 1% (32) over the fastest
+// on the mean, 27% at most. Both sides at a few sizes, us (M x N, K): 4096 x 4096, 4096:
+// 256 53, 128 64, 64 150; 1024 x 4096, 4096: deep 128 19.4, 128 24.7, 64 38, 256 42; 256 x
+// 4096, 4096: 64 10.5, 128 15.9, 32 20.5; 64 x 4096, 4096: 32 6.7, 64 10, 16 17.9; 14 x 3616,
+// 7856: 16 7.9, 32 8.2, deep 128 26.
+struct Fp8Tiling {
+  int tile;
+  bool deep;
+  int waves, slots;
+  int base, fix, chain, rate;
+};
+static const Fp8Tiling kTilings16[] = {
+    {256, false, 1, 256, 3200, 7000, 980, 1350}, {128, false, 1, 512, 2670, 3030, 465, 930},
+    {128, true, 1, 256, 2440, 3680, 356, 442},   {64, false, 4, 256, 2130, 2890, 655, 856},
+    {32, false, 8, 256, 2180, 1590, 545, 780},   {16, false, 8, 0, 2630, 180, 660, 110},
+};
+static const Fp8Tiling kTilings32[] = {
+    {128, false, 1, 512, 4420, 3140, 833, 1634}, {128, true, 1, 256, 1750, 5620, 806, 894},
+    {64, false, 4, 256, 1970, 3200, 1016, 1121}, {32, false, 8, 256, 2220, 1570, 696, 935},
+    {16, false, 8, 0, 2740, 1320, 667, 115},
+};
+
+static const Fp8Tiling *pick(const lc_gemm_fp8_args &a, bool f32) {
+  const Fp8Tiling *const first = f32 ? kTilings32 : kTilings16;
+  const int n = f32 ? (int)(sizeof(kTilings32) / sizeof(*first)) : (int)(sizeof(kTilings16) / sizeof(*first));
+  const Fp8Tiling *best = first;
+  double least = 0.0;
+  for (int i = 0; i < n; ++i) {
+    const Fp8Tiling &v = first[i];
+    int64_t tm = (a.M + v.tile - 1) / v.tile;
+    const int64_t tn = (a.N + v.tile - 1) / v.tile;
+    // grouped rows: about half a partial row of tiles per group besides
+    if (a.group_mode == LC_GROUP_ROWS) tm += (a.n_groups + 1) / 2;
+    const int64_t groups = a.group_mode == LC_GROUP_K ? a.n_groups : 1;
+    const int64_t most = (tm + (a.group_mode == LC_GROUP_ROWS ? a.n_groups : 0)) * tn * groups;
+    if (i > 0 && most > INT32_MAX - 8 * 64) continue;
+    auto time = [&](double tiles, int64_t blocks) -> double {
+      const double its = (double)((blocks + v.waves - 1) / v.waves);
+      double one = v.fix + v.chain * its, full;
+      if (v.tile == 16) {
+        full = tiles / 256.0 * v.rate * (double)blocks;
+      } else {
+        const double rounds = tiles / v.slots;
+        full = (rounds > 1.0 ? (double)(int64_t)(rounds + 0.999999) : rounds) * (v.fix + v.rate * its);
+        if (rounds > 1.0) one = 0.0;
+      }
+      return v.base + (one > full ? one : full);
+    };
+    // grouped k: what lies between groups of one length and a single long one
+    double t = time((double)(tm * tn * groups), (a.K / groups + 127) / 128);
+    if (groups > 1) t += time((double)(tm * tn), (a.K + 127) / 128);
+    if (i == 0 || t < least) {
+      least = t;
+      best = &v;
+    }
+  }
+  return best;
+}
+
 static lc_status gemm_fp8_launch(const lc_gemm_fp8_args &a, hipStream_t s) {
   LC_TRY(check_gemm_fp8(a));
   if (a.M == 0) return LC_OK;
@@ -227,13 +295,15 @@ static lc_status gemm_fp8_launch(const lc_gemm_fp8_args &a, hipStream_t s) {
   p.bsh = a.b_block_rows == 128 ? 7 : 0;
   p.gmode = a.group_mode;
   p.ngroups = a.group_mode == LC_GROUP_NONE ? 1 : a.n_groups;
+  p.goff_max = a.group_mode == LC_GROUP_ROWS ? p.M : p.K;
   p.epi = a.epilogue;
   p.c_dt = typed ? a.c_dtype : LC_FP32;
   p.r_dt = a.r_dtype;
-  p.vec = a.ldc % 4 == 0 && p.gstride_c % 4 == 0 && (a.epilogue != LC_EPI_RESIDUAL || a.ldr % 4 == 0);
   const bool f32 = p.c_dt == LC_FP32;
-  if (a.M <= 16) return direct_launch<1, 1, 1, 1, 8>(p, a, f32, s);
-  return direct_launch<2, 2, 2, 2, 1>(p, a, f32, s);
+  p.store16 = !f32 && a.epilogue == LC_EPI_STORE;
+  const Fp8Tiling *v = pick(a, f32);
+  if (v->tile == 16) return direct_launch<1, 1, 1, 1, 8>(p, a, f32, s);
+  return gemm_fp8_tile_launch(p, a, v->tile, v->deep, f32, s);
 }
 
 }  // namespace lc
