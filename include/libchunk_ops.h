@@ -572,7 +572,7 @@ lc_status lc_moe_dispatch(const lc_moe_args *args, void *stream);
  * Sums are fp32 and of fixed order (partial sums in `scratch`,
  * lc_moe_balance_scratch_bytes, no clearing needed). dn and dwr_accum may each be NULL.
  * n_dtype, w_dtype (wr), dn_dtype and dres_dtype: LC_FP32, LC_BF16 or LC_FP16. d a
- * multiple of 8; 0 <= T < 2^30 (0: counts, loss and a stored dwr_accum are 0). Overlap:
+ * multiple of 8, up to 2^20; 0 <= T < 2^30 (0: counts, loss and a stored dwr_accum are 0). Overlap:
  * dn may lie over dres, element for element (the same type); no other output may
  * overlap a tensor that the call reads. */
 typedef struct lc_moe_balance_args {

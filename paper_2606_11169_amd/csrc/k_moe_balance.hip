@@ -49,31 +49,41 @@ __device__ __forceinline__ void split_bf16(float x, uint16_t (&out)[P]) {
   }
 }
 
-// 8 values at base[idx] as P MFMA fragments
+// 8 values of type DT as they lie in memory
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_v;
 template <int DT>
-__device__ __forceinline__ void load_pieces(const void *base, int64_t idx, bool ok, bf16x8_v (&out)[kPieces<DT>]) {
-  constexpr int P = kPieces<DT>;
-  if constexpr (P == 1) {
-    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_v;
-    u32x4_v v = u32x4_v{0, 0, 0, 0};
-    if (ok) v = *reinterpret_cast<const u32x4_v *>(static_cast<const bf16_t *>(base) + idx);
-    out[0] = __builtin_bit_cast(bf16x8_v, v);
-  } else {
-    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (ok) load8_dt(base, idx, DT, x);
-    typedef __attribute__((ext_vector_type(8))) uint16_t u16x8_v;
-    u16x8_v v[P];
+struct Raw8 {
+  static constexpr int W = DT == LC_FP32 ? 2 : 1;
+  u32x4_v w[W];
+  // byte offset `off` of a buffer; zeros past its end
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      uint16_t s[P];
-      split_bf16<P>(x[c], s);
-#pragma unroll
-      for (int i = 0; i < P; ++i) v[i][c] = s[i];
-    }
-#pragma unroll
-    for (int i = 0; i < P; ++i) out[i] = __builtin_bit_cast(bf16x8_v, v[i]);
+    for (int i = 0; i < W; ++i)
+      w[i] = __builtin_bit_cast(u32x4_v, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(off + 16 * i), 0, 0));
   }
-}
+  // as bf16 pieces
+  __device__ __forceinline__ void pieces(bf16x8_v (&out)[kPieces<DT>]) const {
+    constexpr int P = kPieces<DT>;
+    if constexpr (P == 1) {
+      out[0] = __builtin_bit_cast(bf16x8_v, w[0]);
+    } else {
+      typedef __attribute__((ext_vector_type(8))) uint16_t u16x8_v;
+      u16x8_v v[P];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        float x;
+        if constexpr (DT == LC_FP32) x = __uint_as_float(w[c >> 2][c & 3]);
+        else x = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[0][c >> 1] >> (16 * (c & 1))));
+        uint16_t s[P];
+        split_bf16<P>(x, s);
+#pragma unroll
+        for (int i = 0; i < P; ++i) v[i][c] = s[i];
+      }
+#pragma unroll
+      for (int i = 0; i < P; ++i) out[i] = __builtin_bit_cast(bf16x8_v, v[i]);
+    }
+  }
+};
 
 // acc += a b over the pieces, smallest products first
 template <int PA, int PB>
@@ -88,205 +98,245 @@ __device__ __forceinline__ f32x4_v mul_pieces(const bf16x8_v (&a)[PA], const bf1
   return acc;
 }
 
-constexpr int kFwdTokens = 32;   // tokens per tile
-constexpr int kFwdBlocks = 256;  // partial sums at most
+constexpr int kFwdBlocks = 512;  // workgroups of the forward, and partial sums, at most
 
-// Sums of the partial sums part[nblk][2 E + 2] (P_e, counts, sum of lse^2, N), the loss
-// and the counts; by one workgroup of 256 threads.
-__device__ void balance_finish(const BalanceP &p, int nblk, float *sp, int *sc) {
-  const int tid = threadIdx.x, ld = 2 * p.E + 2;
-  const int col = tid & 63, sl = tid >> 6;
-  __syncthreads();
-  // thread (col, sl): its quarter of the blocks, in order; then the quarters in order
-  double ps = 0.0, zs = 0.0;
-  int cs = 0, ns = 0;
-  const int b0 = (int)((int64_t)nblk * sl / 4), b1 = (int)((int64_t)nblk * (sl + 1) / 4);
-  for (int b = b0; b < b1; ++b) {
-    const float *q = p.part + (int64_t)b * ld;
-    if (col < p.E) {
-      ps += q[col];
-      cs += __float_as_int(q[p.E + col]);
-    }
-    if (col == 0) {
-      zs += q[2 * p.E];
-      ns += __float_as_int(q[2 * p.E + 1]);
-    }
-  }
-  double *const dp = reinterpret_cast<double *>(sp);  // [4][64], then 4 of z
-  dp[tid] = ps;
-  sc[tid] = cs;
-  if (col == 0) {
-    dp[256 + sl] = zs;
-    sc[256 + sl] = ns;
-  }
-  __syncthreads();
-  if (tid < 64) {
-    double a = dp[tid], z = dp[256];
-    int c = sc[tid], N = sc[256];
-    for (int s = 1; s < 4; ++s) {
-      a += dp[64 * s + tid];
-      c += sc[64 * s + tid];
-      z += dp[256 + s];
-      N += sc[256 + s];
-    }
-    double l = tid < p.E ? a * c : 0.0;
+// Sums of the partial sums part[2 E + 2][kFwdBlocks] (sums of probs, counts, sum of lse^2,
+// N), the loss and the counts; by one workgroup, 8 lanes for each entry, every one of them
+// reading whole lines of blocks in turn. In 64 bits: once per call.
+__global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceP p, int nblk) {
+  __shared__ double sums[136];
+  const int lane = threadIdx.x & 63, j = threadIdx.x & 7, n = 2 * p.E + 2;
+  for (int e = threadIdx.x >> 3; e < n; e += 128) {
+    const bool whole = (e >= p.E && e < 2 * p.E) || e == n - 1;  // a count: an integer's bits
+    double s = 0.0;
+    for (int b0 = 0; b0 < nblk; b0 += 256) {
+      float4 v[8];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-    if (tid < p.E) p.counts[tid] = c;
-    if (tid == 0) {
-      p.counts[p.E] = N;
-      const double n = N;
-      p.loss[0] = N > 0 ? (float)(p.E * l / (2.0 * n * n)) : 0.0f;
-      p.loss[1] = N > 0 ? (float)(z / n) : 0.0f;
+      for (int u = 0; u < 8; ++u)
+        v[u] = *reinterpret_cast<const float4 *>(p.part + e * kFwdBlocks + b0 + 32 * u + 4 * j);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (b0 + 32 * u + 4 * j + i < nblk) s += whole ? (double)__float_as_int(w[i]) : (double)w[i];
+      }
     }
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) s += __shfl_xor(s, o, 64);
+    if (j == 0) sums[e] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  const int e = min(lane, p.E - 1);
+  const double N = sums[n - 1];
+  double l = lane < p.E ? sums[e] * sums[p.E + e] : 0.0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+  if (lane < p.E) p.counts[lane] = (int)sums[p.E + e];
+  if (lane == 0) {
+    p.counts[p.E] = (int)N;
+    p.loss[0] = N > 0.0 ? (float)(p.E * l / (2.0 * N * N)) : 0.0f;
+    p.loss[1] = N > 0.0 ? (float)(sums[n - 2] / N) : 0.0f;
   }
 }
 
-__global__ __launch_bounds__(256) void balance_finish_kernel(BalanceP p, int nblk) {
-  __shared__ __align__(16) float sp[2 * 260];
-  __shared__ int sc[260];
-  balance_finish(p, nblk, sp, sc);
-}
-
-// A workgroup takes tiles of 32 tokens: its four waves split d (64 values in turn), and
-// the waves' logits are added in LDS in wave order. EF: experts / 16, rounded up.
-template <int ND, int WD, int EF>
-__global__ __launch_bounds__(256) void balance_fwd_kernel(BalanceP p) {
-  constexpr int LD = 16 * EF + 4;  // a token's logits in LDS
-  __shared__ __align__(16) float sl[4][kFwdTokens * LD];
-  __shared__ float sz[kFwdTokens];
+// A workgroup of 8 waves takes tiles of 16 MT tokens. The waves split d, 64 values (whole
+// lines of bf16) in turn, the next ones' loads under way while one multiplies; their logits
+// are added in LDS in a fixed order. Large tiles read Wr (from L2) less often, small ones
+// fill the chip at fewer tokens. EF: experts / 16, rounded up.
+template <int ND, int WD, int EF, int MT>
+__global__ __launch_bounds__(512) void balance_fwd_kernel(BalanceP p) {
+  constexpr int TT = 16 * MT, LD = 16 * EF + 4;  // tokens; a token's logits in LDS
+  __shared__ __align__(16) float sl[4][TT * LD];
+  __shared__ float sz[TT], sps[8][64];
   __shared__ int scnt[65];
-  static_assert(sizeof(sl) >= 5200, "balance_finish's sums");
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int i16 = lane & 15, g = lane >> 4;
   if (tid < 65) scnt[tid] = 0;
   float psum = 0.0f, zsum = 0.0f;  // thread e: the workgroup's sum of probs; thread 0: of lse^2
   for (int64_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
-    const int64_t t0 = tile * kFwdTokens;
-    f32x4_v acc[2][EF];
+    const int64_t t0 = tile * TT;
+    f32x4_v acc[MT][EF];
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int a = 0; a < MT; ++a)
 #pragma unroll
       for (int b = 0; b < EF; ++b) acc[a][b] = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k0 = wave * 64; k0 < p.d; k0 += 256) {
+    // Steps of 32 of d; n's rows (from HBM) are read four steps ahead (two where registers
+    // end), Wr's (from L2) two.
+    // A wave's step s: values 512 (s / 2) + 64 wave + 32 (s % 2) ..
+    constexpr int AHEAD = MT * EF > 16 ? 2 : 4;
+    Raw8<ND> ra[AHEAD][MT];
+    Raw8<WD> rb[2][EF];
+    // in a workgroup that starts at 0; others start elsewhere and wrap round, so that they do
+    // not all read the same lines of Wr at once.
+    const int turns = (p.d + 511) / 512, start = blockIdx.x % turns;
+    auto first = [&](int s) {
+      const int turn = s >> 1;
+      return turn < turns ? 512 * (turn + start - (turn + start >= turns ? turns : 0)) + 64 * wave + 32 * (s & 1) + 8 * g : p.d;
+    };
+    constexpr int NS = ND == LC_FP32 ? 4 : 2, WS = WD == LC_FP32 ? 4 : 2;
+    const int rows = (int)min(p.T - t0, (int64_t)TT);
+    const auto rn = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char *>(static_cast<const char *>(p.n) + t0 * p.d * NS), 0, rows * p.d * NS, 0x00020000);
+    const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p.wr), 0, p.E * p.d * WS, 0x00020000);
+    auto fetch_a = [&](Raw8<ND> (&x)[MT], int k) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = k0 + 32 * h + 8 * g;
-        bf16x8_v fa[2][kPieces<ND>], fb[EF][kPieces<WD>];
+      for (int a = 0; a < MT; ++a)
+        x[a].load(rn, k < p.d ? (uint32_t)((16 * a + i16) * p.d + k) * NS : 0x80000000u);
+    };
+    auto fetch_b = [&](Raw8<WD> (&x)[EF], int k) {
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const int64_t t = t0 + 16 * a + i16;
-          const bool ok = t < p.T && k < p.d;
-          load_pieces<ND>(p.n, ok ? t * p.d + k : 0, ok, fa[a]);
-        }
+      for (int b = 0; b < EF; ++b) x[b].load(rw, k < p.d ? (uint32_t)((16 * b + i16) * p.d + k) * WS : 0x80000000u);
+    };
+    auto multiply = [&](const Raw8<ND> (&x)[MT], const Raw8<WD> (&y)[EF]) {
+      bf16x8_v fa[MT][kPieces<ND>];
 #pragma unroll
-        for (int b = 0; b < EF; ++b) {
-          const int e = 16 * b + i16;
-          const bool ok = e < p.E && k < p.d;
-          load_pieces<WD>(p.wr, ok ? (int64_t)e * p.d + k : 0, ok, fb[b]);
-        }
+      for (int a = 0; a < MT; ++a) x[a].pieces(fa[a]);
 #pragma unroll
-        for (int a = 0; a < 2; ++a)
+      for (int b = 0; b < EF; ++b) {
+        bf16x8_v fb[kPieces<WD>];
+        y[b].pieces(fb);
 #pragma unroll
-          for (int b = 0; b < EF; ++b) acc[a][b] = mul_pieces(fb[b], fa[a], acc[a][b]);
+        for (int a = 0; a < MT; ++a) acc[a][b] = mul_pieces(fb, fa[a], acc[a][b]);
+      }
+    };
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) fetch_a(ra[s], first(s));
+#pragma unroll
+    for (int s = 0; s < 2; ++s) fetch_b(rb[s], first(s));
+    for (int s0 = 0; s0 < 2 * turns; s0 += 4) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {  // (steps past the last: zeros)
+        multiply(ra[u % AHEAD], rb[u & 1]);
+        fetch_b(rb[u & 1], first(s0 + u + 2));
+        fetch_a(ra[u % AHEAD], first(s0 + u + AHEAD));
       }
     }
-    // lane: token 16 a + i16, experts 16 b + 4 g ..
+    // lane: token 16 a + i16, experts 16 b + 4 g ..; waves 4 to 7 hand theirs to waves 0 to 3
+    auto place = [&](int w, int a, int b) { return reinterpret_cast<f32x4_v *>(&sl[w][(16 * a + i16) * LD + 16 * b + 4 * g]); };
     __syncthreads();  // the last tile's readers are done
+    if (wave >= 4) {
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+      for (int a = 0; a < MT; ++a)
 #pragma unroll
-      for (int b = 0; b < EF; ++b)
-        *reinterpret_cast<f32x4_v *>(&sl[wave][(16 * a + i16) * LD + 16 * b + 4 * g]) = acc[a][b];
+        for (int b = 0; b < EF; ++b) *place(wave - 4, a, b) = acc[a][b];
+    }
+    __syncthreads();
+    if (wave < 4) {
+#pragma unroll
+      for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int b = 0; b < EF; ++b) *place(wave, a, b) = acc[a][b] + *place(wave, a, b);
+    }
     __syncthreads();
     // 8 lanes per token, experts j, j + 8, ...
-    const int tl = tid >> 3, j = tid & 7;
-    const int64_t t = t0 + tl;
-    const bool live = t < p.T && (!p.mask || p.mask[t] != 0);
-    float l[2 * EF], m = -INFINITY, sum = 0.0f;
+    const int j = tid & 7;
+    for (int tl = tid >> 3; tl < TT; tl += 64) {
+      const int64_t t = t0 + tl;
+      const bool live = t < p.T && (!p.mask || p.mask[t] != 0);
+      float l[2 * EF], m = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 2 * EF; ++i) {
-      const int e = j + 8 * i;
-      float v = sl[0][tl * LD + e];
+      for (int i = 0; i < 2 * EF; ++i) {
+        const int e = j + 8 * i;
+        float v = sl[0][tl * LD + e];
 #pragma unroll
-      for (int u = 1; u < 4; ++u) v += sl[u][tl * LD + e];
-      l[i] = v;
-      if (e < p.E) m = v > m || v != v ? v : m;  // (a NaN stays)
-    }
+        for (int u = 1; u < 4; ++u) v += sl[u][tl * LD + e];
+        l[i] = v;
+        if (e < p.E) m = v > m || v != v ? v : m;  // (a NaN stays)
+      }
 #pragma unroll
-    for (int o = 1; o < 8; o *= 2) {
-      const float v = __shfl_xor(m, o, 64);
-      m = v > m || v != v ? v : m;
-    }
+      for (int o = 1; o < 8; o *= 2) {
+        const float v = __shfl_xor(m, o, 64);
+        m = v > m || v != v ? v : m;
+      }
 #pragma unroll
-    for (int i = 0; i < 2 * EF; ++i) {
-      l[i] = j + 8 * i < p.E ? expf(l[i] - m) : 0.0f;
-      sum += l[i];
-    }
+      for (int i = 0; i < 2 * EF; ++i) {
+        l[i] = j + 8 * i < p.E ? expf(l[i] - m) : 0.0f;
+        sum += l[i];
+      }
 #pragma unroll
-    for (int o = 1; o < 8; o *= 2) sum += __shfl_xor(sum, o, 64);
-    const float inv = 1.0f / sum, lse = live ? m + logf(sum) : 0.0f;
-    __syncthreads();  // logits read
+      for (int o = 1; o < 8; o *= 2) sum += __shfl_xor(sum, o, 64);
+      const float inv = 1.0f / sum, lse = live ? m + logf(sum) : 0.0f;
+      // (a token's logits are read and overwritten by its own 8 lanes, which run together)
 #pragma unroll
-    for (int i = 0; i < 2 * EF; ++i) {
-      const int e = j + 8 * i;
-      const float v = live ? l[i] * inv : 0.0f;
-      sl[0][tl * LD + e] = v;
-      if (t < p.T && e < p.E) p.probs[t * p.E + e] = v;
-    }
-    if (j == 0) {
-      sz[tl] = lse * lse;
-      if (t < p.T) p.lse[t] = lse;
-      if (live) {  // (integer counts: any order gives the same)
-        const int a = p.sel[2 * t], b = p.sel[2 * t + 1];
-        if (a >= 0 && a < p.E) atomicAdd(&scnt[a], 1);
-        if (b >= 0 && b < p.E && b != a) atomicAdd(&scnt[b], 1);
-        atomicAdd(&scnt[64], 1);
+      for (int i = 0; i < 2 * EF; ++i) {
+        const int e = j + 8 * i;
+        const float v = live ? l[i] * inv : 0.0f;
+        sl[0][tl * LD + e] = v;
+        if (t < p.T && e < p.E) p.probs[t * p.E + e] = v;
+      }
+      if (j == 0) {
+        sz[tl] = lse * lse;
+        if (t < p.T) p.lse[t] = lse;
+        if (live) {  // (integer counts: any order gives the same)
+          const int a = p.sel[2 * t], b = p.sel[2 * t + 1];
+          if (a >= 0 && a < p.E) atomicAdd(&scnt[a], 1);
+          if (b >= 0 && b < p.E && b != a) atomicAdd(&scnt[b], 1);
+          atomicAdd(&scnt[64], 1);
+        }
       }
     }
     __syncthreads();
-    if (tid < p.E) {
-      float s = 0.0f;
-      for (int i = 0; i < kFwdTokens; ++i) s += sl[0][i * LD + tid];
-      psum += s;
+    {  // wave w: tokens w TT / 8 .. of expert `lane`
+      float v = 0.0f;
+      if (lane < 16 * EF)
+#pragma unroll
+        for (int i = 0; i < TT / 8; ++i) v += sl[0][(wave * (TT / 8) + i) * LD + lane];
+      sps[wave][lane] = v;
     }
-    if (tid == 0) {
-      float s = 0.0f;
-      for (int i = 0; i < kFwdTokens; ++i) s += sz[i];
-      zsum += s;
+    __syncthreads();
+    if (tid < 64) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) psum += sps[u][tid];
+      float z = 0.0f;
+      for (int i = tid; i < TT; i += 64) z += sz[i];
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
+      zsum += z;
     }
   }
   __syncthreads();  // counts
-  float *const q = p.part + (int64_t)blockIdx.x * (2 * p.E + 2);
+  if (gridDim.x == 1 && tid < 64) {  // a single workgroup finishes by itself
+    const int c = scnt[tid], N = scnt[64];
+    double l = tid < p.E ? (double)psum * c : 0.0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+    if (tid < p.E) p.counts[tid] = c;
+    if (tid == 0) {
+      const double n = N;
+      p.counts[p.E] = N;
+      p.loss[0] = N > 0 ? (float)(p.E * l / (2.0 * n * n)) : 0.0f;
+      p.loss[1] = N > 0 ? (float)(zsum / n) : 0.0f;
+    }
+    return;
+  }
+  float *const q = p.part + blockIdx.x;
   if (tid < p.E) {
-    q[tid] = psum;
-    q[p.E + tid] = __int_as_float(scnt[tid]);
+    q[tid * kFwdBlocks] = psum;
+    q[(p.E + tid) * kFwdBlocks] = __int_as_float(scnt[tid]);
   }
   if (tid == 0) {
-    q[2 * p.E] = zsum;
-    q[2 * p.E + 1] = __int_as_float(scnt[64]);
-  }
-  if (gridDim.x == 1) {  // a single workgroup finishes by itself
-    __threadfence_block();
-    balance_finish(p, 1, &sl[0][0], reinterpret_cast<int *>(&sl[0][0]) + 1040);
+    q[2 * p.E * kFwdBlocks] = zsum;
+    q[(2 * p.E + 1) * kFwdBlocks] = __int_as_float(scnt[64]);
   }
 }
 
 constexpr int kBwdTokens = 32;
-constexpr int kBwdCols = 128;
+constexpr int kBwdCols = 256;
 
-// A workgroup takes kBwdCols columns and a split's tokens, 32 at a time. dl of a tile is
-// formed in LDS in three bf16 pieces, [token][expert] for dn = dl Wr and [expert][token]
-// for dWr = dl^T n; Wr's fragments stay in registers for all tiles, dWr's sums too. n's
-// fragments (tokens along k) are transposing LDS reads of the rows.
+// A workgroup of 8 waves takes kBwdCols columns (32 per wave) and a split's tokens, 32 at a
+// time; a tile's loads are under way while the one before is multiplied. dl of a tile is
+// formed in LDS in three bf16 pieces, a row per token: read by rows for dn = dl Wr, with
+// transposing reads (tokens along k) for dWr = dl^T n, n's rows likewise. Wr's fragments
+// stay in registers for all tiles, dWr's sums too. Row r of a fragment b of columns is
+// column 8 (r / 4) + 4 b + r % 4 of the wave's 32, which leaves a lane 8 neighbouring ones.
 template <int ND, int WD, int EF>
-__global__ __launch_bounds__(256) void balance_bwd_kernel(BalanceP p) {
+__global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void balance_bwd_kernel(BalanceP p) {
   constexpr int PN = kPieces<ND>, PW = kPieces<WD>, KE = (EF + 1) / 2;
   constexpr int LE = 32 * KE + 8;  // [token][expert] row
-  constexpr int LT = kBwdTokens + 8;
   constexpr int LN = kBwdCols + 16;
   __shared__ __align__(16) uint16_t s_te[3][kBwdTokens * LE];
-  __shared__ __align__(16) uint16_t s_et[3][16 * EF * LT];
   __shared__ __align__(16) uint16_t s_n[PN][kBwdTokens * LN];
   __shared__ float s_f[64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -299,22 +349,43 @@ __global__ __launch_bounds__(256) void balance_bwd_kernel(BalanceP p) {
   const float rn = N > 0 ? 1.0f / (float)N : 0.0f;
   const float cb = p.coef * p.E * rn, cz = 2.0f * p.z_coef * rn;
   if (tid < 64) s_f[tid] = tid < p.E ? (float)p.counts[tid] * 0.5f * rn : 0.0f;
-  for (int i = tid; i < kBwdTokens * LE; i += 256) s_te[0][i] = s_te[1][i] = s_te[2][i] = 0;
-  for (int i = tid; i < 16 * EF * LT; i += 256) s_et[0][i] = s_et[1][i] = s_et[2][i] = 0;
+  for (int i = tid; i < kBwdTokens * LE; i += 512) s_te[0][i] = s_te[1][i] = s_te[2][i] = 0;
 
-  // Wr fragments: rows columns cw + 16 b + i16, k experts 32 k + 8 g ..
+  // Wr fragments: k experts 32 k + 8 g ..
+  const int colf = 8 * (i16 >> 2) + (i16 & 3);
+  // (16-bit Wr: rows in LDS, read across like n's, which leaves registers for a second
+  // workgroup)
+  constexpr bool WL = PW == 1;
+  __shared__ __align__(16) uint16_t s_w[WL ? 32 * KE * LN : 8];
+  if constexpr (WL) {
+    for (int i = tid; i < 32 * KE * (kBwdCols / 8); i += 512) {
+      const int e = i / (kBwdCols / 8), c = i % (kBwdCols / 8) * 8;
+      u32x4_v v = u32x4_v{0, 0, 0, 0};
+      if (p.dn && e < p.E && c0 + c < p.d)
+        v = *reinterpret_cast<const u32x4_v *>(static_cast<const bf16_t *>(p.wr) + (int64_t)e * p.d + c0 + c);
+      *reinterpret_cast<u32x4_v *>(&s_w[e * LN + c]) = v;
+    }
+  }
+  // each 16 lanes: rows (k) 8 g + i16 / 4 (and + 4), four columns of run i16 % 4
+  auto across = [&](const uint16_t *rows, int ld, int col) -> bf16x8_v {
+    typedef __attribute__((address_space(3))) s16x4_v lds_v4;
+    lds_t *q = LDS_AS(char, const_cast<uint16_t *>(rows + (8 * g + (i16 >> 2)) * ld + col));
+    const s16x4_v v[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)q),
+                          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(q + 4 * ld * 2))};
+    return __builtin_bit_cast(bf16x8_v, v);
+  };
   bf16x8_v fw[2][KE][PW];
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int b = 0; b < 2 && !WL; ++b)
 #pragma unroll
     for (int k = 0; k < KE; ++k) {
       typedef __attribute__((ext_vector_type(8))) uint16_t u16x8_v;
       u16x8_v v[PW];
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        const int e = 32 * k + 8 * g + c, col = cw + 16 * b + i16;
+        const int e = 32 * k + 8 * g + c, col = cw + colf + 4 * b;
         float x = 0.0f;
-        if (e < p.E && col < p.d) {
+        if (p.dn && e < p.E && col < p.d) {
           const int64_t at = (int64_t)e * p.d + col;
           if constexpr (WD == LC_FP32) x = static_cast<const float *>(p.wr)[at];
           else if constexpr (WD == LC_BF16) x = bf2f(static_cast<const bf16_t *>(p.wr)[at]);
@@ -328,120 +399,187 @@ __global__ __launch_bounds__(256) void balance_bwd_kernel(BalanceP p) {
 #pragma unroll
       for (int i = 0; i < PW; ++i) fw[b][k][i] = __builtin_bit_cast(bf16x8_v, v[i]);
     }
-  f32x4_v aw[EF][2];  // dWr: experts 16 a + i16, columns 16 b + 4 g ..
+  f32x4_v aw[EF][2];  // dWr: experts 16 a + i16, columns 8 g + 4 b ..
 #pragma unroll
   for (int a = 0; a < EF; ++a)
 #pragma unroll
     for (int b = 0; b < 2; ++b) aw[a][b] = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
 
-  for (int64_t tile = tile0; tile < tile1; ++tile) {
-    const int64_t t0 = tile * kBwdTokens;
+  // What a thread reads of a tile. dl: token tid / 16, experts 4 (tid % 16) ..; n: rows
+  // tid / 32 and + 16, columns 8 (tid % 32) ..; dres as the products leave dn: token 16 a +
+  // i16, columns 8 g + 4 b ... All of it, and dn's stores, are buffer accesses without a
+  // branch: what is not there lies past the buffer's end. Behind a branch the compiler
+  // cannot count the accesses in flight and waits for all of them, stores too, where it
+  // needs the first.
+  constexpr uint32_t NONE = 0x80000000u;
+  const int tl = tid >> 4, e4 = 4 * (tid & 15), nr = tid >> 5, nc = 8 * (tid & 31);
+  constexpr int NS = ND == LC_FP32 ? 4 : 2;
+  const int rs = p.dres_dt == LC_FP32 ? 4 : 2, os = p.dn_dt == LC_FP32 ? 4 : 2;
+  const uint32_t off_n = c0 + nc < p.d ? (uint32_t)(nr * p.d + c0 + nc) * NS : NONE;
+  const uint32_t off_c = cw + 8 * g < p.d ? (uint32_t)(i16 * p.d + cw + 8 * g) : NONE;  // (in values)
+  auto rows_of = [&](const void *base, int64_t tile, int have, int64_t width, int size) {
+    return __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char *>(static_cast<const char *>(base) + tile * kBwdTokens * width * size), 0,
+        base ? (int)(have * width * size) : 0, 0x00020000);
+  };
+  auto have_of = [&](int64_t tile) {
+    return tile < tile1 ? (int)min(p.T - tile * kBwdTokens, (int64_t)kBwdTokens) : 0;
+  };
+  struct Tile {
+    uint32_t pr[4], lse;
+    uint64_t sel, w, dw;  // pairs
+    uint8_t mask, mask_n[2];
+    Raw8<ND> n[2];
+  };
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_v;
+  auto fetch = [&](Tile &x, int64_t tile) {
+    const int have = have_of(tile);
+    const auto m = rows_of(p.mask, tile, have, 1, 1);
+    x.mask = __builtin_amdgcn_raw_buffer_load_b8(m, tl, 0, 0);
+    const auto q = rows_of(p.dw ? p.sel : nullptr, tile, have, 2, 4), w = rows_of(p.w, tile, have, 2, 4),
+               dw = rows_of(p.dw, tile, have, 2, 4);
+    x.sel = __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(q, 8 * tl, 0, 0));
+    x.w = __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(w, 8 * tl, 0, 0));
+    x.dw = __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(dw, 8 * tl, 0, 0));
+    x.lse = __builtin_amdgcn_raw_buffer_load_b32(rows_of(p.lse, tile, have, 1, 4), 4 * tl, 0, 0);
+    const auto pr = rows_of(p.probs, tile, have, p.E, 4);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      x.pr[c] = __builtin_amdgcn_raw_buffer_load_b32(pr, e4 + c < p.E ? (uint32_t)(tl * p.E + e4 + c) * 4 : NONE, 0, 0);
+    const auto n = rows_of(p.dwr ? p.n : nullptr, tile, have, p.d, NS);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      x.mask_n[u] = __builtin_amdgcn_raw_buffer_load_b8(m, nr + 16 * u, 0, 0);
+      x.n[u].load(n, off_n + (off_n == NONE ? 0u : (uint32_t)(16 * u * p.d) * NS));
+    }
+  };
+  u32x4_v res[2][2];  // eight values: one word of 16-bit ones, two of fp32
+  auto fetch_res = [&](int64_t tile) {
+    const auto r = rows_of(p.dn ? p.dres : nullptr, tile, have_of(tile), p.d, rs);
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const uint32_t at = off_c == NONE ? NONE : (off_c + (uint32_t)(16 * a * p.d)) * rs;
+      res[a][0] = __builtin_bit_cast(u32x4_v, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, 0));
+      if (rs == 4) res[a][1] = __builtin_bit_cast(u32x4_v, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(at + 16), 0, 0));
+    }
+  };
+  auto add_res = [&](float (&v)[8], const u32x4_v (&r)[2]) {
+    if (p.dres_dt == LC_FP32) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) v[c] += __uint_as_float(r[c >> 2][c & 3]);
+    } else if (p.dres_dt == LC_BF16) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) v[c] += __uint_as_float(c & 1 ? r[0][c >> 1] & 0xFFFF0000u : r[0][c >> 1] << 16);
+    } else {
+      const f16x8_v h = __builtin_bit_cast(f16x8_v, r[0]);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) v[c] += (float)h[c];
+    }
+  };
+  auto work = [&](Tile &x, int64_t tile) {
+    const int have = have_of(tile);
     __syncthreads();  // the last tile's fragments are read
-    {  // dl: 8 lanes per token, experts 8 j .. 8 j + 7
-      const int tl = tid >> 3, j = tid & 7;
-      const int64_t t = t0 + tl;
-      const bool live = t < p.T && (!p.mask || p.mask[t] != 0);
-      float pr[8], dot = 0.0f;
+    {
+      const bool live = tl < have && (!p.mask || x.mask != 0);
+      float pr[4], dot = 0.0f;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const int e = 8 * j + c;
-        pr[c] = live && e < p.E ? p.probs[t * p.E + e] : 0.0f;
-        dot += pr[c] * s_f[e];
+      for (int c = 0; c < 4; ++c) {
+        pr[c] = live ? __uint_as_float(x.pr[c]) : 0.0f;
+        dot += pr[c] * s_f[e4 + c];
       }
 #pragma unroll
-      for (int o = 1; o < 8; o *= 2) dot += __shfl_xor(dot, o, 64);
-      const float z = live ? cz * p.lse[t] : 0.0f;
-      int e0 = -1, e1 = -1;
-      float g0 = 0.0f, g1 = 0.0f;
-      if (live && p.dw) {
-        e0 = p.sel[2 * t];
-        e1 = p.sel[2 * t + 1];
-        if (e0 < 0 || e0 >= p.E) e0 = -1;
-        if (e1 < 0 || e1 >= p.E || e1 == p.sel[2 * t]) e1 = -1;
-        const float w0 = e0 >= 0 ? p.w[2 * t] : 0.0f, w1 = e1 >= 0 ? p.w[2 * t + 1] : 0.0f;
-        const float d0 = e0 >= 0 ? p.dw[2 * t] : 0.0f, d1 = e1 >= 0 ? p.dw[2 * t + 1] : 0.0f;
-        const float inner = w0 * d0 + w1 * d1;
-        g0 = w0 * (d0 - inner);
-        g1 = w1 * (d1 - inner);
-      }
-      if (8 * j < 16 * EF) {
+      for (int o = 1; o < 16; o *= 2) dot += __shfl_xor(dot, o, 64);
+      const float z = live ? cz * __uint_as_float(x.lse) : 0.0f;
+      const int e0 = (int)(uint32_t)x.sel, e1 = (int)(x.sel >> 32);
+      const bool pair = live && p.dw, ok0 = pair && e0 >= 0 && e0 < p.E, ok1 = pair && e1 >= 0 && e1 < p.E && e1 != e0;
+      const float w0 = ok0 ? __uint_as_float((uint32_t)x.w) : 0.0f, w1 = ok1 ? __uint_as_float((uint32_t)(x.w >> 32)) : 0.0f;
+      const float d0 = ok0 ? __uint_as_float((uint32_t)x.dw) : 0.0f, d1 = ok1 ? __uint_as_float((uint32_t)(x.dw >> 32)) : 0.0f;
+      const float inner = w0 * d0 + w1 * d1, g0 = w0 * (d0 - inner), g1 = w1 * (d1 - inner);
+      if (e4 < 16 * EF) {
+        uint16_t s[4][3];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const int e = 8 * j + c;
+        for (int c = 0; c < 4; ++c) {
+          const int e = e4 + c;
           float v = pr[c] * (cb * (s_f[e] - dot) + z);
-          v += e == e0 ? g0 : e == e1 ? g1 : 0.0f;
+          v += ok0 && e == e0 ? g0 : ok1 && e == e1 ? g1 : 0.0f;
           if (!live || e >= p.E) v = 0.0f;
-          uint16_t s[3];
-          split_bf16<3>(v, s);
+          split_bf16<3>(v, s[c]);
+        }
 #pragma unroll
-          for (int i = 0; i < 3; ++i) {
-            s_te[i][tl * LE + e] = s[i];
-            s_et[i][e * LT + tl] = s[i];
-          }
+        for (int i = 0; i < 3; ++i) {
+          *reinterpret_cast<uint2 *>(&s_te[i][tl * LE + e4]) =
+              make_uint2(s[0][i] | (uint32_t)s[1][i] << 16, s[2][i] | (uint32_t)s[3][i] << 16);
         }
       }
     }
-    if (p.dwr) {  // n: 16 lanes per token, 8 columns each
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int tl = 16 * u + (tid >> 4), c = 8 * (tid & 15);
-        const int64_t t = t0 + tl;
-        const bool ok = t < p.T && c0 + c < p.d && (!p.mask || p.mask[t] != 0);
-        bf16x8_v f[PN];
-        load_pieces<ND>(p.n, ok ? t * p.d + c0 + c : 0, ok, f);
+    for (int u = 0; u < 2; ++u) {
+      bf16x8_v f[PN];
+      x.n[u].pieces(f);
+      const bool live = !p.mask || x.mask_n[u] != 0;
 #pragma unroll
-        for (int i = 0; i < PN; ++i) *reinterpret_cast<bf16x8_v *>(&s_n[i][tl * LN + c]) = f[i];
-      }
+      for (int i = 0; i < PN; ++i)
+        *reinterpret_cast<u32x4_v *>(&s_n[i][(nr + 16 * u) * LN + nc]) =
+            live ? __builtin_bit_cast(u32x4_v, f[i]) : u32x4_v{0, 0, 0, 0};
     }
+    fetch(x, tile + 1);
     __syncthreads();
-    if (p.dwr) {
-      bf16x8_v fn[2][PN];  // columns 16 b + i16, tokens 8 g ..
+    {
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {  // tokens 16 a + i16
+        f32x4_v s[2] = {f32x4_v{0.0f, 0.0f, 0.0f, 0.0f}, f32x4_v{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+        for (int k = 0; k < KE; ++k) {
+          bf16x8_v fd[3];
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            fd[i] = *reinterpret_cast<const bf16x8_v *>(&s_te[i][(16 * a + i16) * LE + 32 * k + 8 * g]);
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            if constexpr (WL) fw[b][k][0] = across(s_w + 32 * k * LN, LN, 32 * wave + 8 * (i16 & 3) + 4 * b);
+            s[b] = mul_pieces(fw[b][k], fd, s[b]);
+          }
+        }
+        const auto out = rows_of(p.dn, tile, have, p.d, os);
+        float v[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]};
+        add_res(v, res[a]);
+        const uint32_t at = off_c == NONE ? NONE : (off_c + (uint32_t)(16 * a * p.d)) * os;
+        if (p.dn_dt == LC_FP32) {
+          const f32x4_v lo = f32x4_v{v[0], v[1], v[2], v[3]}, hi = f32x4_v{v[4], v[5], v[6], v[7]};
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_v, lo), out, (int)at, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_v, hi), out, (int)(at + 16), 0, 0);
+        } else if (p.dn_dt == LC_BF16) {
+          const bf16x8_v o = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3],
+                              (__bf16)v[4], (__bf16)v[5], (__bf16)v[6], (__bf16)v[7]};
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_v, o), out, (int)at, 0, 0);
+        } else {
+          const f16x8_v o = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3],
+                             (_Float16)v[4], (_Float16)v[5], (_Float16)v[6], (_Float16)v[7]};
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_v, o), out, (int)at, 0, 0);
+        }
+      }
+      fetch_res(tile + 1);
+    }
+    {
+      bf16x8_v fn[2][PN];
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < PN; ++i) {
-          // each 16 lanes: rows 8 g + i16 / 4 (and + 4), columns 4 (i16 % 4) ..
-          lds_t *q = LDS_AS(char, &s_n[i][(8 * g + (i16 >> 2)) * LN + 32 * wave + 16 * b + 4 * (i16 & 3)]);
-          typedef __attribute__((address_space(3))) s16x4_v lds_v4;
-          const s16x4_v v[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)q),
-                                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(q + 4 * LN * 2))};
-          fn[b][i] = __builtin_bit_cast(bf16x8_v, v);
-        }
+        for (int i = 0; i < PN; ++i) fn[b][i] = across(s_n[i], LN, 32 * wave + 8 * (i16 & 3) + 4 * b);
 #pragma unroll
       for (int a = 0; a < EF; ++a) {
         bf16x8_v fd[3];
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-          fd[i] = *reinterpret_cast<const bf16x8_v *>(&s_et[i][(16 * a + i16) * LT + 8 * g]);
+        for (int i = 0; i < 3; ++i) fd[i] = across(s_te[i], LE, 16 * a + 4 * (i16 & 3));
 #pragma unroll
         for (int b = 0; b < 2; ++b) aw[a][b] = mul_pieces(fn[b], fd, aw[a][b]);
       }
     }
-    if (p.dn) {
-#pragma unroll
-      for (int a = 0; a < 2; ++a) {  // tokens 16 a + i16
-        bf16x8_v fd[KE][3];
-#pragma unroll
-        for (int k = 0; k < KE; ++k)
-#pragma unroll
-          for (int i = 0; i < 3; ++i)
-            fd[k][i] = *reinterpret_cast<const bf16x8_v *>(&s_te[i][(16 * a + i16) * LE + 32 * k + 8 * g]);
-        const int64_t t = t0 + 16 * a + i16;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int col = cw + 16 * b + 4 * g;
-          const bool ok = t < p.T && col < p.d;
-          const int64_t at = ok ? t * p.d + col : 0;
-          float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          if (ok && p.dres) x = load4_dt(p.dres, at, p.dres_dt);
-          f32x4_v s = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int k = 0; k < KE; ++k) s = mul_pieces(fw[b][k], fd[k], s);
-          if (ok) store4_dt(p.dn, at, p.dn_dt, x.x + s[0], x.y + s[1], x.z + s[2], x.w + s[3]);
-        }
-      }
-    }
-  }
+  };
+  Tile x;
+  fetch(x, tile0);
+  fetch_res(tile0);
+  for (int64_t tile = tile0; tile < tile1; ++tile) work(x, tile);
   if (p.dwr) {
     float *const out = p.splits > 1 ? p.part + (int64_t)split * p.E * p.d : p.dwr;
     const bool add = p.splits == 1 && !p.store;
@@ -449,7 +587,7 @@ __global__ __launch_bounds__(256) void balance_bwd_kernel(BalanceP p) {
     for (int a = 0; a < EF; ++a)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int e = 16 * a + i16, col = cw + 16 * b + 4 * g;
+        const int e = 16 * a + i16, col = cw + 8 * g + 4 * b;
         if (e >= p.E || col >= p.d) continue;
         float4 *q = reinterpret_cast<float4 *>(out + (int64_t)e * p.d + col);
         float4 v = make_float4(aw[a][b][0], aw[a][b][1], aw[a][b][2], aw[a][b][3]);
@@ -490,10 +628,10 @@ __global__ __launch_bounds__(256) void balance_dwr_kernel(BalanceP p) {
   *out = s;
 }
 
-// Parts of the tokens in the backward: enough workgroups to fill the chip twice
+// Parts of the tokens in the backward: as many workgroups as run at once, two per compute unit
 int bwd_splits(int64_t T, int64_t d) {
   const int64_t chunks = (d + kBwdCols - 1) / kBwdCols, tiles = (T + kBwdTokens - 1) / kBwdTokens;
-  const int64_t want = (512 + chunks - 1) / chunks;
+  const int64_t want = chunks < 512 ? 512 / chunks : 1;
   return (int)(tiles < 1 ? 1 : tiles < want ? tiles : want);
 }
 
@@ -518,7 +656,7 @@ static lc_status check_balance(const lc_moe_balance_args &a, bool backward) {
   if (a.T < 0 || a.d <= 0 || a.E < 2 || a.E > 64)
     return fail(LC_ERR_INVALID_ARG, "moe balance: need T >= 0, d > 0 and 2 <= E <= 64");
   if (a.T >= ((int64_t)1 << 30)) return fail(LC_ERR_UNSUPPORTED, "moe balance: too many tokens");
-  if (a.d % 8) return fail(LC_ERR_UNSUPPORTED, "moe balance: d %% 8 != 0");
+  if (a.d % 8 || a.d > (1 << 20)) return fail(LC_ERR_UNSUPPORTED, "moe balance: d %% 8 != 0 or d > 2^20");
   if (!valid_dtype(a.n_dtype) || !valid_dtype(a.w_dtype))
     return fail(LC_ERR_INVALID_ARG, "moe balance: unknown dtype");
   if (!a.counts || !aligned16(a.counts) || (!backward && (!a.loss || !aligned16(a.loss))))
@@ -575,21 +713,41 @@ static BalanceP balance_params(const lc_moe_balance_args &a) {
 static lc_status balance_forward(const lc_moe_balance_args &a, hipStream_t s) {
   LC_TRY(check_balance(a, false));
   BalanceP p = balance_params(a);
-  p.tiles = (a.T + kFwdTokens - 1) / kFwdTokens;
+  // Tokens per tile / 16: the least rounds of tiles over the compute units by a tile's
+  // expected time, which grows with its tokens and by 2 tokens' worth for its reads of Wr.
+  // Tiles of more than 32 tokens are for bf16 (the others' registers end there).
+  const bool wide = a.n_dtype == LC_BF16 && a.w_dtype == LC_BF16;
+  int mt = 1;
+  int64_t least = 0;
+  for (int m : {1, 2, 4, 5}) {
+    if (m > 2 && !wide) break;
+    const int64_t tiles = (a.T + 16 * m - 1) / (16 * m), time = (tiles + 255) / 256 * (m + 2);
+    if (m == 1 || time < least) {
+      least = time;
+      mt = m;
+    }
+  }
+  p.tiles = (a.T + 16 * mt - 1) / (16 * mt);
   const int nblk = (int)(p.tiles < kFwdBlocks ? p.tiles : kFwdBlocks);
   if (nblk > 0) {
     with_dtype(a.n_dtype, [&](auto nd) {
       with_dtype(a.w_dtype, [&](auto wd) {
         with_experts(a.E, [&](auto ef) {
-          hipLaunchKernelGGL((balance_fwd_kernel<decltype(nd)::value, decltype(wd)::value, decltype(ef)::value>),
-                             dim3((unsigned)nblk), dim3(256), 0, s, p);
+          constexpr int ND = decltype(nd)::value, WD = decltype(wd)::value, EF = decltype(ef)::value;
+          const dim3 grid((unsigned)nblk), threads(512);
+          if constexpr (ND == LC_BF16 && WD == LC_BF16) {
+            if (mt == 4) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 4>), grid, threads, 0, s, p);
+            if (mt == 5) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 5>), grid, threads, 0, s, p);
+          }
+          if (mt == 2) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 2>), grid, threads, 0, s, p);
+          if (mt == 1) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 1>), grid, threads, 0, s, p);
         });
       });
     });
     LC_TRY(check_launch("balance_fwd_kernel"));
   }
   if (nblk == 1) return LC_OK;
-  hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(256), 0, s, p, nblk);
+  hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(1024), 0, s, p, nblk);
   return check_launch("balance_finish_kernel");
 }
 
@@ -608,7 +766,7 @@ static lc_status balance_backward(const lc_moe_balance_args &a, hipStream_t s) {
     with_dtype(a.w_dtype, [&](auto wd) {
       with_experts(a.E, [&](auto ef) {
         hipLaunchKernelGGL((balance_bwd_kernel<decltype(nd)::value, decltype(wd)::value, decltype(ef)::value>),
-                           dim3(grid), dim3(256), 0, s, p);
+                           dim3(grid), dim3(512), 0, s, p);
       });
     });
   });
