@@ -7,12 +7,12 @@
 // From a's bits, a = 1.f * 2^(e - 127): s = e - 8 (15), one more where f > 0.75. The
 // scaling by a power of two is exact, so the only rounding is the conversion's.
 //
-// A workgroup of 256 threads takes a tile of 128 x 128 values: thread (tx, ty) of 16 x
-// 16 holds 8 rows (8 ty ..) of 8 columns (8 tx ..) in registers, read once for both
+// A workgroup of 512 threads takes a tile of 128 x 128 values: thread (tx, ty) of 16 x
+// 32 holds 4 rows (4 ty ..) of 8 columns (8 tx ..) in registers, read once for both
 // layouts. A row block's 128 values sit in the 16 lanes of a DPP row (largest value in
-// four DPP steps); a column block's in the 16 thread rows (through LDS). Row layout: 8
-// bytes per lane and row, 128-byte lines. Column layout: a thread's 8 rows of a column
-// are 8 bytes in LDS, read back as whole 128-byte lines. 16-bit inputs find their
+// four DPP steps); a column block's in the 32 thread rows (through LDS). Row layout: 8
+// bytes per lane and row, 128-byte lines. Column layout: a thread's 4 rows of a column
+// are a word in LDS, read back as whole 128-byte lines. 16-bit inputs find their
 // largest values two at a time on the bit patterns (v_pk_max_u16: magnitudes order as
 // integers, and unlike a floating maximum a signalling NaN does not swallow the rest).
 #include "common.hpp"
@@ -78,16 +78,21 @@ __device__ __forceinline__ float half_value(uint32_t bits16) {
 }
 
 constexpr int kColRow = 144;  // bytes of a column's 128 in LDS, with padding
+constexpr int R = 4;           // rows of a thread
 
 // XD: type of x; W: rows are weighted; E5: e5m2, else e4m3; SQ: blocks of 128 x 128
 template <int XD, bool W, bool E5, bool SQ>
-__global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t first) {
-  constexpr bool H = XD != LC_FP32 && !W;  // values stay pairs of 16 bits
-  constexpr int NW = H ? 4 : 8;            // words of 8 values
-  constexpr uint32_t INF = !H ? 0x7F800000u : XD == LC_BF16 ? 0x7F80u : 0x7C00u;
+__global__ __launch_bounds__(512) void fp8_quantize_kernel(QuantP p, uint32_t first) {
+  constexpr bool H = XD != LC_FP32;  // values stay pairs of 16 bits in registers
+  constexpr bool P = H && !W;        // and their magnitudes are compared as such
+  constexpr int NW = H ? 4 : 8;      // words of 8 values
+  constexpr int NM = P ? 4 : 8;      // words of 8 magnitudes
+  constexpr uint32_t INF = !P ? 0x7F800000u : XD == LC_BF16 ? 0x7F80u : 0x7C00u;
   __shared__ __align__(16) uint8_t tile8[128 * kColRow];
-  __shared__ __align__(16) uint32_t cmax[16][16 * NW];
   __shared__ __align__(16) uint8_t cexp[128];
+  // (the thread rows' maxima are read before the tile's bytes are written)
+  auto cmax = reinterpret_cast<uint32_t(*)[16 * NM]>(tile8);
+  static_assert(sizeof(tile8) >= 32 * 16 * NM * 4, "maxima of 32 thread rows");
 
   const int tid = threadIdx.x, lane = tid & 63, tx = tid & 15, ty = tid >> 4;
   const uint32_t wg = first + blockIdx.x;
@@ -137,18 +142,18 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t fi
   const int c0 = ct * 128 + tx * 8;
 
   // ---- the thread's 8 x 8 values
-  uint32_t w[8][NW];
+  uint32_t w[R][NW];
+  float wt[R];  // the rows' weights
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t r = r0 + 8 * ty + i;
+  for (int i = 0; i < R; ++i) {
+    const int64_t r = r0 + R * ty + i;
     int64_t src = r;
     bool ok = r < rlim && c0 < p.d;
     if (ok && p.index) {
       src = p.index[r];
       ok = src >= 0 && src < p.x_rows;
     }
-    float wt = 1.0f;
-    if constexpr (W) wt = ok ? p.weight[r] : 1.0f;
+    if constexpr (W) wt[i] = ok ? p.weight[r] : 1.0f;
     constexpr int XS = XD == LC_FP32 ? 4 : 2;
     const char *row = static_cast<const char *>(p.x) + (ok ? src * p.ld_x + c0 : 0) * XS;
     uint32_t v[XD == LC_FP32 ? 8 : 4];
@@ -166,29 +171,20 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t fi
           }
       }
     }
-    if constexpr (XD == LC_FP32 && !W) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) w[i][c] = v[c];
-    } else if constexpr (XD == LC_FP32) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) w[i][c] = __float_as_uint(__uint_as_float(v[c]) * wt);
-    } else if constexpr (W) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) w[i][c] = __float_as_uint(half_value<XD>((v[c >> 1] >> (16 * (c & 1))) & 0xFFFFu) * wt);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) w[i][k] = v[k];
-    }
+    for (int k = 0; k < NW; ++k) w[i][k] = v[k];
   }
   auto value = [&](int i, int c) -> float {
-    if constexpr (H) return half_value<XD>(c & 1 ? w[i][c >> 1] >> 16 : w[i][c >> 1] & 0xFFFFu);
-    else return __uint_as_float(w[i][c]);
+    float x;
+    if constexpr (H) x = half_value<XD>(c & 1 ? w[i][c >> 1] >> 16 : w[i][c >> 1] & 0xFFFFu);
+    else x = __uint_as_float(w[i][c]);
+    return W ? x * wt[i] : x;
   };
 
   // ---- largest magnitudes: of the thread's 8 values of each row, of each column
-  uint32_t rm[8], cm[NW];
+  uint32_t rm[R], cm[NM];
   auto magnitude = [&](uint32_t u, bool finite) -> uint32_t {
-    if constexpr (H) {
+    if constexpr (P) {
       u &= 0x7FFF7FFFu;
       if (finite) {
         if ((u & 0xFFFFu) >= INF) u &= 0xFFFF0000u;
@@ -201,33 +197,46 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t fi
     return u;
   };
   auto largest = [&](uint32_t a, uint32_t b) -> uint32_t {
-    if constexpr (H) return max_pair(a, b);
+    if constexpr (P) return max_pair(a, b);
     else return max(a, b);
   };
   auto local_max = [&](bool finite) {
 #pragma unroll
-    for (int k = 0; k < NW; ++k) cm[k] = 0;
+    for (int k = 0; k < NM; ++k) cm[k] = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < R; ++i) {
       uint32_t m = 0;
 #pragma unroll
-      for (int k = 0; k < NW; ++k) {
-        const uint32_t u = magnitude(w[i][k], finite);
+      for (int k = 0; k < NM; ++k) {
+        uint32_t u;
+        if constexpr (P) u = magnitude(w[i][k], finite);
+        else u = magnitude(__float_as_uint(value(i, k)), finite);
         m = largest(m, u);
         cm[k] = largest(cm[k], u);
       }
-      if constexpr (H) m = max(m & 0xFFFFu, m >> 16);
+      if constexpr (P) m = max(m & 0xFFFFu, m >> 16);
       rm[i] = m;
     }
   };
+  // 16-bit values are widened and weighted anew for each use: kept as 64 products they take
+  // twice the registers (203, two workgroups per compute unit)
+  auto forget = [&]() {
+    if constexpr (H) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int k = 0; k < NW; ++k) asm volatile("" : "+v"(w[i][k]));
+    }
+  };
   local_max(false);
+  forget();
   uint32_t any = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) any = max(any, rm[i]);
+  for (int i = 0; i < R; ++i) any = max(any, rm[i]);
   if (__syncthreads_or(any >= INF)) local_max(true);  // an infinity or NaN in the tile: without them
   // fp32 bits of a magnitude
   auto bits32 = [&](uint32_t m) -> uint32_t {
-    if constexpr (H) return __float_as_uint(half_value<XD>(m));
+    if constexpr (P) return __float_as_uint(half_value<XD>(m));
     else return m;
   };
 
@@ -235,12 +244,13 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t fi
   if constexpr (SQ) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, rm[i]);
+    for (int i = 0; i < R; ++i) m = max(m, rm[i]);
     m = row_max(m);
     if (tx == 0) cmax[ty][0] = m;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = max(m, cmax[i][0]);
+    for (int i = 0; i < 32; ++i) m = max(m, cmax[i][0]);
+    __syncthreads();
     sq = scale_byte<E5>(bits32(m));
     if (tid == 0) {
       if (rows) p.scale[(int64_t)ct * p.ld_s + slot] = (uint8_t)sq;
@@ -251,8 +261,8 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t fi
   // ---- row layout
   if (rows) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t r = r0 + 8 * ty + i;
+    for (int i = 0; i < R; ++i) {
+      const int64_t r = r0 + R * ty + i;
       uint32_t s = sq;
       if constexpr (!SQ) s = scale_byte<E5>(bits32(row_max(rm[i])));
       const float up = scale_up(s);
@@ -270,21 +280,22 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t fi
 
   // ---- column layout
   if (!cols) return;  // uniform
+  forget();
   float up[8];
   if constexpr (SQ) {
 #pragma unroll
     for (int c = 0; c < 8; ++c) up[c] = scale_up(sq);
   } else {
 #pragma unroll
-    for (int k = 0; k < NW; ++k) cmax[ty][tx * NW + k] = cm[k];
+    for (int k = 0; k < NM; ++k) cmax[ty][tx * NM + k] = cm[k];
     __syncthreads();
-    if (tid < 16 * NW) {
+    if (tid < 16 * NM) {
       uint32_t m = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) m = largest(m, cmax[i][tid]);
-      const int c = ct * 128 + (H ? 2 * tid : tid);
+      for (int i = 0; i < 32; ++i) m = largest(m, cmax[i][tid]);
+      const int c = ct * 128 + (P ? 2 * tid : tid);
       uint8_t *const to = p.scale_t + (int64_t)cb * p.ld_st + c;
-      if constexpr (H) {
+      if constexpr (P) {
         const uint32_t a = scale_byte<E5>(bits32(m & 0xFFFFu)), b = scale_byte<E5>(bits32(m >> 16));
         cexp[2 * tid] = (uint8_t)a;
         cexp[2 * tid + 1] = (uint8_t)b;
@@ -305,15 +316,13 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(QuantP p, uint32_t fi
   // banks apart
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
-    uint2 o;
-    o.x = pack4<E5>(value(0, c) * up[c], value(1, c) * up[c], value(2, c) * up[c], value(3, c) * up[c]);
-    o.y = pack4<E5>(value(4, c) * up[c], value(5, c) * up[c], value(6, c) * up[c], value(7, c) * up[c]);
-    *reinterpret_cast<uint2 *>(tile8 + (16 * c + tx) * kColRow + 8 * ty) = o;
+    *reinterpret_cast<uint32_t *>(tile8 + (16 * c + tx) * kColRow + R * ty) =
+        pack4<E5>(value(0, c) * up[c], value(1, c) * up[c], value(2, c) * up[c], value(3, c) * up[c]);
   }
   __syncthreads();
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int j = u * 256 + tid, line = j >> 3, ch = j & 7;  // line 16 c + tx
+  for (int u = 0; u < 2; ++u) {
+    const int j = u * 512 + tid, line = j >> 3, ch = j & 7;  // line 16 c + tx
     const int col = ct * 128 + 8 * (line & 15) + (line >> 4);
     if (col < p.d)
       *reinterpret_cast<uint4 *>(p.qt + (int64_t)col * p.ld_qt + (int64_t)cb * 128 + 16 * ch) =
@@ -389,7 +398,7 @@ static lc_status quantize_launch(const lc_fp8_quantize_args &a, hipStream_t s) {
       constexpr int XD = decltype(xd)::value;
       auto go = [&](auto w_, auto e_, auto s_) {
         hipLaunchKernelGGL((fp8_quantize_kernel<XD, decltype(w_)::value, decltype(e_)::value, decltype(s_)::value>),
-                           dim3(count), dim3(256), 0, s, p, first);
+                           dim3(count), dim3(512), 0, s, p, first);
       };
       using T_ = std::true_type;
       using F_ = std::false_type;

@@ -2,6 +2,8 @@
 balance loss, without a GPU: every call breaks one documented rule and must return its status from
 the host-side checks, before anything is enqueued (addresses are aligned fakes that are never
 dereferenced; calls without rows return LC_OK)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -119,3 +121,13 @@ def test_balance_scratch_bytes():
     assert lc.lc_moe_balance_scratch_bytes(0, 8, 2) > 0
     # the backward's partial sums stay a small part of what it reads
     assert lc.lc_moe_balance_scratch_bytes(1 << 20, 4096, 64) <= 64 << 20
+
+
+def test_packed_arguments_have_the_structs_layout():
+    """The calls pack their arguments as bytes: sizes, and the place of every field, as in the structs."""
+    for packed, cls in ((lc._FP8_QUANTIZE, lc.lc_fp8_quantize_args), (lc._GEMM_FP8, lc.lc_gemm_fp8_args),
+                        (lc._MOE_BALANCE, lc.lc_moe_balance_args)):
+        assert packed.size == ctypes.sizeof(cls)
+        values = [i + 1 for i in range(len(cls._fields_))]
+        got = cls.from_buffer_copy(packed.pack(*values))
+        assert [getattr(got, f[0]) for f in cls._fields_] == values
