@@ -193,8 +193,8 @@ int64_t lc_fp8_padded_rows(int64_t T, int32_t n_groups);
  * K, lda, ldb and group_stride_b are multiples of 16 (a row's values between its own
  * length and K are zeros, as lc_fp8_quantize leaves them), ld_a_scale and ld_b_scale of
  * 4. Any M >= 0 (0: nothing happens) and N >= 1, each below 2^30; K below 2^30, lda
- * and ldb up to 2^22, ldc and ldr up to 2^30. Deterministic: a result depends on its
- * operands, sizes and types only. C may lie over R, element for element (the same
+ * and ldb up to 2^22, ldc and ldr up to 2^30, an operand's scales below 2^31 bytes.
+ * Deterministic: a result depends on its operands, sizes and types only. C may lie over R, element for element (the same
  * type and stride); no other output may overlap a tensor that the call reads. */
 typedef struct lc_gemm_fp8_args {
   int32_t a_dtype, b_dtype;

@@ -21,7 +21,6 @@ struct Fp8P {
   int goff_max;        // offsets end there: M (grouped rows) or K
   int epi, c_dt, r_dt;
   int walk;            // tile rows of a group of the tile walk (MAP)
-  uint32_t tiles;      // tiles in all (grouped rows: at most)
   int store16;         // STORE of 16-bit values
 };
 
@@ -38,6 +37,8 @@ struct Fp8Tile {
   int kb0, kb1, kend;
   const uint8_t *B, *sb;
   int64_t c_off;
+  // values of a row from kb0 on; a group without blocks may begin behind the last value
+  __device__ __forceinline__ int span() const { return max(kend - kb0 * KB, 0); }
 };
 
 // Tile of workgroup wg; false where it has none (uniform in the workgroup). Group
@@ -98,6 +99,7 @@ __device__ __forceinline__ bool fp8_find_tile(const Fp8P &p, uint32_t wg, Fp8Til
       const int slot = (int)(wg / (uint32_t)p.tiles_n);
       const uint64_t later = __ballot(end > slot);
       const int g = later ? __builtin_ctzll(later) : 0;
+      there = there && later != 0;
       t.m0 = __builtin_amdgcn_readlane(lo, g) + (slot - __builtin_amdgcn_readlane(end - nt, g)) * BM;
       t.m_lim = __builtin_amdgcn_readlane(hi, g);
       tn = wg % (uint32_t)p.tiles_n;
@@ -274,7 +276,7 @@ lc_status fp8_grid(Fp8P &p, uint32_t *grid) {
   int64_t n = rows * p.tiles_n;
   if (p.gmode == LC_GROUP_K) n = (n + 7) / 8 * 8 * p.ngroups;
   if (n > (int64_t)INT32_MAX) return fail(LC_ERR_UNSUPPORTED, "gemm fp8: too many outputs");
-  p.tiles = *grid = (uint32_t)n;
+  *grid = (uint32_t)n;
   return LC_OK;
 }
 

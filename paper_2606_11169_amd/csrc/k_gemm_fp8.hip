@@ -12,37 +12,22 @@
 namespace lc {
 namespace {
 
-// Fragments straight from global memory: WM x WN x WK waves of MF x NF blocks of 16 x
-// 16; the WK waves of one place take the k blocks in turn and their sums are added in
-// LDS in order.
-template <int FA, int FB, bool F32, int MF, int NF, int WM, int WN, int WK>
-__global__ __launch_bounds__(64 * WM * WN * WK) void fp8_direct_kernel(Fp8P p, uint32_t first) {
-  constexpr int BM = 16 * MF * WM, BN = 16 * NF * WN;
+// Tiles of 16 x 16, fragments straight from global memory: 8 waves take the k blocks in
+// turn, a block's loads under way while the one before is multiplied, and their sums are
+// added in LDS in order. For very small products, where a tile's time is a few latencies:
+// 1 x 2048 x 2048 6.2 us by this kernel, 6.3 by tiles of 32.
+template <int FA, int FB, bool F32>
+__global__ __launch_bounds__(512) void fp8_direct_kernel(Fp8P p, uint32_t first) {
+  constexpr int T = 16, W = 8;
   Fp8Tile t;
-  if (!fp8_tile<BM, BN>(p, first + blockIdx.x, t)) return;
+  if (!fp8_tile<T, T>(p, first + blockIdx.x, t)) return;  // before any barrier
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int i16 = lane & 15, g = lane >> 4;
-  const int wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN;
 
-  const uint8_t *pa[MF], *pb[NF];
-  int64_t oa[MF], ob[NF];  // scale bytes of the lane's rows in a line
-#pragma unroll
-  for (int i = 0; i < MF; ++i) {
-    const int64_t m = min(t.m0 + (wm * MF + i) * 16 + i16, t.m_lim - 1);  // (rows past the end: unused)
-    pa[i] = p.A + m * p.lda + 16 * g;
-    oa[i] = m >> p.ash;
-  }
-#pragma unroll
-  for (int j = 0; j < NF; ++j) {
-    const int64_t n = min(t.n0 + (wn * NF + j) * 16 + i16, p.N - 1);
-    pb[j] = t.B + n * p.ldb + 16 * g;
-    ob[j] = n >> p.bsh;
-  }
-  f32x4_v acc[MF][NF];
-#pragma unroll
-  for (int i = 0; i < MF; ++i)
-#pragma unroll
-    for (int j = 0; j < NF; ++j) acc[i][j] = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
+  // (rows past the end: the last one's values, unused)
+  const int64_t ra = min(t.m0 + i16, t.m_lim - 1), rb = min(t.n0 + i16, p.N - 1);
+  const uint8_t *const pa = p.A + ra * p.lda + 16 * g, *const pb = t.B + rb * p.ldb + 16 * g;
+  const uint8_t *const qa = p.sa + (ra >> p.ash), *const qb = t.sb + (rb >> p.bsh);
 
   auto frag = [&](const uint8_t *q, int k) -> i32x8_v {  // k: the lane's first of the block
     typedef __attribute__((ext_vector_type(4))) int i4;
@@ -51,98 +36,60 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void fp8_direct_kernel(Fp8P p, u
     if (k + 64 < t.kend) hi = *reinterpret_cast<const i4 *>(q + 64);
     return i32x8_v{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
   };
-  // the blocks of this wave, the next one's values on their way while one is multiplied
   struct Block {
-    i32x8_v a[MF], b[NF];
-    int ea[MF], eb[NF];
+    i32x8_v a, b;
+    int ea, eb;
   };
   auto fetch = [&](Block &x, int kb) {  // (a block past the last: zeros)
-    const int k = kb * KB + 16 * g;
     const bool in = kb < t.kb1;
     const int64_t at = in ? kb : t.kb0;
-#pragma unroll
-    for (int i = 0; i < MF; ++i) {
-      x.a[i] = frag(pa[i] + at * KB, in ? k : t.kend);
-      x.ea[i] = p.sa[at * p.ldsa + oa[i]];
-    }
-#pragma unroll
-    for (int j = 0; j < NF; ++j) {
-      x.b[j] = frag(pb[j] + at * KB, in ? k : t.kend);
-      x.eb[j] = t.sb[at * p.ldsb + ob[j]];
-    }
+    const int k = in ? kb * KB + 16 * g : t.kend;
+    x.a = frag(pa + at * KB, k);
+    x.ea = qa[at * p.ldsa];
+    x.b = frag(pb + at * KB, k);
+    x.eb = qb[at * p.ldsb];
   };
+  f32x4_v acc = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
   auto multiply = [&](const Block &x) {
     if constexpr (F32) {
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        bf16x8_v ca[MF];
-#pragma unroll
-        for (int i = 0; i < MF; ++i) ca[i] = fp8_to_bf16<FA>(x.a[i][2 * h], x.a[i][2 * h + 1], fp8_scale(x.ea[i]));
-#pragma unroll
-        for (int j = 0; j < NF; ++j) {
-          const bf16x8_v cb = fp8_to_bf16<FB>(x.b[j][2 * h], x.b[j][2 * h + 1], fp8_scale(x.eb[j]));
-#pragma unroll
-          for (int i = 0; i < MF; ++i)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb, ca[i], acc[i][j], 0, 0, 0);
-        }
-      }
+      for (int h = 0; h < 4; ++h)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_to_bf16<FB>(x.b[2 * h], x.b[2 * h + 1], fp8_scale(x.eb)),
+                                                      fp8_to_bf16<FA>(x.a[2 * h], x.a[2 * h + 1], fp8_scale(x.ea)),
+                                                      acc, 0, 0, 0);
     } else {
-#pragma unroll
-      for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = fp8_mul<FA, FB>(x.a[i], x.b[j], x.ea[i], x.eb[j], acc[i][j]);
+      acc = fp8_mul<FA, FB>(x.a, x.b, x.ea, x.eb, acc);
     }
   };
-  if (t.kb0 + wk < t.kb1) {
+  if (t.kb0 + wave < t.kb1) {
     Block x, y;
-    fetch(x, t.kb0 + wk);
-    for (int kb = t.kb0 + wk; kb < t.kb1; kb += 2 * WK) {
-      fetch(y, kb + WK);
+    fetch(x, t.kb0 + wave);
+    for (int kb = t.kb0 + wave; kb < t.kb1; kb += 2 * W) {
+      fetch(y, kb + W);
       multiply(x);
-      if (kb + WK >= t.kb1) break;
-      fetch(x, kb + 2 * WK);
+      if (kb + W >= t.kb1) break;
+      fetch(x, kb + 2 * W);
       multiply(y);
     }
   }
-  if constexpr (WK > 1) {
-    __shared__ __align__(16) float part[WK - 1][WM * WN][MF * NF * 256];
-    if (wk > 0) {
+  __shared__ __align__(16) float part[W - 1][256];
+  if (wave > 0) *reinterpret_cast<f32x4_v *>(&part[wave - 1][4 * lane]) = acc;
+  __syncthreads();
+  if (wave > 0) return;
 #pragma unroll
-      for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j)
-          *reinterpret_cast<f32x4_v *>(&part[wk - 1][wm * WN + wn][(i * NF + j) * 256 + 4 * lane]) = acc[i][j];
-    }
-    __syncthreads();
-    if (wk > 0) return;
-#pragma unroll
-    for (int s = 0; s < WK - 1; ++s)
-#pragma unroll
-      for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j)
-          acc[i][j] += *reinterpret_cast<const f32x4_v *>(&part[s][wm * WN + wn][(i * NF + j) * 256 + 4 * lane]);
-  }
-#pragma unroll
-  for (int i = 0; i < MF; ++i)
-#pragma unroll
-    for (int j = 0; j < NF; ++j) {
-      const int m = t.m0 + (wm * MF + i) * 16 + i16, n = t.n0 + (wn * NF + j) * 16 + 4 * g;
-      if (m < t.m_lim && n < p.N) fp8_store4(p, t.c_off, m, n, acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
-    }
+  for (int s = 0; s < W - 1; ++s) acc += *reinterpret_cast<const f32x4_v *>(&part[s][4 * lane]);
+  const int m = t.m0 + i16, n = t.n0 + 4 * g;
+  if (m < t.m_lim && n < p.N) fp8_store4(p, t.c_off, m, n, acc[0], acc[1], acc[2], acc[3]);
 }
 
-template <int MF, int NF, int WM, int WN, int WK>
-lc_status direct_launch(Fp8P p, const lc_gemm_fp8_args &a, bool f32, hipStream_t s) {
-  constexpr int BM = 16 * MF * WM, BN = 16 * NF * WN;
+static lc_status direct_launch(Fp8P p, const lc_gemm_fp8_args &a, bool f32, hipStream_t s) {
   uint32_t grid;
-  LC_TRY((fp8_grid<BM, BN>(p, &grid)));
+  LC_TRY((fp8_grid<16, 16>(p, &grid)));
   launch_parts(grid, [&](uint32_t first, uint32_t count) {
     fp8_with_formats(a, [&](auto fa, auto fb) {
       constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value;
-      const dim3 threads(64 * WM * WN * WK);
-      if (f32) hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, true, MF, NF, WM, WN, WK>), dim3(count), threads, 0, s, p, first);
-      else hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, false, MF, NF, WM, WN, WK>), dim3(count), threads, 0, s, p, first);
+      if (f32) hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, true>), dim3(count), dim3(512), 0, s, p, first);
+      else hipLaunchKernelGGL((fp8_direct_kernel<FA, FB, false>), dim3(count), dim3(512), 0, s, p, first);
     });
   });
   return check_launch("fp8_direct_kernel");
@@ -175,6 +122,9 @@ static lc_status check_gemm_fp8(const lc_gemm_fp8_args &a) {
     return fail(LC_ERR_INVALID_ARG, "gemm fp8: leading dimension too small");
   if (a.lda > (1 << 22) || a.ldb > (1 << 22) || a.ld_a_scale > MOST || a.ld_b_scale > MOST || a.ldc > MOST)
     return fail(LC_ERR_UNSUPPORTED, "gemm fp8: leading dimension too large");
+  const int64_t lines = (a.K + 127) / 128;  // (offsets of scales within a tile are 32 bits)
+  if (lines * a.ld_a_scale > INT32_MAX || lines * a.ld_b_scale > INT32_MAX)
+    return fail(LC_ERR_UNSUPPORTED, "gemm fp8: scales of 2^31 bytes or more");
   if (a.epilogue == LC_EPI_RESIDUAL) {
     if (a.M > 0 && (!a.R || !aligned16(a.R))) return fail(LC_ERR_INVALID_ARG, "gemm fp8: null or unaligned residual");
     if (!valid_dtype(a.r_dtype) || a.ldr < a.N || a.ldr > MOST)
@@ -302,7 +252,7 @@ static lc_status gemm_fp8_launch(const lc_gemm_fp8_args &a, hipStream_t s) {
   const bool f32 = p.c_dt == LC_FP32;
   p.store16 = !f32 && a.epilogue == LC_EPI_STORE;
   const Fp8Tiling *v = pick(a, f32);
-  if (v->tile == 16) return direct_launch<1, 1, 1, 1, 8>(p, a, f32, s);
+  if (v->tile == 16) return direct_launch(p, a, f32, s);
   return gemm_fp8_tile_launch(p, a, v->tile, v->deep, f32, s);
 }
 

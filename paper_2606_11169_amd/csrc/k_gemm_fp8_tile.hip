@@ -78,7 +78,7 @@ struct Fp8Stream {
     opnd = wave / (NW / 2);
     w = wave % (NW / 2);
     ns = t.kb1 - t.kb0;
-    kspan = t.kend - t.kb0 * KB;  // values of a row from the first block on
+    kspan = t.span();
     kl = 16 * (lane & 7);
     const bool a = opnd == 0;
     const int row0 = a ? t.m0 : t.n0, rows = min((a ? t.m_lim : p.N) - row0, BT);
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(64 * W) void fp8_split_kernel(Fp8P p, uint32_t firs
   if (!fp8_tile<T, T, true>(p, first + blockIdx.x, t)) return;  // before any barrier
 
   lds_t *const R = LDS_AS(char, ring), *const mine = R + wave * 2 * STAGE;
-  const int kspan = t.kend - t.kb0 * KB, nb = t.kb1 - t.kb0;
+  const int kspan = t.span(), nb = t.kb1 - t.kb0;
   const int n = (nb - wave + W - 1) / W;  // this wave's blocks
   i32x4_v rs[2], rb[2];
   uint32_t vo[2], so[2];

@@ -353,7 +353,7 @@ __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void b
 
   // Wr fragments: k experts 32 k + 8 g ..
   const int colf = 8 * (i16 >> 2) + (i16 & 3);
-  // (16-bit Wr: rows in LDS, read across like n's, which leaves registers for a second
+  // (bf16 Wr: rows in LDS, read across like n's, which leaves registers for a second
   // workgroup)
   constexpr bool WL = PW == 1;
   __shared__ __align__(16) uint16_t s_w[WL ? 32 * KE * LN : 8];

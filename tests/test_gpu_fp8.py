@@ -236,6 +236,8 @@ PRODUCTS = [
     (1000, 1000, 1008, "e4m3", "e4m3", "fp32", 1, 1), (2050, 1030, 272, "e4m3", "e4m3", "bf16", 1, 128),
     (513, 4100, 528, "e4m3", "e5m2", "bf16", 1, 1), (4100, 700, 144, "e4m3", "e4m3", "bf16", 128, 128),
     (2304, 2304, 144, "e4m3", "e4m3", "bf16", 1, 1), (2300, 2310, 144, "e5m2", "e4m3", "fp32", 1, 128),
+    (2570, 3101, 272, "e4m3", "e4m3", "bf16", 1, 128), (2561, 3200, 16, "e5m2", "e5m2", "fp16", 128, 1),
+    (40, 3101, 1040, "e4m3", "e4m3", "bf16", 1, 1), (530, 3601, 144, "e4m3", "e5m2", "fp32", 1, 1),
 ]
 
 
@@ -254,7 +256,8 @@ def test_product(M, N, K, a, b, c, ab, bb, kind):
     assert bool((Cm[:, N:] == 77.0).all())
 
 
-@pytest.mark.parametrize("M,N,K", [(5, 60, 160), (70, 133, 272), (300, 520, 144), (2304, 2304, 144)])
+@pytest.mark.parametrize("M,N,K", [(5, 60, 160), (70, 133, 272), (300, 520, 144), (300, 3102, 144), (2304, 2304, 144),
+                                   (2570, 3101, 144)])
 @pytest.mark.parametrize("epi,c,r", [("store_f32", "fp32", None), ("accum", "fp32", None), ("residual", "fp32", "fp32"),
                                      ("residual", "bf16", "fp32"), ("residual", "fp32", "bf16"),
                                      ("residual", "fp16", "fp16")])
@@ -290,7 +293,9 @@ def test_residual_in_place():
     ([0, 0, 1, 18, 18, 200, 300], 310, 200, 400, "bf16", 128), ([5, 40, 40, 45], 64, 130, 144, "fp32", 1),
     ([0, 9, 9, 11, 12], 12, 513, 272, "bf16", 128), ([0] * 40 + [64] * 20 + [70], 75, 96, 160, "fp16", 128),
     ([0, 700, 1500, 1500, 3001], 3003, 1034, 272, "bf16", 128), ([0, 900, 2500], 2500, 1040, 144, "fp32", 128),
-    ([0, 0, 0], 30, 64, 128, "bf16", 1)], ids=str)
+    ([0, 0, 0], 30, 64, 128, "bf16", 1), ([0, 1, 130], 130, 1030, 1040, "bf16", 128),
+    ([0, 17, 40], 40, 5201, 1040, "bf16", 1), ([3, 3, 300], 300, 2100, 272, "fp32", 128),
+    ([0, 129, 130, 130], 130, 3601, 528, "fp16", 128), ([0, 1000, 1257, 2570], 2570, 2901, 144, "bf16", 1)], ids=str)
 def test_grouped_rows(offsets, M, N, K, c, bb, kind):
     G = len(offsets) - 1
     A, sa, va = operand(M, K, "e4m3", 1, 1, kind)
@@ -313,7 +318,9 @@ def test_grouped_rows(offsets, M, N, K, c, bb, kind):
     ([300], 40, 72, "bf16", "store"), ([0, 5, 130, 0, 128], 65, 129, "fp32", "store"), ([1, 1, 1], 200, 300, "bf16", "store"),
     ([700, 0, 33], 258, 513, "bf16", "store"), ([40, 200, 0], 130, 260, "fp32", "accum"),
     ([3] * 64, 24, 40, "fp16", "store"), ([500, 600], 2304, 1030, "bf16", "store"),
-    ([400, 0, 200], 1040, 1032, "fp32", "accum")], ids=str)
+    ([400, 0, 200], 1040, 1032, "fp32", "accum"), ([2000, 3], 300, 300, "bf16", "store"), ([5, 200], 1500, 300, "fp16", "store"),
+    ([0, 900], 300, 3601, "bf16", "store"), ([1, 800], 65, 3601, "fp32", "accum"), ([200, 100], 3101, 4101, "bf16", "store"),
+    ([200, 0], 300, 3601, "fp32", "store")], ids=str)
 def test_grouped_k(lengths, M, N, c, epi, kind):
     """Operands in the column layout: groups from multiples of 128 on, columns of no group behind."""
     G, T = len(lengths), sum(lengths)
@@ -401,3 +408,142 @@ def test_deterministic():
             (A.float() + 1).sum()
     assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
     assert torch.equal(out[3], out[4]) and torch.equal(out[3], out[5])
+
+
+@pytest.mark.parametrize("lengths", [[0, 1], [1, 0], [0, 1, 0, 0]], ids=str)
+@pytest.mark.parametrize("M,N,K,c", [(1, 130, 144, "fp32"), (1, 1, 16, "bf16"), (33, 65, 400, "bf16"), (129, 4100, 528, "bf16"),
+                                     (3329, 1100, 144, "bf16"), (129, 3601, 144, "fp32"), (3329, 3601, 144, "fp16")])
+def test_grouped_k_ends_inside_a_block(M, N, K, c, lengths):
+    """K that is no multiple of 128, one group with all of it; an empty group behind begins past K."""
+    A, sa, va = operand(M, K, "e4m3", 1, 1, "small")
+    B, sb, vb = operand(N, K, "e4m3", 1, 2, "small")
+    off = torch.tensor([0] + lengths).cumsum(0).mul(K).to(torch.int32)
+    Cm = torch.full((len(lengths), M, N), 3.0, dtype=DT[c][1], device="cuda")
+    lc.lc_gemm_fp8(lc.LC_EPI_STORE, M, N, K, A.cuda(), A.stride(0), sa.cuda(), sa.stride(0), B.cuda(), B.stride(0),
+                   sb.cuda(), sb.stride(0), Cm, N, c_dtype=DT[c][0], b_block_rows=1, group_mode=lc.LC_GROUP_K,
+                   n_groups=len(lengths), group_offsets=off.cuda(), group_stride_c=M * N)
+    want = (va @ vb.T).to(DT[c][1]).double()
+    for got, n in zip(Cm.double().cpu(), lengths):
+        assert torch.equal(got, want * n)
+
+
+@pytest.mark.parametrize("far", ["C", "A", "R"])
+def test_far_rows(far):
+    """Rows whose offsets pass 2^32 elements (C, the residual) or bytes (A)."""
+    M, N, K = (1100, 70, 144) if far == "A" else (70000, 20, 32)
+    A, sa, va = operand(M, K, "e4m3", 1, 1, "small")
+    B, sb, vb = operand(N, K, "e4m3", 1, 2, "small")
+    want = va @ vb.T
+    lda, ldc = (1 << 22, N) if far == "A" else (A.stride(0), 1 << 16)
+    if far == "A":
+        wide = torch.empty(M, lda, dtype=torch.uint8, device="cuda")
+        wide[:, :A.shape[1]] = A.cuda()
+    else:
+        wide = A.cuda()
+    Cm = torch.empty(M, ldc if far == "C" else N, dtype=torch.bfloat16, device="cuda")
+    if far == "R":
+        R = torch.empty(M, ldc, dtype=torch.bfloat16, device="cuda")
+        add = torch.randint(-9, 10, (M, N), generator=torch.Generator().manual_seed(3))
+        R[:, :N] = add.cuda().bfloat16()
+        want = want + add
+    lc.lc_gemm_fp8(lc.LC_EPI_RESIDUAL if far == "R" else lc.LC_EPI_STORE, M, N, K, wide, lda, sa.cuda(), sa.stride(0),
+                   B.cuda(), B.stride(0), sb.cuda(), sb.stride(0), Cm, Cm.stride(0), b_block_rows=1,
+                   R=R if far == "R" else None, ldr=ldc, r_dtype=lc.LC_BF16)
+    assert torch.equal(Cm[:, :N].double().cpu(), want.bfloat16().double())
+
+
+@pytest.mark.parametrize("layouts,T,d", [("r", 70000, 40), ("c", 129, 70000)])
+def test_quantize_far_offsets(layouts, T, d):
+    """Outputs, and rows of x, past 2^32 bytes."""
+    x = values(T, d, "bf16", 4)
+    ld_x = 1 << 16 if d < 1 << 16 else d
+    wide = torch.empty(T, ld_x, dtype=torch.bfloat16, device="cuda")
+    wide[:, :d] = x.cuda()
+    rows, cols = layouts == "r", layouts == "c"
+    ld = 1 << 16
+    q = torch.zeros(T if rows else d, ld, dtype=torch.uint8, device="cuda")
+    blocks = up(d if rows else T, 128) // 128
+    s = torch.zeros(blocks, up(T if rows else d, 4), dtype=torch.uint8, device="cuda")
+    lc.lc_fp8_quantize(T, d, wide, lc.LC_BF16, lc.LC_FP8_E4M3, ld_x=ld_x, **{
+        "q" if rows else "qt": q, "ld_q" if rows else "ld_qt": ld, "scale" if rows else "scale_t": s,
+        "ld_scale" if rows else "ld_scale_t": s.stride(0)})
+    full = x.double() if rows else x.double().T.contiguous()
+    want_s, want = ref_blocks(full, "e4m3", 1)
+    got = q[:, :full.shape[1]].contiguous().cpu()
+    same(got.view(torch.float8_e4m3fn).float(), want)
+    assert torch.equal(s.cpu()[:, :want_s.shape[1]], want_s)
+    assert cols or bool((q[:, up(d, 16):] == 0).all())
+
+
+class Chain:
+    """x quantised both ways, its product with itself, in 16 and 32 bits, and its gradient-like product
+    over the rows in two groups: buffers of its own, and what a call of all of it gives."""
+
+    def __init__(self, T, d, seed):
+        self.T, self.d = T, d
+        self.x = values(T, d, "bf16", seed).cuda()
+        self.off = torch.tensor([0, T // 3, T], dtype=torch.int32, device="cuda")
+        self.b = Quant(T, d, 1, "rc", 2)
+        z = lambda *s, t: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
+        self.c, self.f = z(T, T, t=torch.bfloat16), z(T, T, t=torch.float32)
+        self.g = z(2, d, d, t=torch.bfloat16)
+
+    def run(self, stream=None):
+        T, d, b = self.T, self.d, self.b
+        lc.lc_fp8_quantize(T, d, self.x, lc.LC_BF16, lc.LC_FP8_E4M3, n_groups=2, group_offsets=self.off, stream=stream,
+                           **b.args())
+        K = up(d, 16)
+        for C, code in ((self.c, lc.LC_BF16), (self.f, lc.LC_FP32)):
+            lc.lc_gemm_fp8(lc.LC_EPI_STORE, T, T, K, b.q, b.q.stride(0), b.s, b.s.stride(0), b.q, b.q.stride(0), b.s,
+                           b.s.stride(0), C, T, c_dtype=code, b_block_rows=1, stream=stream)
+        lc.lc_gemm_fp8(lc.LC_EPI_STORE, d, d, b.cols, b.qt, b.qt.stride(0), b.st, b.st.stride(0), b.qt, b.qt.stride(0), b.st,
+                       b.st.stride(0), self.g, d, b_block_rows=1, group_mode=lc.LC_GROUP_K, n_groups=2,
+                       group_offsets=self.off, group_stride_c=d * d, stream=stream)
+
+    def results(self):
+        return [t.clone() for t in (self.b.q, self.b.s, self.b.qt, self.b.st, self.c, self.f, self.g)]
+
+
+def test_captured_graph():
+    """Captured once, replayed with new inputs and offsets, eager work between: as eager calls give."""
+    a, e = Chain(300, 264, 1), Chain(300, 264, 1)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        a.run(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        a.run(torch.cuda.current_stream())
+    for turn, cut in enumerate((100, 0, 300, 7)):
+        x = values(300, 264, "bf16", 20 + turn).cuda()
+        for chain in (a, e):
+            chain.x.copy_(x)
+            chain.off.copy_(torch.tensor([0, cut, 300], dtype=torch.int32))
+            # columns behind the last group stay as they were: the same in both
+            for t in (chain.b.qt, chain.b.st):
+                t.fill_(MARK)
+        e.run()
+        torch.cuda.synchronize()
+        graph.replay()
+        want = e.results()
+        torch.cuda.synchronize()
+        for got, w in zip(a.results(), want):
+            assert torch.equal(got.view(torch.uint8), w.view(torch.uint8))
+
+
+def test_streams():
+    """Chains on streams of their own at once give what each gives alone."""
+    sizes = [(300, 264), (1030, 520), (40, 1000), (700, 136)]
+    chains = [Chain(T, d, i) for i, (T, d) in enumerate(sizes)]
+    for c in chains:
+        c.run()
+    torch.cuda.synchronize()
+    want = [c.results() for c in chains]
+    streams = [torch.cuda.Stream() for _ in chains]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, s in zip(chains, streams):
+            c.run(s)
+    torch.cuda.synchronize()
+    for c, w in zip(chains, want):
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(c.results(), w))

@@ -288,6 +288,34 @@ def test_streams():
 
 # ------------------------------------------------------------------ a mixture's pass in 8 bits
 
+def test_far_tokens():
+    """Tokens whose offsets pass 2^31 values: zeros but for a few, which decide what is checked."""
+    T, d, E, few = 40000, 1 << 16, 4, [0, 7, 32767, 32768, 32769, 39990, 39999]
+    s = inputs(len(few), d, E, "bf16", "bf16", 3, std=0.005)
+    n = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+    n[torch.tensor(few, device="cuda")] = s["n"].cuda()
+    z = lambda *k, t=torch.float32: torch.zeros(*k, dtype=t, device="cuda")  # noqa: E731
+    sel = torch.arange(2 * T, dtype=torch.int32).remainder(E).view(T, 2).cuda()
+    mask = z(T, t=torch.uint8)
+    mask[torch.tensor(few, device="cuda")] = 1
+    wr = s["wr"].cuda()
+    p, lse, counts, loss = z(T, E), z(T), z(E + 1, t=torch.int32), z(2)
+    dn, dwr = torch.empty(T, d, dtype=torch.bfloat16, device="cuda"), z(E, d)
+    size = lc.lc_moe_balance_scratch_bytes(T, d, E)
+    scratch = z(size, t=torch.uint8)
+    BF = lc.LC_BF16
+    lc.lc_moe_balance_forward(T, d, E, n, wr, sel, p, lse, counts, loss, scratch, size, BF, BF, mask=mask)
+    lc.lc_moe_balance_backward(T, d, E, n, wr, sel, p, lse, counts, COEF, Z, dn, dwr, scratch, size, BF, BF, BF,
+                               mask=mask, store_dwr=1)
+    at = torch.tensor(few, device="cuda")
+    t = {"n": s["n"], "wr": s["wr"], "sel": sel[at].cpu(), "w": s["w"], "dw": s["dw"], "mask": None,
+         "dres": torch.zeros(len(few), d)}
+    check({"p": p[at], "lse": lse[at], "counts": counts, "loss": loss, "dn": dn[at], "dwr": dwr},
+          reference(t, E, pair=False, dres=False), d, "bf16")
+    dn[at] = 0
+    assert not bool(dn.any()) and float(p.sum()) == pytest.approx(len(few), rel=1e-5)
+
+
 def up(n, to):
     return -(-n // to) * to
 

@@ -78,6 +78,7 @@ KGRP = dict(group_mode=lc.LC_GROUP_K, n_groups=3, group_offsets=F, group_stride_
     (dict(c_dtype=E4), BAD), (dict(lda=264), BAD), (dict(ldb=240), BAD), (dict(ldb=1 << 23), UNSUP),
     (dict(ld_a_scale=96), BAD), (dict(ld_a_scale=102), BAD), (dict(ld_b_scale=0), BAD), (dict(ldc=199), BAD),
     (dict(b_block_rows=1), BAD), (dict(ldc=(1 << 30) + 4), UNSUP),
+    (dict(ld_a_scale=1 << 30), UNSUP), (dict(K=512, lda=512, ldb=512, ld_b_scale=1 << 29), UNSUP),
     (dict(epilogue=lc.LC_EPI_RESIDUAL), BAD), (dict(epilogue=lc.LC_EPI_RESIDUAL, R=F, ldr=199), BAD),
     (dict(epilogue=lc.LC_EPI_RESIDUAL, R=F, ldr=200, r_dtype=9), BAD), (dict(group_mode=3), BAD),
     ({**ROWS, "n_groups": 0}, BAD), ({**ROWS, "n_groups": 65}, BAD), ({**ROWS, "group_offsets": None}, BAD),
@@ -96,7 +97,8 @@ BWD = dict(T=10, d=64, E=8, n=A, wr=B, sel=C, probs=D, lse=E, counts=F, coef=0.1
 
 
 @pytest.mark.parametrize("over,want", [
-    (dict(T=-1), BAD), (dict(T=1 << 30), UNSUP), (dict(d=0), BAD), (dict(d=60), UNSUP), (dict(E=1), BAD),
+    (dict(T=-1), BAD), (dict(T=1 << 30), UNSUP), (dict(d=0), BAD), (dict(d=60), UNSUP),
+    (dict(d=(1 << 20) + 8, scratch_bytes=1 << 40), UNSUP), (dict(E=1), BAD),
     (dict(E=65), BAD), (dict(n=None), BAD), (dict(wr=B + 4), BAD), (dict(sel=None), BAD), (dict(probs=None), BAD),
     (dict(lse=E + 8), BAD), (dict(counts=None), BAD), (dict(loss=None), BAD), (dict(n_dtype=E4), BAD),
     (dict(w_dtype=7), BAD), (dict(scratch=None), BAD), (dict(scratch=H + 4), BAD), (dict(scratch_bytes=100), WS)],
@@ -106,7 +108,8 @@ def test_balance_forward(over, want):
 
 
 @pytest.mark.parametrize("over,want", [
-    (dict(T=-1), BAD), (dict(d=60), UNSUP), (dict(E=65), BAD), (dict(n=None), BAD), (dict(counts=None), BAD),
+    (dict(T=-1), BAD), (dict(d=60), UNSUP), (dict(d=(1 << 20) + 8, scratch_bytes=1 << 40), UNSUP), (dict(E=65), BAD),
+    (dict(n=None), BAD), (dict(counts=None), BAD),
     (dict(w=A), BAD), (dict(dw=A), BAD), (dict(w=A + 4, dw=B), BAD), (dict(dn=G + 2), BAD), (dict(dn_dtype=E5), BAD),
     (dict(dres=A, dres_dtype=8), BAD), (dict(dres=A + 8), BAD), (dict(dwr_accum=H + 4), BAD),
     (dict(coef=float("nan")), BAD), (dict(z_coef=float("nan")), BAD),
