@@ -14,8 +14,8 @@ namespace {
 
 // Tiles of 16 x 16, fragments straight from global memory: 8 waves take the k blocks in
 // turn, a block's loads under way while the one before is multiplied, and their sums are
-// added in LDS in order. For very small products, where a tile's time is a few latencies:
-// 1 x 2048 x 2048 6.2 us by this kernel, 6.3 by tiles of 32.
+// added in LDS in order. For products of few rows or a short k, where a tile's time is a
+// few latencies: 14 x 3616, K 7856 7.9 us, by tiles of 32 8.2.
 template <int FA, int FB, bool F32>
 __global__ __launch_bounds__(512) void fp8_direct_kernel(Fp8P p, uint32_t first) {
   constexpr int T = 16, W = 8;
