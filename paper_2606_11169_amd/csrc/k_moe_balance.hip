@@ -334,8 +334,11 @@ constexpr int kBwdCols = 256;
 template <int ND, int WD, int EF>
 __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void balance_bwd_kernel(BalanceP p) {
   constexpr int PN = kPieces<ND>, PW = kPieces<WD>, KE = (EF + 1) / 2;
-  constexpr int LE = 32 * KE + 8;  // [token][expert] row
-  constexpr int LN = kBwdCols + 16;
+  // Rows in LDS without bank conflicts, 16-bit values: [token][expert] rows of LE, 8 experts
+  // at 8 c at 8 (c ^ (row / 4 % 2)); rows of LN columns, 4 columns at 4 c at 4 (c ^ (row / 2 %
+  // 2)). Read across, 16 lanes take 8 bytes each of 4 rows: next to each other of a dl row,
+  // 16 bytes apart of the others.
+  constexpr int LE = 80, LN = kBwdCols + 32;
   __shared__ __align__(16) uint16_t s_te[3][kBwdTokens * LE];
   __shared__ __align__(16) uint16_t s_n[PN][kBwdTokens * LN];
   __shared__ float s_f[64];
@@ -363,16 +366,27 @@ __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void b
       u32x4_v v = u32x4_v{0, 0, 0, 0};
       if (p.dn && e < p.E && c0 + c < p.d)
         v = *reinterpret_cast<const u32x4_v *>(static_cast<const bf16_t *>(p.wr) + (int64_t)e * p.d + c0 + c);
-      *reinterpret_cast<u32x4_v *>(&s_w[e * LN + c]) = v;
+      *reinterpret_cast<u32x4_v *>(&s_w[e * LN + c]) = (e >> 1 & 1) ? u32x4_v{v[2], v[3], v[0], v[1]} : v;
     }
   }
-  // each 16 lanes: rows (k) 8 g + i16 / 4 (and + 4), four columns of run i16 % 4
-  auto across = [&](const uint16_t *rows, int ld, int col) -> bf16x8_v {
+  // each 16 lanes: rows (k) 8 g + i16 / 4 (and + 4), four columns of run i16 % 4, from
+  // columns lo of the first and hi of the second rows on
+  auto across = [&](const uint16_t *rows, int ld, int lo, int hi) -> bf16x8_v {
     typedef __attribute__((address_space(3))) s16x4_v lds_v4;
-    lds_t *q = LDS_AS(char, const_cast<uint16_t *>(rows + (8 * g + (i16 >> 2)) * ld + col));
-    const s16x4_v v[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)q),
-                          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(q + 4 * ld * 2))};
+    const uint16_t *const at = rows + (8 * g + (i16 >> 2)) * ld;
+    const s16x4_v v[2] = {
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)LDS_AS(char, const_cast<uint16_t *>(at + lo))),
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)LDS_AS(char, const_cast<uint16_t *>(at + 4 * ld + hi)))};
     return __builtin_bit_cast(bf16x8_v, v);
+  };
+  // fragment b of the wave's columns of rows of LN; experts 16 a .. of dl's rows
+  auto columns = [&](const uint16_t *rows, int b) {
+    const int at = 32 * wave + 8 * (i16 & 3) + 4 * (b ^ (i16 >> 3));
+    return across(rows, LN, at, at);
+  };
+  auto experts = [&](const uint16_t *rows, int a) {
+    const int at = 16 * a + 4 * (i16 & 3);
+    return across(rows, LE, at, at ^ 8);
   };
   bf16x8_v fw[2][KE][PW];
 #pragma unroll
@@ -507,7 +521,7 @@ __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void b
         }
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
-          *reinterpret_cast<uint2 *>(&s_te[i][tl * LE + e4]) =
+          *reinterpret_cast<uint2 *>(&s_te[i][tl * LE + (e4 ^ 8 * (tl >> 2 & 1))]) =
               make_uint2(s[0][i] | (uint32_t)s[1][i] << 16, s[2][i] | (uint32_t)s[3][i] << 16);
         }
       }
@@ -516,11 +530,12 @@ __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void b
     for (int u = 0; u < 2; ++u) {
       bf16x8_v f[PN];
       x.n[u].pieces(f);
-      const bool live = !p.mask || x.mask_n[u] != 0;
+      const bool live = !p.mask || x.mask_n[u] != 0, swap = nr >> 1 & 1;
 #pragma unroll
-      for (int i = 0; i < PN; ++i)
-        *reinterpret_cast<u32x4_v *>(&s_n[i][(nr + 16 * u) * LN + nc]) =
-            live ? __builtin_bit_cast(u32x4_v, f[i]) : u32x4_v{0, 0, 0, 0};
+      for (int i = 0; i < PN; ++i) {
+        const u32x4_v v = live ? __builtin_bit_cast(u32x4_v, f[i]) : u32x4_v{0, 0, 0, 0};
+        *reinterpret_cast<u32x4_v *>(&s_n[i][(nr + 16 * u) * LN + nc]) = swap ? u32x4_v{v[2], v[3], v[0], v[1]} : v;
+      }
     }
     fetch(x, tile + 1);
     __syncthreads();
@@ -533,10 +548,10 @@ __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void b
           bf16x8_v fd[3];
 #pragma unroll
           for (int i = 0; i < 3; ++i)
-            fd[i] = *reinterpret_cast<const bf16x8_v *>(&s_te[i][(16 * a + i16) * LE + 32 * k + 8 * g]);
+            fd[i] = *reinterpret_cast<const bf16x8_v *>(&s_te[i][(16 * a + i16) * LE + 32 * k + 8 * (g ^ (i16 >> 2 & 1))]);
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
-            if constexpr (WL) fw[b][k][0] = across(s_w + 32 * k * LN, LN, 32 * wave + 8 * (i16 & 3) + 4 * b);
+            if constexpr (WL) fw[b][k][0] = columns(s_w + 32 * k * LN, b);
             s[b] = mul_pieces(fw[b][k], fd, s[b]);
           }
         }
@@ -565,12 +580,12 @@ __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void b
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < PN; ++i) fn[b][i] = across(s_n[i], LN, 32 * wave + 8 * (i16 & 3) + 4 * b);
+        for (int i = 0; i < PN; ++i) fn[b][i] = columns(s_n[i], b);
 #pragma unroll
       for (int a = 0; a < EF; ++a) {
         bf16x8_v fd[3];
 #pragma unroll
-        for (int i = 0; i < 3; ++i) fd[i] = across(s_te[i], LE, 16 * a + 4 * (i16 & 3));
+        for (int i = 0; i < 3; ++i) fd[i] = experts(s_te[i], a);
 #pragma unroll
         for (int b = 0; b < 2; ++b) aw[a][b] = mul_pieces(fn[b], fd, aw[a][b]);
       }
