@@ -219,6 +219,16 @@ __device__ __forceinline__ float4 fp8_load4(const void *base, int64_t at, int dt
   return make_float4((float)v[0], (float)v[1], (float)v[2], (float)v[3]);
 }
 
+// Results are stored past the caches, at any alignment of their type: kept there, they push
+// the operands out, and written back later, they stand in the way. 4096 x 2816 x 2048 24.2
+// us, kept 26.2, and with a kernel that reads C next 33.5 and 34.2; weight gradients of 8
+// experts (92 MB) 57 and 93.
+template <typename V>
+__device__ __forceinline__ void fp8_stream_store(void *to, const V &v) {
+  typedef V any __attribute__((aligned(2)));
+  __builtin_nontemporal_store(v, static_cast<any *>(to));
+}
+
 // C(m, n .. n + 3) = x by the epilogue; m and n in range, columns from N on left out
 __device__ __forceinline__ void fp8_store4(const Fp8P &p, int64_t c_off, int64_t m, int n, float x0, float x1,
                                            float x2, float x3) {
@@ -230,14 +240,11 @@ __device__ __forceinline__ void fp8_store4(const Fp8P &p, int64_t c_off, int64_t
       x0 += o.x; x1 += o.y; x2 += o.z; x3 += o.w;
     }
     if (p.c_dt == LC_FP32) {
-      const float4 v = make_float4(x0, x1, x2, x3);
-      __builtin_memcpy(static_cast<float *>(p.C) + at, &v, 16);
+      fp8_stream_store(static_cast<float *>(p.C) + at, f32x4_v{x0, x1, x2, x3});
     } else if (p.c_dt == LC_BF16) {
-      const bf16x4_v v = {(__bf16)x0, (__bf16)x1, (__bf16)x2, (__bf16)x3};
-      __builtin_memcpy(static_cast<__bf16 *>(p.C) + at, &v, 8);
+      fp8_stream_store(static_cast<__bf16 *>(p.C) + at, bf16x4_v{(__bf16)x0, (__bf16)x1, (__bf16)x2, (__bf16)x3});
     } else {
-      const f16x4_v v = {(_Float16)x0, (_Float16)x1, (_Float16)x2, (_Float16)x3};
-      __builtin_memcpy(static_cast<_Float16 *>(p.C) + at, &v, 8);
+      fp8_stream_store(static_cast<_Float16 *>(p.C) + at, f16x4_v{(_Float16)x0, (_Float16)x1, (_Float16)x2, (_Float16)x3});
     }
     return;
   }

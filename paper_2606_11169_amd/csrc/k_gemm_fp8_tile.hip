@@ -155,11 +155,11 @@ __device__ __forceinline__ void fp8_epilogue(const Fp8P &p, const Fp8Tile &t, in
           if (p.c_dt == LC_BF16) {
             const bf16x8_v o = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3],
                                 (__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
-            __builtin_memcpy(static_cast<__bf16 *>(p.C) + to, &o, 16);
+            fp8_stream_store(static_cast<__bf16 *>(p.C) + to, o);
           } else {
             const f16x8_v o = {(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3],
                                (_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
-            __builtin_memcpy(static_cast<_Float16 *>(p.C) + to, &o, 16);
+            fp8_stream_store(static_cast<_Float16 *>(p.C) + to, o);
           }
         } else {
           fp8_store4(p, t.c_off, m + r, n, x[0], x[1], x[2], x[3]);
