@@ -17,6 +17,11 @@
 // changes one half, which is read into the registers that the step before has freed, so
 // every fragment is read once per stage and none is held twice. The stage's barrier sits
 // in the middle: its own reads are done, the next stage's may begin.
+//
+// Bound: the matrix cores, under the chip's power. 4096 x 11008 x 4096, bf16 out: 143 us,
+// 2.58 PFLOP/s (a loop of these instructions alone reaches 4.4). 8187 rows of eight experts x
+// 2816 x 2048: 54 us, 1.76, and their weight gradients 57, 1.65: 2048 of k are 16 stages
+// beside a tile's start and end, and the last round of tiles is not full.
 #include "gemm_fp8.hpp"
 
 namespace lc {
@@ -291,7 +296,9 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_tile_kernel(Fp8P p, uint32_t
 // Results of fp32: the same stages, the values converted to bf16 with their scales on the
 // way to the bf16 instruction. A lane's 32 values of a row's 128 are two pieces of 16; a
 // stage is multiplied in two steps, the pieces at 0 and at 64, and while one multiplies the
-// other's are read. A step is two products of 32 k: 8 values of each lane.
+// other's are read. A step is two products of 32 k: 8 values of each lane. Bound: the
+// conversions, two (of two values each) beside every product, which then takes 30 cycles
+// instead of 16: 3001 x 1155 x 1872 22.4 us, 0.58 PFLOP/s.
 template <int FA, int FB, int D>
 __global__ __launch_bounds__(256) void fp8_wide_kernel(Fp8P p, uint32_t first) {
   constexpr int BT = 128, FM = 4, FN = 4;
@@ -377,7 +384,8 @@ __global__ __launch_bounds__(256) void fp8_wide_kernel(Fp8P p, uint32_t first) {
 // Small tiles, k split over the waves: each of W waves takes every W-th block of k for the
 // whole T x T tile and streams it into two stages of its own in LDS, with no barrier but
 // its own wait; the waves' sums are added through LDS in order. For grids of few tiles,
-// where a tile's chain of blocks, each a load's latency long, is the time.
+// where a tile's chain of blocks, each a load's latency long, is the time: 1 x 4096 x 4096
+// 6.2 us (an operand of 16.8 MB at 2.7 TB/s); 64 rows 6.7, by tiles of 128 15.
 // Stage: rows of 128 bytes, 16-byte piece c of row r at c ^ (r / 2 % 8), which keeps
 // fragment reads (16 rows, four pieces) free of bank conflicts without padding.
 template <int FA, int FB, bool F32, int T, int W>

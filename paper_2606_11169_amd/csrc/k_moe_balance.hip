@@ -11,7 +11,10 @@
 // above 2^-24 of the whole are added in fp32, so a bf16 router pays one instruction
 // where fp32 ones would take sixteen times as long. dl is fp32 and takes three pieces.
 //
-// Bound: HBM, by n (forward), and n, dres and dn (backward).
+// Bound: HBM, by n (forward), and n, dres and dn (backward). bf16, us: 4096 tokens x 2048, 8
+// experts, forward 7.8 + 4.8 (sums), backward 22.7 + 4.3 (dWr's parts); 16411 x 4096, 64
+// experts, 54.6 + 4.8 (2.5 TB/s of n; 8 experts 3.7, where a large sum reads 4.0) and 106.8 +
+// 6.8 (3.8 TB/s; 8 experts 4.7).
 #include "common.hpp"
 #include "lds_dma.hpp"
 
