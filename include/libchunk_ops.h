@@ -173,12 +173,14 @@ int64_t lc_fp8_padded_rows(int64_t T, int32_t n_groups);
  * b_block_rows 1 or 128; a scale byte of 255 is NaN). a_dtype and b_dtype:
  * LC_FP8_E4M3 or LC_FP8_E5M2. Then an epilogue as in lc_gemm: LC_EPI_STORE (c_dtype),
  * LC_EPI_STORE_F32, LC_EPI_ACCUM_F32, LC_EPI_RESIDUAL (r_dtype, c_dtype).
- * Sums: a C of 16 bits takes the 8-bit matrix instructions, which add each 8
- * neighbouring products to about 14 bits below the largest of them and the sums of
- * those in fp32: an error of about 1.5e-5 of the result on values of either sign, a
- * hundredth of the result's own rounding. A C of fp32 takes the bf16 instructions on
- * the same values (exact in bf16), whose sums are fp32, at half the rate. There a
- * value times its scale below 2^-126 counts as 0 and from 2^128 on as infinite.
+ * Sums: a C of bf16 takes the 8-bit matrix instructions. From each of 8 neighbouring products
+ * these cut off, towards zero, up to 2^-13 of the largest one, and add the rest and the sums
+ * of eights in fp32: an error of about 1.5e-5 of the product on
+ * values of either sign, at most 7 * 2^-13 of sum |A B| (with its scales) where one product of
+ * eight outweighs seven of its sign; bf16's half step is 2^-8. (With a residual that takes
+ * off most of the product, that error is still one of the product.) A C of fp16 or fp32 takes
+ * the bf16 instructions on the same values (exact in bf16), whose sums are fp32, at half the
+ * rate. There a value times its scale below 2^-126 counts as 0 and from 2^128 on as infinite.
  * Groups as in lc_gemm, 1 to 64:
  *   LC_GROUP_ROWS  rows [off[g], off[g+1]) of A and C with B + g*group_stride_b and
  *                  b_scale + g*group_stride_b_scale (a_block_rows 1); STORE,

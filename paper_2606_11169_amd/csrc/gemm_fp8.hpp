@@ -171,7 +171,7 @@ __device__ __forceinline__ f32x4_v fp8_mul(const i32x8_v &a, const i32x8_v &b, i
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, FB, FA, 0, sb, 0, sa);
 }
 
-// For results of fp32: the values times their scales as bf16 (exact: at most 4
+// For results of fp16 and fp32: the values times their scales as bf16 (exact: at most 4
 // significant bits), for four bf16 instructions.
 // The scale byte s as the float that the conversions take (they read its exponent)
 __device__ __forceinline__ float fp8_scale(int s) { return __uint_as_float((uint32_t)s << 23); }
@@ -289,8 +289,8 @@ lc_status fp8_grid(Fp8P &p, uint32_t *grid) {
 
 }  // namespace
 
-// k_gemm_fp8_tile.hip: tiles of 32, 64, 128 or 256 (256: results of 16 bits); deep: four
-// stages in LDS instead of two (128)
+// k_gemm_fp8_tile.hip: tiles of 32, 64, 128 or 256 (256: results of bf16); deep: four
+// stages in LDS instead of two (128); f32: summed by the bf16 instructions
 lc_status gemm_fp8_tile_launch(Fp8P p, const lc_gemm_fp8_args &a, int tile, bool deep, bool f32, hipStream_t s);
 
 }  // namespace lc

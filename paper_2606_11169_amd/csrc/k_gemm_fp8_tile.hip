@@ -293,7 +293,7 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_tile_kernel(Fp8P p, uint32_t
   fp8_epilogue<FM, FN>(p, t, t.m0 + wm * FM * 16, t.n0 + wn * FN * 16, R0 + wave * (2048 * FN), lane, acc);
 }
 
-// Results of fp32: the same stages, the values converted to bf16 with their scales on the
+// Results of fp16 and fp32: the same stages, the values converted to bf16 with their scales on the
 // way to the bf16 instruction. A lane's 32 values of a row's 128 are two pieces of 16; a
 // stage is multiplied in two steps, the pieces at 0 and at 64, and while one multiplies the
 // other's are read. A step is two products of 32 k: 8 values of each lane. Bound: the

@@ -547,3 +547,47 @@ def test_streams():
     torch.cuda.synchronize()
     for c, w in zip(chains, want):
         assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(c.results(), w))
+
+
+# ------------------------------------------------------------------ sums of one sign
+
+def one_sign(r, k, seed, low, high):
+    """Bytes of positive e4m3 values: every eighth 256, the others from low to high; their values."""
+    g = torch.Generator().manual_seed(seed)
+    v = (low + torch.rand(r, k, generator=g) * (high - low)).to(torch.float8_e4m3fn).double()
+    v[:, ::8] = 256.0
+    b = torch.zeros(r, up(k, 16), dtype=torch.uint8)
+    b[:, :k] = v.float().to(torch.float8_e4m3fn).view(torch.uint8)
+    return b, v
+
+
+@pytest.mark.parametrize("epi", ["store", "residual"])
+@pytest.mark.parametrize("c", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 4096), (17, 65, 2064), (33, 3101, 2064), (130, 300, 4096), (300, 1155, 1872),
+                                   (700, 1030, 1040), (2300, 2310, 528), (2570, 3101, 272)])
+def test_sums_of_one_sign(M, N, K, c, epi):
+    """One product of 2^16 beside seven of 6 to 7.5 in every eight: the 8-bit instruction cuts each of
+    the seven off below 2^(16 - 13), always towards zero: 7 * 2^-13 of the sum at most, whatever K, which
+    is 0.22 of bf16's half step. fp16's half step is 2^-11, so its sums are of fp32 like fp32's own,
+    also where the residual takes off what the product has."""
+    A, va = one_sign(M, K, 1, 6.0, 7.5)
+    B, vb = one_sign(N, K, 2, 1.0, 1.0)
+    e = 14 - int(torch.tensor(K / 8 * 65600.0).log2().ceil())  # results below 2^14
+    mk = lambda b, byte: torch.full((up(K, 128) // 128, up(b.shape[0], 4)), byte, dtype=torch.uint8)  # noqa: E731
+    sa, sb = mk(A, 127 + e), mk(B, 127)
+    want = va @ vb.T * 2.0 ** e
+    mag = want.clone()
+    Cm, R = torch.empty(M, N, dtype=DT[c][1], device="cuda"), None
+    if epi == "residual":
+        R = -(want * (1 + 0.01 * torch.rand(M, N, generator=torch.Generator().manual_seed(3), dtype=torch.float64))).float()
+        want = want + R.double()
+        R = R.cuda()
+    lc.lc_gemm_fp8(lc.LC_EPI_RESIDUAL if R is not None else lc.LC_EPI_STORE, M, N, K, A.cuda(), A.stride(0), sa.cuda(),
+                   sa.stride(0), B.cuda(), B.stride(0), sb.cuda(), sb.stride(0), Cm, N, c_dtype=DT[c][0], b_block_rows=1,
+                   R=R, ldr=N, r_dtype=lc.LC_FP32)
+    sums = 7 * 2.0 ** -13 if c == "bf16" else (K / 32 * 6 + 2) * 2.0 ** -24
+    tol = (sums + (K / 128 + 8) * 2.0 ** -24) * mag + HALF_STEP[c] * want.abs()
+    if c == "fp16":
+        tol = tol + 2.0 ** -25  # half the smallest fp16
+    bad = (Cm.double().cpu() - want).abs() / tol
+    assert float(bad.max()) <= 1.0, bad.max()
