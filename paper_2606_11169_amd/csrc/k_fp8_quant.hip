@@ -281,6 +281,12 @@ __global__ __launch_bounds__(512) void fp8_quantize_kernel(QuantP p, uint32_t fi
           uint2 o;
           o.x = pack4<E5>(value(i, 0) * up, value(i, 1) * up, value(i, 2) * up, value(i, 3) * up);
           o.y = pack4<E5>(value(i, 4) * up, value(i, 5) * up, value(i, 6) * up, value(i, 7) * up);
+          if (W && c0 + 8 > p.d) {  // zeros behind d, whatever 0 times the row's weight is
+            const int have = max(p.d - c0, 0);
+            const uint64_t keep = ((uint64_t)1 << (8 * have)) - 1;  // (have < 8)
+            o.x &= (uint32_t)keep;
+            o.y &= (uint32_t)(keep >> 32);
+          }
           if constexpr (SQ) __builtin_nontemporal_store(u32x2_v{o.x, o.y}, reinterpret_cast<u32x2_v *>(p.q + r * p.ld_q + c0));
           else *reinterpret_cast<uint2 *>(p.q + r * p.ld_q + c0) = o;
         }

@@ -591,3 +591,39 @@ def test_sums_of_one_sign(M, N, K, c, epi):
         tol = tol + 2.0 ** -25  # half the smallest fp16
     bad = (Cm.double().cpu() - want).abs() / tol
     assert float(bad.max()) <= 1.0, bad.max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("q", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("d", [1, 17, 129, 135, 250])
+def test_weighted_padding(d, q, dtype):
+    """Rows whose weight is negative, zero, infinite or NaN: the columns behind d hold zeros (the byte 0)
+    all the same."""
+    T, w = 140, torch.ones(140)
+    x = values(T, d, dtype, d)
+    w[:9] = torch.tensor([-1.5, 0.0, -0.0, float("inf"), -float("inf"), float("nan"), 1e30, -1e-30, 2.0])
+    w[130:133] = torch.tensor([-1.0, float("inf"), float("nan")])
+    for block in (1, 128):
+        b = Quant(T, d, block, "rc", extra=1)
+        lc.lc_fp8_quantize(T, d, x.cuda(), DT[dtype][0], DT[q][0], block_rows=block, row_weight=w.cuda(), **b.args())
+        rows = (x.float() * w[:, None]).double()
+        check_rows(b, rows, q, block)
+        check_cols(b, torch.nn.functional.pad(rows, (0, 0, 0, -T % 128)), q, block, up(T, 128))
+
+
+def test_product_of_infinite_rows():
+    """e5m2 rows weighted by an infinity, d no multiple of 8: the product's row is infinite, not NaN."""
+    T, d, N = 20, 133, 24
+    x, wide = values(T, d, "bf16", 7).abs() + 1, Quant(T, d, 1, "r")
+    w = torch.ones(T)
+    w[3], w[5] = float("inf"), -float("inf")
+    lc.lc_fp8_quantize(T, d, x.cuda(), lc.LC_BF16, lc.LC_FP8_E5M2, row_weight=w.cuda(), **wide.args())
+    y, B = values(N, d, "bf16", 8).abs() + 1, Quant(N, d, 1, "r")
+    lc.lc_fp8_quantize(N, d, y.cuda(), lc.LC_BF16, lc.LC_FP8_E4M3, **B.args())
+    for c in ("bf16", "fp32"):
+        Cm = torch.zeros(T, N, dtype=DT[c][1], device="cuda")
+        lc.lc_gemm_fp8(lc.LC_EPI_STORE, T, N, up(d, 16), wide.q, wide.q.stride(0), wide.s, wide.s.stride(0), B.q, B.q.stride(0),
+                       B.s, B.s.stride(0), Cm, N, a_dtype=lc.LC_FP8_E5M2, c_dtype=DT[c][0], b_block_rows=1)
+        got = Cm.float().cpu()
+        assert bool((got[3] == float("inf")).all()) and bool((got[5] == -float("inf")).all())
+        assert bool(torch.isfinite(got[[i for i in range(T) if i not in (3, 5)]]).all())
