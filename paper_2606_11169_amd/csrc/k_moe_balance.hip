@@ -6,10 +6,11 @@
 //   dl[t, e] = coef E / N p (f_e - sum f p) + 2 z_coef / N lse p + the pair's gate gradient
 //   dn = dres + dl Wr, dWr = dl^T n
 //
-// The three products run on the bf16 matrix cores for every type: a value is cut into
-// bf16 pieces of 8 bits (fp16 into 2, fp32 into 3, exactly), and the pieces' products
-// above 2^-24 of the whole are added in fp32, so a bf16 router pays one instruction
-// where fp32 ones would take sixteen times as long. dl is fp32 and takes three pieces.
+// The three products run on the bf16 matrix cores for every type: a value is split into
+// bf16 pieces of 8 bits (fp16 into 2, fp32 into 3, exactly), and the pieces' products are added
+// in fp32, but for second by third ones: two of at most 2^-25 of the values' powers of two
+// (fp16 by fp32: one of 2^-24). So a bf16 router pays one instruction where fp32 ones would
+// take sixteen times as long. dl is fp32 and takes three pieces.
 //
 // Bound: HBM, by n (forward), and n, dres and dn (backward). bf16, us: 4096 tokens x 2048, 8
 // experts, forward 7.8 + 4.8 (sums), backward 22.7 + 4.3 (dWr's parts); 16411 x 4096, 64
@@ -41,14 +42,18 @@ struct BalanceP {
 
 template <int DT> constexpr int kPieces = DT == LC_FP32 ? 3 : DT == LC_FP16 ? 2 : 1;
 
-// x as P bf16 pieces, largest first: each takes the next 8 bits
+// x as P bf16 pieces, largest first. Three, of an fp32 value: each is what is left rounded to
+// nearest (values that round to infinity are cut), at most 2^-8, then 2^-17 of the value's
+// power of two; exact down to 2^-109, as the last one's step is 2^-133 at least. Two, of an fp16
+// value: the upper 8 bits and the rest, at most 2^-7.
 template <int P>
 __device__ __forceinline__ void split_bf16(float x, uint16_t (&out)[P]) {
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     const uint32_t u = __float_as_uint(x);
-    out[i] = (uint16_t)(u >> 16);
-    x = (u & 0x7F800000u) == 0x7F800000u ? 0.0f : x - __uint_as_float(u & 0xFFFF0000u);
+    if (P == 3 && (i > 0 || (u & 0x7FFFFFFFu) < 0x7F7F8000u)) out[i] = __builtin_bit_cast(uint16_t, (__bf16)x);
+    else out[i] = (uint16_t)(u >> 16);
+    x = (u & 0x7F800000u) == 0x7F800000u ? 0.0f : x - __uint_as_float((uint32_t)out[i] << 16);
   }
 }
 

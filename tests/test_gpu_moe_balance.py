@@ -421,3 +421,77 @@ def test_mixture_pass():
                                w=w, dw=dw, store_dwr=1)
     s = {"n": n.cpu(), "wr": wr.cpu(), "sel": sel.cpu(), "w": w.cpu(), "dw": dw.cpu(), "mask": None, "dres": torch.zeros(T, d)}
     check({"p": p, "lse": lse, "counts": counts, "loss": loss, "dn": dn, "dwr": dwr}, reference(s, E), d)
+
+
+# ------------------------------------------------------------------ values of more bits than bf16's
+
+def single(n, wr, T, d, E, n_dt, w_dt, x):
+    """dn and dwr of one dl: token 0 of its own, with N = 1, lse = x and probs 1 at expert 0, of z_coef 0.5
+    and coef 0: dl[0, 0] is x exactly, all others 0."""
+    p, lse = torch.zeros(T, E, device="cuda"), torch.zeros(T, device="cuda")
+    p[0, 0], lse[0] = 1.0, float(x)
+    counts = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    counts[E] = 1
+    dn, dwr = torch.empty(T, d, device="cuda"), torch.empty(E, d, device="cuda")
+    size = lc.lc_moe_balance_scratch_bytes(T, d, E)
+    sel = torch.tensor([0, 1], dtype=torch.int32).repeat(T, 1).cuda()
+    lc.lc_moe_balance_backward(T, d, E, n.cuda(), wr.cuda(), sel, p, lse, counts, 0.0, 0.5, dn, dwr,
+                               torch.empty(size, dtype=torch.uint8, device="cuda"), size, DT[n_dt][0], DT[w_dt][0], lc.LC_FP32,
+                               store_dwr=1)
+    return dn.cpu().double(), dwr.cpu().double()
+
+
+@pytest.mark.parametrize("n,w", [("fp32", "fp32"), ("fp32", "fp16"), ("fp16", "fp32"), ("fp16", "fp16"), ("fp32", "bf16"),
+                                 ("bf16", "fp32"), ("bf16", "bf16")])
+def test_products_keep_fp32(n, w):
+    """Single products (one value of n meets one of wr, or one dl): fp32's pieces, rounded to nearest,
+    leave out two products of 2^-8 by 2^-17 of the values' powers of two (by fp16's two pieces one of
+    2^-7 by 2^-17): 2^-24 of the product at most; then the
+    smaller pieces' sum is rounded at 2^-7 of the product or below, and the last addition to fp32's step
+    (2^-23, if it is not to nearest). So (1 + 2 + 2^-5) 2^-24; where pieces are cut, up to 7.9 are left out."""
+    T, d, E = 64, 64, 2
+    tol = (1 + 2 + 2.0 ** -5) * 2.0 ** -24
+    g = torch.Generator().manual_seed(3)
+    mk = lambda *s: 1 + torch.rand(*s, generator=g) * 0.999  # noqa: E731
+    value = {"fp32": 1.0078124, "fp16": 1.0068359375, "bf16": 1.0078125}  # (many low bits)
+    for turn in range(4):
+        nv = torch.full((d,), value[n]) if turn == 0 else mk(d)
+        wv = torch.full((d,), value[w]) if turn == 0 else mk(d)
+        nv, wv = nv.to(DT[n][1]), wv.to(DT[w][1])
+        # forward: token t has value t alone; expert 1's weights are 0. Logits of some hundreds, so that
+        # lse is the logit itself
+        N, W = torch.zeros(T, d, dtype=nv.dtype), torch.zeros(E, d, dtype=wv.dtype)
+        N[torch.arange(T), torch.arange(T)] = nv * 16
+        W[0] = wv * 16
+        s = {"n": N, "wr": W, "sel": torch.tensor([[0, 1]] * T, dtype=torch.int32), "mask": None, "w": None, "dw": None,
+             "dres": None}
+        o = call(s, E, n, w, pair=False)
+        want = nv.double() * wv.double() * 256
+        assert float(((o["lse"].cpu().double() - want).abs() / (tol * want)).max()) <= 1.0
+        # backward: dl = x, times wr and n
+        x = (1.0078124 if turn == 0 else mk(1)) * torch.ones(1)
+        N = torch.zeros(T, d, dtype=nv.dtype)
+        N[0] = nv
+        dn, dwr = single(N, W, T, d, E, n, w, x)
+        for got, other in ((dn[0], W[0].double()), (dwr[0], nv.double())):
+            want = float(x) * other
+            assert float(((got - want).abs() / (tol * want)).max()) <= 1.0
+        assert float(dn[1:].abs().max()) == 0 and float(dwr[1].abs().max()) == 0
+
+
+def test_largest_values():
+    """Values next to fp32's largest, whose nearest bf16 is infinite, times small ones."""
+    T, d, E = 3, 8, 2
+    top = torch.tensor([0x7F7FFFFF, 0x7F7F8000, 0x7F7F7FFF, 0x7F000001], dtype=torch.int32).view(torch.float32)
+    n, wr = torch.zeros(T, d), torch.zeros(E, d)
+    n[0, :4], n[1, :4] = top, -top
+    wr[0, :4] = top
+    dn, dwr = single(n, wr, T, d, E, "fp32", "fp32", 2.0 ** -20)
+    want = torch.zeros(E, d, dtype=torch.float64)
+    want[0, :4] = top.double() * 2.0 ** -20
+    assert torch.equal(dwr, want) and torch.equal(dn[0], want[0])
+    wr[0, :4] = torch.tensor([2.0 ** -120, 0, 0, 0])
+    s = {"n": n, "wr": wr, "sel": torch.tensor([[0, 1]] * T, dtype=torch.int32), "mask": None, "w": None, "dw": None,
+         "dres": None}
+    o = call(s, E, "fp32", "fp32", pair=False)
+    assert float(o["lse"][0]) == float(top[0].double() * 2.0 ** -120)
