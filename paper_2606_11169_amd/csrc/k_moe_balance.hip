@@ -42,18 +42,25 @@ struct BalanceP {
 
 template <int DT> constexpr int kPieces = DT == LC_FP32 ? 3 : DT == LC_FP16 ? 2 : 1;
 
-// x as P bf16 pieces, largest first. Three, of an fp32 value: each is what is left rounded to
-// nearest (values that round to infinity are cut), at most 2^-8, then 2^-17 of the value's
-// power of two; exact down to 2^-109, as the last one's step is 2^-133 at least. Two, of an fp16
-// value: the upper 8 bits and the rest, at most 2^-7.
+// a and b as P bf16 pieces each, largest first, in pairs (a low). Three, of fp32 values: each
+// is what is left rounded to nearest, at most 2^-8, then 2^-17 of the value's power of two;
+// exact down to 2^-109, as the last one's step is 2^-133 at least. (The first is clamped: what
+// rounds to infinity is cut.) Two, of fp16 values: the upper 8 bits and the rest, at most 2^-7.
+// A NaN of any payload, and in two or three pieces an infinity, leaves a NaN among the pieces.
 template <int P>
-__device__ __forceinline__ void split_bf16(float x, uint16_t (&out)[P]) {
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t (&out)[P]) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_v;
+  constexpr float MOST = 3.3895313892515355e38f;  // bf16's largest
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const uint32_t u = __float_as_uint(x);
-    if (P == 3 && (i > 0 || (u & 0x7FFFFFFFu) < 0x7F7F8000u)) out[i] = __builtin_bit_cast(uint16_t, (__bf16)x);
-    else out[i] = (uint16_t)(u >> 16);
-    x = (u & 0x7F800000u) == 0x7F800000u ? 0.0f : x - __uint_as_float((uint32_t)out[i] << 16);
+    if constexpr (P == 3) {
+      const float u = i == 0 ? __builtin_amdgcn_fmed3f(a, -MOST, MOST) : a, v = i == 0 ? __builtin_amdgcn_fmed3f(b, -MOST, MOST) : b;
+      out[i] = __builtin_bit_cast(uint32_t, bf16x2_v{(__bf16)u, (__bf16)v});
+    } else {
+      out[i] = (__float_as_uint(a) >> 16) | (__float_as_uint(b) & 0xFFFF0000u);
+    }
+    a -= __uint_as_float(out[i] << 16);
+    b -= __uint_as_float(out[i] & 0xFFFF0000u);
   }
 }
 
@@ -75,15 +82,17 @@ struct Raw8 {
     if constexpr (P == 1) {
       out[0] = __builtin_bit_cast(bf16x8_v, w[0]);
     } else {
-      typedef __attribute__((ext_vector_type(8))) uint16_t u16x8_v;
-      u16x8_v v[P];
+      u32x4_v v[P];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        float x;
-        if constexpr (DT == LC_FP32) x = __uint_as_float(w[c >> 2][c & 3]);
-        else x = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[0][c >> 1] >> (16 * (c & 1))));
-        uint16_t s[P];
-        split_bf16<P>(x, s);
+      for (int c = 0; c < 4; ++c) {
+        float x[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if constexpr (DT == LC_FP32) x[h] = __uint_as_float(w[c >> 1][2 * (c & 1) + h]);
+          else x[h] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[0][c] >> (16 * h)));
+        }
+        uint32_t s[P];
+        split_bf16<P>(x[0], x[1], s);
 #pragma unroll
         for (int i = 0; i < P; ++i) v[i][c] = s[i];
       }
@@ -401,20 +410,23 @@ __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void b
   for (int b = 0; b < 2 && !WL; ++b)
 #pragma unroll
     for (int k = 0; k < KE; ++k) {
-      typedef __attribute__((ext_vector_type(8))) uint16_t u16x8_v;
-      u16x8_v v[PW];
+      float x[8];
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         const int e = 32 * k + 8 * g + c, col = cw + colf + 4 * b;
-        float x = 0.0f;
+        x[c] = 0.0f;
         if (p.dn && e < p.E && col < p.d) {
           const int64_t at = (int64_t)e * p.d + col;
-          if constexpr (WD == LC_FP32) x = static_cast<const float *>(p.wr)[at];
-          else if constexpr (WD == LC_BF16) x = bf2f(static_cast<const bf16_t *>(p.wr)[at]);
-          else x = (float)static_cast<const _Float16 *>(p.wr)[at];
+          if constexpr (WD == LC_FP32) x[c] = static_cast<const float *>(p.wr)[at];
+          else if constexpr (WD == LC_BF16) x[c] = bf2f(static_cast<const bf16_t *>(p.wr)[at]);
+          else x[c] = (float)static_cast<const _Float16 *>(p.wr)[at];
         }
-        uint16_t s[PW];
-        split_bf16<PW>(x, s);
+      }
+      u32x4_v v[PW];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t s[PW];
+        split_bf16<PW>(x[2 * c], x[2 * c + 1], s);
 #pragma unroll
         for (int i = 0; i < PW; ++i) v[i][c] = s[i];
       }
@@ -518,20 +530,20 @@ __global__ __launch_bounds__(512, kPieces<ND> + kPieces<WD> == 2 ? 4 : 2) void b
       const float d0 = ok0 ? __uint_as_float((uint32_t)x.dw) : 0.0f, d1 = ok1 ? __uint_as_float((uint32_t)(x.dw >> 32)) : 0.0f;
       const float inner = w0 * d0 + w1 * d1, g0 = w0 * (d0 - inner), g1 = w1 * (d1 - inner);
       if (e4 < 16 * EF) {
-        uint16_t s[4][3];
+        float v[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const int e = e4 + c;
-          float v = pr[c] * (cb * (s_f[e] - dot) + z);
-          v += ok0 && e == e0 ? g0 : ok1 && e == e1 ? g1 : 0.0f;
-          if (!live || e >= p.E) v = 0.0f;
-          split_bf16<3>(v, s[c]);
+          v[c] = pr[c] * (cb * (s_f[e] - dot) + z);
+          v[c] += ok0 && e == e0 ? g0 : ok1 && e == e1 ? g1 : 0.0f;
+          if (!live || e >= p.E) v[c] = 0.0f;
         }
+        uint32_t s[2][3];
+        split_bf16<3>(v[0], v[1], s[0]);
+        split_bf16<3>(v[2], v[3], s[1]);
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
-          *reinterpret_cast<uint2 *>(&s_te[i][tl * LE + (e4 ^ 8 * (tl >> 2 & 1))]) =
-              make_uint2(s[0][i] | (uint32_t)s[1][i] << 16, s[2][i] | (uint32_t)s[3][i] << 16);
-        }
+        for (int i = 0; i < 3; ++i)
+          *reinterpret_cast<uint2 *>(&s_te[i][tl * LE + (e4 ^ 8 * (tl >> 2 & 1))]) = make_uint2(s[0][i], s[1][i]);
       }
     }
 #pragma unroll

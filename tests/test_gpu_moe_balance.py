@@ -495,3 +495,40 @@ def test_largest_values():
          "dres": None}
     o = call(s, E, "fp32", "fp32", pair=False)
     assert float(o["lse"][0]) == float(top[0].double() * 2.0 ** -120)
+
+
+def quiet(bits):
+    """An fp32 value of these bits."""
+    return torch.tensor([bits], dtype=torch.int32).view(torch.float32)
+
+
+@pytest.mark.parametrize("bits", [0x7F800001, 0x7F80FFFF, -0x7FFFFF, 0x7FC00000], ids=hex)
+def test_nan_of_any_payload(bits):
+    """A NaN of fp32 whose bits all lie below bf16's is a NaN in every result that it reaches."""
+    T, d, E = 70, 64, 8
+    s = inputs(T, d, E, "fp32", "fp32", 8)
+    a = call(s, E, "fp32", "fp32")
+    keep = torch.arange(T) != 10
+    # (values through integers: moving a signalling NaN as a float may quiet it)
+    s["n"].view(torch.int32)[10, 3] = bits
+    s["wr"][:, 3] = -s["wr"][:, 3].abs()  # as an infinity it would leave probabilities of 0
+    a = call({**s, "n": torch.where(torch.isnan(s["n"]), 0.0, s["n"])}, E, "fp32", "fp32")
+    b = call(s, E, "fp32", "fp32")
+    assert torch.equal(a["p"].cpu()[keep], b["p"].cpu()[keep]) and bool(torch.isnan(b["p"][10]).all())
+    assert bool(torch.isnan(b["loss"]).all()) and bool(torch.isnan(b["dn"][10]).all())
+    # given finite probs, n's NaN reaches dwr's column alone
+    size = lc.lc_moe_balance_scratch_bytes(T, d, E)
+    scratch, dwr = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty(E, d, device="cuda")
+    args = (T, d, E, s["n"].cuda(), s["wr"].cuda(), s["sel"].cuda(), a["p"], a["lse"], a["counts"], COEF, Z)
+    lc.lc_moe_balance_backward(*args, None, dwr, scratch, size, lc.LC_FP32, lc.LC_FP32, lc.LC_FP32, store_dwr=1)
+    assert bool(torch.isnan(dwr[:, 3]).all()) and not bool(torch.isnan(dwr[:, torch.arange(d) != 3]).any())
+    # a weight: expert 2's logits are NaN, not -inf
+    s = inputs(T, d, E, "fp32", "fp32", 8)
+    s["n"][:, 5] = s["n"][:, 5].abs() * (1 if bits < 0 else -1) - (0 if bits < 0 else 1e-3)
+    s["wr"].view(torch.int32)[2, 5] = bits
+    b = call(s, E, "fp32", "fp32")
+    assert bool(torch.isnan(b["p"]).all()) and bool(torch.isnan(b["lse"]).all())
+    dn = b["dn"]
+    lc.lc_moe_balance_backward(T, d, E, s["n"].cuda(), s["wr"].cuda(), s["sel"].cuda(), a["p"], a["lse"], a["counts"], COEF, Z,
+                               dn, None, None, 0, lc.LC_FP32, lc.LC_FP32, lc.LC_FP32)
+    assert bool(torch.isnan(dn[:, 5]).all()) and not bool(torch.isnan(dn[:, torch.arange(d) != 5]).any())
