@@ -569,7 +569,9 @@ lc_status lc_moe_dispatch(const lc_moe_args *args, void *stream);
  *   dwr_accum[e] += sum_t dl[t, e] n[t]              (fp32 [E, d]; stored if store_dwr is
  *                                                     1, and where N is 0 it is 0 or stays)
  * A token that does not count has dl = 0, whatever its values: what it holds reaches
- * no result, infinities and NaN included. A pair that is not placed carries no gradient
+ * no result, infinities and NaN included. In the forward an infinite value gives what the
+ * formula gives with it (an expert whose logits are -inf has probability 0); in the backward
+ * what an infinity of n, wr, w or dw reaches is infinite or NaN. A pair that is not placed carries no gradient
  * (a pair whose partner is not placed: with the partner's w and dw taken as 0).
  * Sums are fp32 and of fixed order (partial sums in `scratch`,
  * lc_moe_balance_scratch_bytes, no clearing needed). dn and dwr_accum may each be NULL.

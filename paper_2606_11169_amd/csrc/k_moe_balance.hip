@@ -76,6 +76,11 @@ struct Raw8 {
     for (int i = 0; i < W; ++i)
       w[i] = __builtin_bit_cast(u32x4_v, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(off + 16 * i), 0, 0));
   }
+  __device__ __forceinline__ float value(int c) const {
+    if constexpr (DT == LC_FP32) return __uint_as_float(w[c >> 2][c & 3]);
+    else if constexpr (DT == LC_BF16) return __uint_as_float(w[0][c >> 1] << 16 * (1 - (c & 1)) & 0xFFFF0000u);
+    else return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[0][c >> 1] >> 16 * (c & 1)));
+  }
   // as bf16 pieces
   __device__ __forceinline__ void pieces(bf16x8_v (&out)[kPieces<DT>]) const {
     constexpr int P = kPieces<DT>;
@@ -85,14 +90,8 @@ struct Raw8 {
       u32x4_v v[P];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        float x[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if constexpr (DT == LC_FP32) x[h] = __uint_as_float(w[c >> 1][2 * (c & 1) + h]);
-          else x[h] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[0][c] >> (16 * h)));
-        }
         uint32_t s[P];
-        split_bf16<P>(x[0], x[1], s);
+        split_bf16<P>(value(2 * c), value(2 * c + 1), s);
 #pragma unroll
         for (int i = 0; i < P; ++i) v[i][c] = s[i];
       }
@@ -239,7 +238,19 @@ __global__ __launch_bounds__(512) void balance_fwd_kernel(BalanceP p) {
 #pragma unroll
         for (int b = 0; b < EF; ++b) *place(wave - 4, a, b) = acc[a][b];
     }
-    __syncthreads();
+    constexpr bool MANY = kPieces<ND> + kPieces<WD> > 2;
+    int odd = 0;  // a NaN among the products
+    if constexpr (MANY) {
+#pragma unroll
+      for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int b = 0; b < EF; ++b)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) odd |= acc[a][b][c] != acc[a][b][c] ? 1 : 0;
+      odd = __syncthreads_or(odd);
+    } else {
+      __syncthreads();
+    }
     if (wave < 4) {
 #pragma unroll
       for (int a = 0; a < MT; ++a)
@@ -247,6 +258,32 @@ __global__ __launch_bounds__(512) void balance_fwd_kernel(BalanceP p) {
         for (int b = 0; b < EF; ++b) *place(wave, a, b) = acc[a][b] + *place(wave, a, b);
     }
     __syncthreads();
+    // Pieces leave a NaN where a value is infinite (times a piece of 0, or of the other sign):
+    // a wave for each such logit adds the values themselves. Once per tile at the most.
+    if constexpr (MANY) {
+      if (odd) {
+        for (int tl = 0; tl < rows; ++tl) {
+          if (p.mask && p.mask[t0 + tl] == 0) continue;
+          for (int e = wave; e < p.E; e += 8) {
+            const int at = tl * LD + e;
+            float v = sl[0][at] + sl[1][at] + sl[2][at] + sl[3][at];
+            if (v == v) continue;
+            v = 0.0f;
+            for (int k = 8 * lane; k < p.d; k += 512) {
+              Raw8<ND> x;
+              Raw8<WD> y;
+              x.load(rn, (uint32_t)(tl * p.d + k) * NS);
+              y.load(rw, (uint32_t)(e * p.d + k) * WS);
+#pragma unroll
+              for (int c = 0; c < 8; ++c) v = fmaf(x.value(c), y.value(c), v);
+            }
+            v = wave_sum(v);
+            if (lane < 4) sl[lane][at] = lane == 0 ? v : 0.0f;
+          }
+        }
+        __syncthreads();
+      }
+    }
     // 8 lanes per token, experts j, j + 8, ...
     const int j = tid & 7;
     for (int tl = tid >> 3; tl < TT; tl += 64) {

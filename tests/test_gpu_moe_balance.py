@@ -532,3 +532,46 @@ def test_nan_of_any_payload(bits):
     lc.lc_moe_balance_backward(T, d, E, s["n"].cuda(), s["wr"].cuda(), s["sel"].cuda(), a["p"], a["lse"], a["counts"], COEF, Z,
                                dn, None, None, 0, lc.LC_FP32, lc.LC_FP32, lc.LC_FP32)
     assert bool(torch.isnan(dn[:, 5]).all()) and not bool(torch.isnan(dn[:, torch.arange(d) != 5]).any())
+
+
+@pytest.mark.parametrize("n,w", [("bf16", "bf16"), ("bf16", "fp32"), ("fp16", "fp16"), ("fp32", "fp32"), ("fp32", "bf16"),
+                                 ("fp16", "fp32"), ("bf16", "fp16"), ("fp32", "fp16"), ("fp16", "bf16")])
+@pytest.mark.parametrize("E", [3, 40])
+def test_infinite_weights(E, n, w):
+    """An expert whose logits are -inf has probability 0, and the others what they have without it, in
+    every type; an infinite value of a token leaves its row NaN (inf - inf)."""
+    T, d = 90, 200
+    s = inputs(T, d, E, n, w, E)
+    s["n"][:, 7] = s["n"][:, 7].abs() + 0.125
+    s["n"][4, 7] = 1.0  # (a value of one bf16 piece)
+    s["wr"][1, 7] = -float("inf")
+    o = call(s, E, n, w)
+    keep = [e for e in range(E) if e != 1]
+    l = s["n"].double() @ s["wr"][keep].double().T
+    p, lse = torch.softmax(l, 1), torch.logsumexp(l, 1)
+    D = (d / 32 * 9 + 16) * 2.0 ** -24 * (s["n"].double().abs() @ s["wr"][keep].double().abs().T).amax(1, keepdim=True)
+    rel = torch.expm1(2 * D) + 2.0 ** -20
+    got = o["p"].cpu().double()
+    assert bool((got[:, 1] == 0).all()) and bool(((got[:, keep] - p).abs() <= rel * p + 2.0 ** -126).all())
+    assert bool(((o["lse"].cpu().double() - lse).abs() <= D[:, 0] + 2.0 ** -22 * (1 + lse.abs())).all())
+    s = inputs(T, d, E, n, w, E)
+    s["n"][4, 7] = float("inf")
+    o = call(s, E, n, w)
+    assert bool(torch.isnan(o["p"][4]).all()) and bool(torch.isfinite(o["p"][torch.arange(T) != 4]).all())
+
+
+def test_infinite_weights_in_the_backward():
+    """What an infinite weight reaches is not finite, and nothing else changes."""
+    T, d, E = 70, 64, 8
+    for n, w in (("bf16", "bf16"), ("fp32", "fp32"), ("fp16", "fp16"), ("bf16", "fp32")):
+        s = inputs(T, d, E, n, w, 8)
+        a = call(s, E, n, w)
+        s["wr"][2, 5] = float("inf")
+        size = lc.lc_moe_balance_scratch_bytes(T, d, E)
+        dn, dwr = torch.empty(T, d, device="cuda"), torch.empty(E, d, device="cuda")
+        lc.lc_moe_balance_backward(T, d, E, s["n"].cuda(), s["wr"].cuda(), s["sel"].cuda(), a["p"], a["lse"], a["counts"], COEF, Z,
+                                   dn, dwr, torch.empty(size, dtype=torch.uint8, device="cuda"), size, DT[n][0], DT[w][0],
+                                   lc.LC_FP32, w=s["w"].cuda(), dw=s["dw"].cuda(), store_dwr=1)
+        keep = torch.arange(d) != 5
+        assert not bool(torch.isfinite(dn[:, 5]).any())
+        assert torch.equal(dn[:, keep], a["dn"][:, keep]) and torch.equal(dwr, a["dwr"])
