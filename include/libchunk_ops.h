@@ -573,7 +573,7 @@ lc_status lc_moe_dispatch(const lc_moe_args *args, void *stream);
  * formula gives with it (an expert whose logits are -inf has probability 0); in the backward
  * what an infinity of n, wr, w or dw reaches is infinite or NaN. A pair that is not placed carries no gradient
  * (a pair whose partner is not placed: with the partner's w and dw taken as 0).
- * Sums are fp32 and of fixed order (partial sums in `scratch`,
+ * Sums are fp32, those of the losses from tile to tile of tokens fp64, and of fixed order (partial sums in `scratch`,
  * lc_moe_balance_scratch_bytes, no clearing needed). dn and dwr_accum may each be NULL.
  * n_dtype, w_dtype (wr), dn_dtype and dres_dtype: LC_FP32, LC_BF16 or LC_FP16. d a
  * multiple of 8, up to 2^20; 0 <= T < 2^30 (0: counts, loss and a stored dwr_accum are 0). Overlap:

@@ -170,7 +170,10 @@ __global__ __launch_bounds__(512) void balance_fwd_kernel(BalanceP p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int i16 = lane & 15, g = lane >> 4;
   if (tid < 65) scnt[tid] = 0;
-  float psum = 0.0f, zsum = 0.0f;  // thread e: the workgroup's sum of probs; thread 0: of lse^2
+  // thread e: the workgroup's sum of probs; thread 0: of lse^2. In 64 bits from tile to tile: a
+  // workgroup takes any number of them (in fp32 the losses of 2^24 like tokens were off by 530
+  // and 51 * 2^-24)
+  double psum = 0.0, zsum = 0.0;
   for (int64_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
     const int64_t t0 = tile * TT;
     f32x4_v acc[MT][EF];
@@ -341,9 +344,10 @@ __global__ __launch_bounds__(512) void balance_fwd_kernel(BalanceP p) {
     }
     __syncthreads();
     if (tid < 64) {
+      float v = 0.0f, z = 0.0f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) psum += sps[u][tid];
-      float z = 0.0f;
+      for (int u = 0; u < 8; ++u) v += sps[u][tid];
+      psum += v;
       for (int i = tid; i < TT; i += 64) z += sz[i];
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
@@ -353,7 +357,7 @@ __global__ __launch_bounds__(512) void balance_fwd_kernel(BalanceP p) {
   __syncthreads();  // counts
   if (gridDim.x == 1 && tid < 64) {  // a single workgroup finishes by itself
     const int c = scnt[tid], N = scnt[64];
-    double l = tid < p.E ? (double)psum * c : 0.0;
+    double l = tid < p.E ? psum * c : 0.0;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
     if (tid < p.E) p.counts[tid] = c;
@@ -367,11 +371,11 @@ __global__ __launch_bounds__(512) void balance_fwd_kernel(BalanceP p) {
   }
   float *const q = p.part + blockIdx.x;
   if (tid < p.E) {
-    q[tid * kFwdBlocks] = psum;
+    q[tid * kFwdBlocks] = (float)psum;
     q[(p.E + tid) * kFwdBlocks] = __int_as_float(scnt[tid]);
   }
   if (tid == 0) {
-    q[2 * p.E * kFwdBlocks] = zsum;
+    q[2 * p.E * kFwdBlocks] = (float)zsum;
     q[(2 * p.E + 1) * kFwdBlocks] = __int_as_float(scnt[64]);
   }
 }

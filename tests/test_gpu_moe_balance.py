@@ -575,3 +575,27 @@ def test_infinite_weights_in_the_backward():
         keep = torch.arange(d) != 5
         assert not bool(torch.isfinite(dn[:, 5]).any())
         assert torch.equal(dn[:, keep], a["dn"][:, keep]) and torch.equal(dwr, a["dwr"])
+
+
+@pytest.mark.parametrize("T", [1 << 24, (1 << 24) + 70001, 80, 700])
+def test_long_sums(T):
+    """Losses of many like tokens, against 64-bit sums of the probabilities and lse that the call itself
+    gives: a tile's at most 128 values are added in fp32 (waves of up to 16, then 8 waves: 24 roundings),
+    tiles in 64 bits, a workgroup's sums are rounded to fp32 once and so are lse^2 and the loss: 28
+    roundings of 2^-24, however many tokens there are."""
+    d, E = 8, 2
+    g = torch.Generator().manual_seed(5)
+    row, wr = torch.randn(d, generator=g).bfloat16().cuda(), torch.randn(E, d, generator=g).bfloat16().cuda()
+    n = row.repeat(T, 1)
+    p, lse = torch.empty(T, E, device="cuda"), torch.empty(T, device="cuda")
+    sel = torch.tensor([0, 1], dtype=torch.int32, device="cuda").repeat(T, 1)
+    sel[: T // 3] = torch.tensor([1, 7], dtype=torch.int32, device="cuda")
+    counts, loss = torch.zeros(E + 1, dtype=torch.int32, device="cuda"), torch.zeros(2, device="cuda")
+    size = lc.lc_moe_balance_scratch_bytes(T, d, E)
+    lc.lc_moe_balance_forward(T, d, E, n, wr, sel, p, lse, counts, loss, torch.empty(size, dtype=torch.uint8, device="cuda"),
+                              size, lc.LC_BF16, lc.LC_BF16)
+    assert counts.tolist() == [T - T // 3, T, T]
+    f = counts[:E].double() / (2 * T)
+    want = torch.stack([E * (f * p.double().sum(0)).sum() / T, (lse.double() ** 2).sum() / T]).cpu()
+    off = (loss.cpu().double() - want).abs() / (28 * 2.0 ** -24 * want)
+    assert float(off.max()) <= 1.0, off
