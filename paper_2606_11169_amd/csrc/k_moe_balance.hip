@@ -790,12 +790,17 @@ static lc_status balance_forward(const lc_moe_balance_args &a, hipStream_t s) {
   LC_TRY(check_balance(a, false));
   BalanceP p = balance_params(a);
   // Tokens per tile / 16: the least rounds of tiles over the compute units by a tile's
-  // expected time, which grows with its tokens and by 2 tokens' worth for its reads of Wr.
-  // Tiles of more than 32 tokens are for bf16 (the others' registers end there).
+  // expected time, which grows with its tokens and by 32 tokens' worth for its reads of Wr: every
+  // number of tokens up to 28672 then takes one round. Both sides, us (4096 x 64 experts, 2048 x
+  // 8), by this rule and by the fastest of 1, 2, 4 and 5: 10000 tokens (3) 36.7, 41.3 and 16.1, 17.1;
+  // 16411 (5) 51.8, 77.0 by 4 and 21.2, 25.2 by 1; 24000 (6) 71.6, 92.5 and 25.3, 28.4; 28000 (7) 85.1,
+  // 94.2 and 27.9, 31.6. (Above 16 experts 7 spills 10 to 49 registers, above 48 6 spills 31, nearly
+  // all of them outside the loop over d.) 8 is left out: 30000 tokens 109.2, by 4 95.5, and 30.5, by 4 32.3. Tiles of more than 32
+  // tokens are for bf16 (the others' registers end there).
   const bool wide = a.n_dtype == LC_BF16 && a.w_dtype == LC_BF16;
   int mt = 1;
   int64_t least = 0;
-  for (int m : {1, 2, 4, 5}) {
+  for (int m = 1; m <= 7; ++m) {
     if (m > 2 && !wide) break;
     const int64_t tiles = (a.T + 16 * m - 1) / (16 * m), time = (tiles + 255) / 256 * (m + 2);
     if (m == 1 || time < least) {
@@ -812,8 +817,11 @@ static lc_status balance_forward(const lc_moe_balance_args &a, hipStream_t s) {
           constexpr int ND = decltype(nd)::value, WD = decltype(wd)::value, EF = decltype(ef)::value;
           const dim3 grid((unsigned)nblk), threads(512);
           if constexpr (ND == LC_BF16 && WD == LC_BF16) {
+            if (mt == 3) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 3>), grid, threads, 0, s, p);
             if (mt == 4) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 4>), grid, threads, 0, s, p);
             if (mt == 5) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 5>), grid, threads, 0, s, p);
+            if (mt == 6) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 6>), grid, threads, 0, s, p);
+            if (mt == 7) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 7>), grid, threads, 0, s, p);
           }
           if (mt == 2) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 2>), grid, threads, 0, s, p);
           if (mt == 1) hipLaunchKernelGGL((balance_fwd_kernel<ND, WD, EF, 1>), grid, threads, 0, s, p);

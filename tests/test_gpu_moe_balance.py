@@ -599,3 +599,12 @@ def test_long_sums(T):
     want = torch.stack([E * (f * p.double().sum(0)).sum() / T, (lse.double() ** 2).sum() / T]).cpu()
     off = (loss.cpu().double() - want).abs() / (28 * 2.0 ** -24 * want)
     assert float(off.max()) <= 1.0, off
+
+
+@pytest.mark.parametrize("E", [7, 24, 40, 64])
+@pytest.mark.parametrize("T", [4097, 8193, 12289, 16385, 20481, 24577, 28673, 33000])
+def test_forward_tiles(T, E):
+    """Token counts next to each border between the forward's tile heights."""
+    d = 72
+    s = inputs(T, d, E, "bf16", "bf16", T + E, masked=T % 3 == 0)
+    check(call(s, E, "bf16", "bf16", dn="bf16"), reference(s, E, dres=False), d, "bf16")
