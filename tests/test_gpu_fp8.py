@@ -627,3 +627,88 @@ def test_product_of_infinite_rows():
         got = Cm.float().cpu()
         assert bool((got[3] == float("inf")).all()) and bool((got[5] == -float("inf")).all())
         assert bool(torch.isfinite(got[[i for i in range(T) if i not in (3, 5)]]).all())
+
+
+# ------------------------------------------------------------------ every tiling
+
+def kernel_names(call):
+    """Names of the kernels that call() runs."""
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA], acc_events=True) as prof:
+        call()
+        torch.cuda.synchronize()
+    return [e.key for e in prof.key_averages()]
+
+
+SPLIT, DIRECT, TILE, WIDE = "fp8_split_kernel", "fp8_direct_kernel", "fp8_tile_kernel", "fp8_wide_kernel"
+TILINGS = [
+    # the kernel, its last template arguments; groups; M, N, K (grouped k: rows in all)
+    ("bf16", DIRECT, "false>", None, 17, 40, 144), ("bf16", SPLIT, "32, 8>", None, 333, 600, 656),
+    ("bf16", SPLIT, "64, 4>", None, 130, 4101, 400), ("bf16", TILE, "128, 2, 2, 2>", None, 600, 2050, 144),
+    ("bf16", TILE, "128, 2, 2, 4>", None, 3100, 333, 400), ("bf16", TILE, "256, 4, 2, 2>", None, 2600, 3101, 144),
+    ("bf16", DIRECT, "false>", "rows", 17, 40, 144), ("bf16", SPLIT, "32, 8>", "rows", 333, 333, 144),
+    ("bf16", SPLIT, "64, 4>", "rows", 2100, 133, 144), ("bf16", TILE, "128, 2, 2, 2>", "rows", 2600, 333, 144),
+    ("bf16", TILE, "128, 2, 2, 4>", "rows", 2600, 333, 400), ("bf16", TILE, "256, 4, 2, 2>", "rows", 2600, 3101, 144),
+    ("bf16", DIRECT, "false>", "k", 17, 40, 144), ("bf16", SPLIT, "32, 8>", "k", 130, 133, 144),
+    ("bf16", SPLIT, "64, 4>", "k", 65, 1041, 144), ("bf16", TILE, "128, 2, 2, 2>", "k", 130, 2050, 144),
+    ("bf16", TILE, "128, 2, 2, 4>", "k", 600, 600, 560), ("bf16", TILE, "256, 4, 2, 2>", "k", 2600, 3101, 144),
+    ("fp32", DIRECT, "true>", None, 65, 3101, 144), ("fp32", SPLIT, "32, 8>", None, 65, 133, 144),
+    ("fp32", SPLIT, "64, 4>", None, 130, 4101, 400), ("fp32", WIDE, "2>", None, 1041, 4101, 144),
+    ("fp32", WIDE, "4>", None, 3100, 600, 144),
+    ("fp32", SPLIT, "32, 8>", "rows", 65, 133, 144), ("fp32", SPLIT, "64, 4>", "rows", 2100, 133, 144),
+    ("fp32", WIDE, "2>", "rows", 1041, 3101, 144), ("fp32", WIDE, "4>", "rows", 2600, 333, 144),
+    ("fp32", SPLIT, "32, 8>", "k", 65, 133, 144), ("fp32", SPLIT, "64, 4>", "k", 65, 2050, 144),
+    ("fp32", WIDE, "2>", "k", 333, 4101, 400), ("fp32", WIDE, "4>", "k", 130, 4101, 144),
+    ("fp16", DIRECT, "true>", None, 65, 3101, 144), ("fp16", SPLIT, "64, 4>", "rows", 2100, 133, 144),
+    ("fp16", WIDE, "2>", "rows", 1041, 3101, 144), ("fp16", WIDE, "4>", "k", 130, 4101, 144),
+]
+
+
+@pytest.mark.parametrize("kind", ["small", "real"])
+@pytest.mark.parametrize("c,kernel,form,mode,M,N,K", TILINGS, ids=str)
+def test_every_tiling(c, kernel, form, mode, M, N, K, kind):
+    """Each tiling that the rule takes, plain, by rows and by k (groups that all have rows, one empty
+    in the middle, rows or columns of no group behind), stored, and accumulated in fp32; it is the kernel
+    meant here that runs."""
+    n = M if mode == "rows" else K
+    lengths = [n // 3, 0, n - n // 3 - (5 if mode == "rows" else 0)]
+    G, off = (3, [0, lengths[0], lengths[0], sum(lengths)]) if mode else (0, [0, M])
+    grouped = {}
+    if mode == "k":
+        starts, K = [0, up(lengths[0], 128), up(lengths[0], 128)], lc.lc_fp8_padded_rows(K, G)
+    A, sa, va = operand(M, K, "e4m3", 1, 1, kind)
+    parts = [operand(N, K, "e4m3", 1, 10 + i, kind, 0.02) for i in range(G if mode == "rows" else 1)]
+    B, sb = torch.cat([p[0] for p in parts]), torch.cat([p[1] for p in parts])
+    if mode == "k":
+        used = torch.zeros(K, dtype=torch.bool)
+        for s, m in zip(starts, lengths):
+            used[s:s + m] = True
+        A[:, :K][:, ~used], va[:, ~used] = 0, 0
+    if mode:
+        grouped = dict(group_mode=lc.LC_GROUP_ROWS if mode == "rows" else lc.LC_GROUP_K, n_groups=G,
+                       group_offsets=torch.tensor(off, dtype=torch.int32, device="cuda"), group_stride_b=N * B.stride(0),
+                       group_stride_b_scale=parts[0][1].numel(), group_stride_c=M * (N + 5))
+    A, sa, B, sb, va = A.cuda(), sa.cuda(), B.cuda(), sb.cuda(), va.cuda()
+    vb = [p[2].cuda() for p in parts]
+    for epi in ("store", "accum") if c == "fp32" else ("store",):
+        Cm = torch.full((G if mode == "k" else 1, M, N + 5), 3.0, dtype=DT[c][1], device="cuda")
+
+        def call():
+            lc.lc_gemm_fp8(lc.LC_EPI_ACCUM_F32 if epi == "accum" else lc.LC_EPI_STORE, M, N, K, A, A.stride(0), sa,
+                           sa.stride(0), B, B.stride(0), sb, sb.stride(0), Cm, N + 5, c_dtype=DT[c][0], b_block_rows=1,
+                           **grouped)
+
+        names = [k for k in kernel_names(call) if "fp8_" in k]
+        assert len(names) == 1 and kernel in names[0] and names[0].split("(lc::")[0].endswith(form), names
+        add = 3.0 if epi == "accum" else 0.0
+        for i in range(max(1, G)):
+            if mode == "k":
+                x, y, got, k = va[:, starts[i]:starts[i] + lengths[i]], vb[0][:, starts[i]:starts[i] + lengths[i]], Cm[i], lengths[i]
+            elif mode == "rows":
+                x, y, got, k = va[off[i]:off[i + 1]], vb[i], Cm[0, off[i]:off[i + 1]], K
+            else:
+                x, y, got, k = va, vb[0], Cm[0], K
+            if x.shape[0]:
+                check_product(got[:, :N], (x @ y.T + add).cpu(), (x.abs() @ y.abs().T + add).cpu(), c, k, kind)
+        assert bool((Cm[:, :, N:] == 3.0).all())
+        if mode == "rows":
+            assert bool((Cm[0, off[-1]:] == 3.0).all())
