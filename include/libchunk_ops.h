@@ -191,7 +191,7 @@ int64_t lc_fp8_padded_rows(int64_t T, int32_t n_groups);
  *                  zeros follow up to the next multiple of 128. K: the columns of
  *                  both operands (lc_fp8_padded_rows; what offsets reach past it
  *                  is left out). An empty group's C is 0 (accumulated: as it was);
- *                  STORE, STORE_F32 or ACCUM_F32.
+ *                  STORE, STORE_F32 or ACCUM_F32. The groups' C do not overlap.
  * K, lda, ldb and group_stride_b are multiples of 16 (a row's values between its own
  * length and K are zeros, as lc_fp8_quantize leaves them), ld_a_scale and ld_b_scale of
  * 4. Any M >= 0 (0: nothing happens) and N >= 1, each below 2^30; K below 2^30, lda

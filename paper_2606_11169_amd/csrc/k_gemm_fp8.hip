@@ -148,6 +148,13 @@ static lc_status check_gemm_fp8(const lc_gemm_fp8_args &a) {
         return fail(LC_ERR_INVALID_ARG, "gemm fp8: bad group stride of B or its scales");
     } else if (a.group_stride_c < 0 || a.group_stride_c > FAR) {
       return fail(LC_ERR_INVALID_ARG, "gemm fp8: bad group_stride_c");
+    } else if (a.group_stride_c < (a.M - 1) * a.ldc + a.N) {
+      // groups not one behind the other: rows of two, `far` elements apart, must not meet
+      for (int64_t g = 1; g < a.n_groups; ++g) {
+        const int64_t far = g * a.group_stride_c, rows = far / a.ldc, rest = far % a.ldc;
+        if ((rows < a.M && rest < a.N) || (rows + 1 < a.M && a.ldc - rest < a.N))
+          return fail(LC_ERR_INVALID_ARG, "gemm fp8: the groups' results overlap (group_stride_c)");
+      }
     }
   }
   return LC_OK;

@@ -134,3 +134,26 @@ def test_packed_arguments_have_the_structs_layout():
         values = [i + 1 for i in range(len(cls._fields_))]
         got = cls.from_buffer_copy(packed.pack(*values))
         assert [getattr(got, f[0]) for f in cls._fields_] == values
+
+
+@pytest.mark.parametrize("over,want", [
+    (dict(group_stride_c=0), BAD), (dict(group_stride_c=199), BAD), (dict(group_stride_c=200), BAD),
+    (dict(group_stride_c=99 * 200 + 199), BAD), (dict(group_stride_c=99 * 200 + 200, M=0), OK),
+    (dict(group_stride_c=0, n_groups=1, M=0), OK),
+    # side by side in wider rows: three groups of 200 columns in rows of 600, not of 599; by whole rows
+    (dict(group_stride_c=200, ldc=600, M=0), OK), (dict(group_stride_c=200, ldc=599), BAD),
+    (dict(group_stride_c=600, ldc=200), BAD), (dict(group_stride_c=700, ldc=400), BAD)], ids=str)
+def test_groups_of_k_do_not_overlap(over, want):
+    """Results of two groups in one place would be written in any order."""
+    assert status_of(lc.lc_gemm_fp8, **{**GEMM, **KGRP, **over}) == want
+
+
+def test_groups_of_k_overlap_as_counted():
+    """The refusal against every element's place, for small sizes (what
+    is not refused goes on to the launch, which fails without a GPU)."""
+    for M, N, ldc, G in ((3, 16, 16, 3), (3, 16, 40, 2), (4, 20, 50, 3), (1, 16, 16, 2), (5, 16, 35, 2)):
+        for stride in range(0, (M + 1) * ldc, 3):
+            places = [g * stride + m * ldc + n for g in range(G) for m in range(M) for n in range(N)]
+            got = status_of(lc.lc_gemm_fp8, **{**GEMM, **KGRP, "M": M, "N": N, "ldc": ldc, "n_groups": G, "ld_a_scale": 8,
+                                               "ld_b_scale": 4, "b_block_rows": 128, "group_stride_c": stride})
+            assert (got == BAD) == (len(set(places)) < len(places)), (M, N, ldc, G, stride)
