@@ -187,7 +187,8 @@ int64_t lc_fp8_padded_rows(int64_t T, int32_t n_groups);
  *                  STORE_F32 or ACCUM_F32. Rows of no group are not written.
  *   LC_GROUP_K     C + g*group_stride_c receives the sum over the columns of group g
  *                  in the column layout of lc_fp8_quantize: columns P(g) to P(g) +
- *                  its length of both operands, with group_offsets as given there;
+ *                  its length of both operands, with group_offsets as given there, all
+ *                  within [0, T] (T, where that call cuts them off, is not known here);
  *                  zeros follow up to the next multiple of 128. K: the columns of
  *                  both operands (lc_fp8_padded_rows; what offsets reach past it
  *                  is left out). An empty group's C is 0 (accumulated: as it was);
