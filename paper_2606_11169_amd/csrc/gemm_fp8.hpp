@@ -20,7 +20,6 @@ struct Fp8P {
   int gmode, ngroups;
   int goff_max;        // offsets end there: M (grouped rows) or K
   int epi, c_dt, r_dt;
-  int walk;            // tile rows of a group of the tile walk (MAP)
   int store16;         // STORE of 16-bit values
 };
 
@@ -45,7 +44,7 @@ struct Fp8Tile {
 // offsets are read with a lane per group (at most 64). Grouped rows: the row tiles of
 // the groups one after the other, all columns of one first. MAP: workgroups are dealt
 // to the 8 XCDs in turn, so XCD x takes the x-th eighth of the tiles, walked in groups
-// of p.walk tile rows: neighbours share rows of A and columns of B in its L2. (Selects
+// of WALK tile rows: neighbours share rows of A and columns of B in its L2. (Selects
 // instead of branches throughout: behind divergent branches the kernels' loops are
 // compiled with vector registers for what is uniform, and the 256 tile spills: 4096 x
 // 11008 x 4096 605 us, without spills 145.)
@@ -53,9 +52,14 @@ __device__ __forceinline__ uint32_t fp8_xcd_tile(uint32_t wg, uint32_t n) {
   const uint32_t x = wg & 7u;
   return x * (n >> 3) + min(x, n & 7u) + (wg >> 3);
 }
+// Of 1 to 6 and 8 tile rows 4 is within 1% of the fastest, at odd and even numbers of tile
+// columns (2048 x 2176 x 4096 alone 4%: 25.6 us by 1, 26.6), us by 1, 3, 4, 8: 4096 x 11008 x 4096 (43 columns of 256) 152, 145, 144, 144;
+// 4096 x 11264 x 4096 (44) 154, 146, 143, 144; 4096 x 4352 x 4096 (17) 100, 86, 85, 85; 8192 x 8192
+// x 1024 (32) 77, 71, 70, 80; in fp32 4096 x 4224 x 4096 (33 of 128) 134, 128, 127, 127.
 __device__ __forceinline__ void fp8_walk(const Fp8P &p, uint32_t wg, uint32_t &tm, uint32_t &tn) {
-  const uint32_t per = (uint32_t)p.walk * (uint32_t)p.tiles_n, first = wg / per * (uint32_t)p.walk;
-  const uint32_t rows = min((uint32_t)p.tiles_m - first, (uint32_t)p.walk);
+  constexpr uint32_t WALK = 4;
+  const uint32_t per = WALK * (uint32_t)p.tiles_n, first = wg / per * WALK;
+  const uint32_t rows = min((uint32_t)p.tiles_m - first, WALK);
   tm = first + wg % per % rows;
   tn = wg % per / rows;
 }
@@ -277,7 +281,6 @@ template <int BM, int BN>
 lc_status fp8_grid(Fp8P &p, uint32_t *grid) {
   p.tiles_m = (p.M + BM - 1) / BM;
   p.tiles_n = (p.N + BN - 1) / BN;
-  p.walk = (p.tiles_n & 1) ? 3 : 4;
   // grouped rows: each group may add a partial tile
   const int64_t rows = (int64_t)p.tiles_m + (p.gmode == LC_GROUP_ROWS ? p.ngroups : 0);
   int64_t n = rows * p.tiles_n;
