@@ -53,9 +53,10 @@ __device__ __forceinline__ uint32_t fp8_xcd_tile(uint32_t wg, uint32_t n) {
   return x * (n >> 3) + min(x, n & 7u) + (wg >> 3);
 }
 // Of 1 to 6 and 8 tile rows 4 is within 1% of the fastest, at odd and even numbers of tile
-// columns (2048 x 2176 x 4096 alone 4%: 25.6 us by 1, 26.6), us by 1, 3, 4, 8: 4096 x 11008 x 4096 (43 columns of 256) 152, 145, 144, 144;
-// 4096 x 11264 x 4096 (44) 154, 146, 143, 144; 4096 x 4352 x 4096 (17) 100, 86, 85, 85; 8192 x 8192
-// x 1024 (32) 77, 71, 70, 80; in fp32 4096 x 4224 x 4096 (33 of 128) 134, 128, 127, 127.
+// columns (2048 x 2176 x 4096 alone 4%: 25.6 us by 1, 26.6). us by 1, 3, 4, 8: 4096 x 11008 x 4096
+// (43 columns of 256) 152, 145, 144, 144; 4096 x 11264 x 4096 (44) 154, 146, 143, 144; 4096 x 4352 x
+// 4096 (17) 100, 86, 85, 85; 8192 x 8192 x 1024 (32) 77, 71, 70, 80; in fp32 4096 x 4224 x 4096 (33
+// of 128) 134, 128, 127, 127.
 __device__ __forceinline__ void fp8_walk(const Fp8P &p, uint32_t wg, uint32_t &tm, uint32_t &tn) {
   constexpr uint32_t WALK = 4;
   const uint32_t per = WALK * (uint32_t)p.tiles_n, first = wg / per * WALK;

@@ -205,8 +205,10 @@ static const Fp8Tiling *pick(const lc_gemm_fp8_args &a, bool f32) {
     if (i > 0 && most > INT32_MAX - 8 * 64) continue;
     // Grouped: every workgroup first reads the offsets and looks its tile up. In ns per 256
     // tiles of 16, per further round of the others; fitted with 940 grouped products of up to 32
-    // groups, where the choice then costs 4% over the fastest on the mean (without 8 and 17%:
-    // 52 rows x 12634, K 320, 32 groups 41 us by 16, 9 by 128).
+    // groups, the first and the last with rows and those between empty, where the choice then costs
+    // 4% over the fastest on the mean (without 8 and 17%: 52 rows x 12634, K 320, 32 groups 41 us by
+    // 16, 9 by 128). Groups that all have rows were not in the fit: 8187 rows x 2816 x 2048 of eight
+    // take 128, where 256 is faster: 1023 or 1026 rows each 55.8 us, 52.1; 100 to 2000 56.9, 52.1.
     double look = 0.0;
     if (a.group_mode != LC_GROUP_NONE) {
       const double rounds = (double)most / (v.tile == 16 ? 256 : v.slots);

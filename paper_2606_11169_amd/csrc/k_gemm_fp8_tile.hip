@@ -18,10 +18,11 @@
 // every fragment is read once per stage and none is held twice. The stage's barrier sits
 // in the middle: its own reads are done, the next stage's may begin.
 //
-// Bound: the matrix cores, under the chip's power. 4096 x 11008 x 4096, bf16 out: 143 us,
-// 2.58 PFLOP/s (a loop of these instructions alone reaches 4.4). 8187 rows of eight experts x
-// 2816 x 2048: 54 us, 1.76, and their weight gradients 57, 1.65: 2048 of k are 16 stages
-// beside a tile's start and end, and the last round of tiles is not full.
+// Bound: the matrix cores, under the chip's power. 4096 x 11008 x 4096, bf16 out: 142 us,
+// 2.60 PFLOP/s (a loop of these instructions alone reaches 4.4). 2048 of k are 16 stages beside a
+// tile's start and end, and the last round of tiles is not full: 8187 rows of eight experts x 2816 x
+// 2048 55 us (1023 or 1026 rows each), 57 (100 to 2000), 54 (two with 5102 and 3085, six with none),
+// 1.66 to 1.74 PFLOP/s; their weight gradients 59, 57 and 55.
 #include "gemm_fp8.hpp"
 
 namespace lc {
@@ -298,7 +299,9 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_tile_kernel(Fp8P p, uint32_t
 // stage is multiplied in two steps, the pieces at 0 and at 64, and while one multiplies the
 // other's are read. A step is two products of 32 k: 8 values of each lane. Bound: the
 // conversions, two (of two values each) beside every product, which then takes 30 cycles
-// instead of 16: 3001 x 1155 x 1872 22.4 us, 0.58 PFLOP/s.
+// instead of 16: 3001 x 1155 x 1872 22.5 us, 0.58 PFLOP/s; 4096 x 11008 x 4096 297 us, 1.24, in fp16
+// 287, accumulated 363 (C, 180 MB, is read too; the bf16 product of lc_gemm accumulates in 334);
+// the eight experts' weight gradients (1023 or 1026 rows each) 103, accumulated 175 (lc_gemm 146).
 template <int FA, int FB, int D>
 __global__ __launch_bounds__(256) void fp8_wide_kernel(Fp8P p, uint32_t first) {
   constexpr int BT = 128, FM = 4, FN = 4;

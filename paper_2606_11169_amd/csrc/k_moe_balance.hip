@@ -13,9 +13,10 @@
 // take sixteen times as long. dl is fp32 and takes three pieces.
 //
 // Bound: HBM, by n (forward), and n, dres and dn (backward). bf16, us: 4096 tokens x 2048, 8
-// experts, forward 7.8 + 4.8 (sums), backward 22.7 + 4.3 (dWr's parts); 16411 x 4096, 64
-// experts, 54.6 + 4.8 (2.5 TB/s of n; 8 experts 3.7, where a large sum reads 4.0) and 106.8 +
-// 6.8 (3.8 TB/s; 8 experts 4.7).
+// experts, forward 7.1 + 3.0 (sums), backward 21.9 + 4.2 (dWr's parts); 16411 x 4096, 64 experts,
+// 52.3 + 5.3 (n at 2.6 TB/s) and 100.8 + 6.3 (reads and writes past L2, each column chunk's
+// probs among them, at 4.8 TB/s, a copy's rate; of 4096 x 2048 at 4.1). 8192 tokens x 4096, 64
+// experts, forward and backward with fp32 n and Wr 68, 114, fp16 36, 106, bf16 33, 93.
 #include "common.hpp"
 #include "lds_dma.hpp"
 
@@ -262,7 +263,8 @@ __global__ __launch_bounds__(512) void balance_fwd_kernel(BalanceP p) {
     }
     __syncthreads();
     // Pieces leave a NaN where a value is infinite (times a piece of 0, or of the other sign):
-    // a wave for each such logit adds the values themselves. Once per tile at the most.
+    // a wave for each such logit adds the values themselves. (8192 tokens x 4096, 64 experts, fp32:
+    // 70 us, one token of NaN 114, all of them 600.)
     if constexpr (MANY) {
       if (odd) {
         for (int tl = 0; tl < rows; ++tl) {
